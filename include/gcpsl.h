@@ -437,6 +437,109 @@ typedef struct gcpsl_kernel_stat {
 int gcpsl_timing(gcpsl_ctx *ctx, int32_t on);
 int gcpsl_timing_read(gcpsl_ctx *ctx, gcpsl_kernel_stat *out, int32_t cap, int32_t *n);
 
+/*
+ * Operators on caller-owned tensors, without a context: layers over rows
+ * grouped by cluster, dropout and label scores.  They serve what surrounds a
+ * round and has no fixed batch: evaluating the fused model, or training one
+ * layer per cluster, on all n_n examples of every cluster at once.
+ *
+ * A tensor [rows][cols] is given by its first element and the elements
+ * between its rows (0 <= ld < 2^31; an output's rows must not overlap); a
+ * row's elements are consecutive and any element alignment will do (16-byte
+ * aligned rows are read fastest).  dtype GCPSL_F32 or GCPSL_BF16 is the type
+ * of the activations and weights; biases, weight gradients and scores are
+ * fp32, and so are all sums; a result is rounded once.  Outputs must not
+ * overlap inputs unless said otherwise.  Every call is asynchronous on
+ * `stream`, allocates nothing and reads nothing on the host but its
+ * arguments, so that it may be captured in a graph.  No rows is a valid
+ * call.  EINVAL on a bad argument, EUNSUPPORTED where one launch would need
+ * more than 2^31 workgroups, EHIP on a failed launch.
+ *
+ * Grouped rows: offsets is a device array [G + 1], 1 <= G <= 1024; rows
+ * [offsets[g], offsets[g + 1]) belong to group g, 0 <= offsets[0] <= ... <=
+ * offsets[G] <= rows; a group may have none.  Rows outside every group are
+ * not written.  (Offsets outside [0, rows] are taken as the nearest bound,
+ * so no offsets make a call touch memory outside its tensors; where they
+ * decrease, which rows are written is unspecified.)  Weights of group g are
+ * [n][k] at w + g w_gs, biases [n] at bias + g bias_gs (bias may be NULL); a
+ * stride of 0 gives every group the same ones.  1 <= n, k <= 2^28.
+ *
+ * Dropout: element (r, j) of a [rows][cols] tensor is kept if its 16-bit
+ * draw is at least t = rint(65536 p), 0 <= p <= 65535/65536, and then
+ * multiplied by 65536 / (65536 - t); otherwise it is 0 whatever it held.
+ * The draw is bits [16 (j mod 4), + 16) of output number r ceil(cols / 4) +
+ * floor(j / 4) of SplitMix64 from state mix64(seed + 0x44524F50): a function
+ * of seed, row and column alone, so that no mask is stored.  Layers and
+ * rounds that are to drop independently take seeds of their own.
+ */
+
+/* y_r = dropout(relu(W_g x_r + b_g)) for every row r of every group g: x
+ * [rows][k], y [rows][n].  relu 0 leaves the ReLU out (a NaN passes through
+ * it), p 0 the dropout. */
+int gcpsl_group_forward(int32_t dtype, int32_t G, int64_t rows, int32_t n, int32_t k, const int32_t *offsets,
+                        const void *x, int64_t ldx, const void *w, int64_t w_gs, const float *bias, int64_t bias_gs,
+                        int32_t relu, double p, uint64_t seed, void *y, int64_t ldy, void *stream);
+
+/* dx_r = W_g^T dy_r: dy [rows][n], dx [rows][k].  With gate [rows][k] (the
+ * layer's input, itself the result of a ReLU and a dropout of probability p),
+ * the gradient through those: dx is multiplied by dropout's 65536 / (65536 -
+ * t) where gate > 0 and 0 elsewhere.  gate NULL needs p 0. */
+int gcpsl_group_input_grad(int32_t dtype, int32_t G, int64_t rows, int32_t n, int32_t k, const int32_t *offsets,
+                           const void *dy, int64_t lddy, const void *w, int64_t w_gs, const void *gate,
+                           int64_t ldgate, double p, void *dx, int64_t lddx, void *stream);
+
+/* dW_g = sum over the rows r of group g of dy_r x_r^T, [n][k] fp32 at dw + g
+ * dw_gs; db_g = sum of dy_r, [n] at db + g db_gs (db may be NULL); both zero
+ * for a group without rows (dw_gs >= n k and db_gs >= n if G > 1).  The
+ * summation order depends on G, rows, n, k and the group's count only: the
+ * same call gives the same bits.  workspace: gcpsl_group_workspace_bytes()
+ * bytes on the device, 16-byte aligned (NULL if that is 0), used until the
+ * call's work on the stream is done. */
+int gcpsl_group_workspace_bytes(int32_t dtype, int32_t G, int64_t rows, int32_t n, int32_t k, size_t *bytes);
+int gcpsl_group_weight_grad(int32_t dtype, int32_t G, int64_t rows, int32_t n, int32_t k, const int32_t *offsets,
+                            const void *dy, int64_t lddy, const void *x, int64_t ldx, float *dw, int64_t dw_gs,
+                            float *db, int64_t db_gs, void *workspace, size_t workspace_bytes, void *stream);
+
+/* y = dropout(x), both [rows][cols], cols <= 2^28; y may be x (ldy = ldx).  The gradient
+ * is the same call on dy with the same seed. */
+int gcpsl_dropout(int32_t dtype, int64_t rows, int64_t cols, const void *x, int64_t ldx, double p, uint64_t seed,
+                  void *y, int64_t ldy, void *stream);
+
+/*
+ * Scores of rows of logits z [rows][L]: with m the row's maximum,
+ *   lse      log sum_c exp(z_c) = m + log sum_c exp(z_c - m)
+ *   logp     z_y - lse of the row's label y = labels[r]; 0 for a label outside
+ *            [0, L) (a row without one)
+ *   entropy  -sum_c p_c log p_c, p = softmax(z)
+ *   top_class, top_logp [rows][top]: the `top` classes of largest logit in
+ *            decreasing order, of equal logits the lower class first (a NaN
+ *            counts as the largest), and their log probabilities;
+ *            0 <= top <= min(L, 32), 1 <= L <= 2^28.
+ * Logits of -inf rule classes out: they add nothing anywhere.  A row of -inf
+ * only has lse -inf, entropy 0 and log probabilities of -inf; a row that holds
+ * a NaN or +inf has NaN for all three.  logp, entropy and lse may be NULL
+ * (labels too if logp is).  workspace: gcpsl_score_workspace_bytes() bytes on
+ * the device, 16-byte aligned (NULL if that is 0), used until the call's work
+ * on the stream is done.
+ */
+int gcpsl_score_workspace_bytes(int32_t dtype, int64_t rows, int32_t L, int32_t top, size_t *bytes);
+int gcpsl_score(int32_t dtype, int64_t rows, int32_t L, const void *z, int64_t ldz, const int32_t *labels,
+                int32_t top, float *logp, float *entropy, float *lse, float *top_logp, int32_t *top_class,
+                void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Gradient of the scores by the logits: with g_logp and g_entropy [rows] the
+ * loss's gradients by logp and entropy (either may be NULL),
+ *   dz_c = g_logp (1[c = y] - p_c) - g_entropy p_c (log p_c + entropy),
+ * p_c = exp(z_c - lse), lse and entropy as gcpsl_score gave them (entropy
+ * only where g_entropy is given).  A row without a label takes no gradient
+ * from logp.  A row whose lse is below -1e30, all its classes ruled out by
+ * -inf or the type's lowest values, has gradient 0.  dz may be z (lddz = ldz).
+ */
+int gcpsl_score_grad(int32_t dtype, int64_t rows, int32_t L, const void *z, int64_t ldz, const int32_t *labels,
+                     const float *lse, const float *entropy, const float *g_logp, const float *g_entropy, void *dz,
+                     int64_t lddz, void *stream);
+
 /* Release the context (host metadata only; device memory is the caller's;
  * a context of gcpsl_create_static releases its device's static workspace). */
 void gcpsl_destroy(gcpsl_ctx *ctx);

@@ -15,6 +15,7 @@
 
 #define GCPSL_TAG_ASSIGN 0x41535349474Eull
 #define GCPSL_TAG_SAMPLE 0x53414D504C45ull
+#define GCPSL_TAG_DROP 0x44524F50ull
 #define GCPSL_GOLDEN 0x9E3779B97F4A7C15ull
 
 __host__ __device__ __forceinline__ uint64_t gc_mix64(uint64_t z) {

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from typing import NamedTuple
 
 import numpy as np
 
@@ -29,6 +30,8 @@ EXPORTS = ["gcpsl_param_count", "gcpsl_state_count", "gcpsl_workspace_bytes", "g
            "gcpsl_fuse_replicas", "gcpsl_fuse_partial", "gcpsl_fuse_finalise",
            "gcpsl_participation", "gcpsl_batch_deviation", "gcpsl_payload",
            "gcpsl_cluster_sizes", "gcpsl_tensor", "gcpsl_timing", "gcpsl_timing_read",
+           "gcpsl_group_forward", "gcpsl_group_input_grad", "gcpsl_group_workspace_bytes", "gcpsl_group_weight_grad",
+           "gcpsl_dropout", "gcpsl_score_workspace_bytes", "gcpsl_score", "gcpsl_score_grad",
            "gcpsl_destroy", "gcpsl_last_error"]
 
 
@@ -97,6 +100,16 @@ def lib():
     L.gcpsl_tensor.argtypes = [vp, C.c_char_p, P(vp), P(i64), P(i32)]
     L.gcpsl_timing.argtypes = [vp, i32]
     L.gcpsl_timing_read.argtypes = [vp, P(KernelStat), i32, P(i32)]
+    f64, size = C.c_double, C.c_size_t
+    group = [i32, i32, i64, i32, i32, vp]  # dtype, G, rows, n, k, offsets
+    L.gcpsl_group_forward.argtypes = group + [vp, i64, vp, i64, vp, i64, i32, f64, u64, vp, i64, vp]
+    L.gcpsl_group_input_grad.argtypes = group + [vp, i64, vp, i64, vp, i64, f64, vp, i64, vp]
+    L.gcpsl_group_workspace_bytes.argtypes = group[:5] + [P(size)]
+    L.gcpsl_group_weight_grad.argtypes = group + [vp, i64, vp, i64, vp, i64, vp, i64, vp, size, vp]
+    L.gcpsl_dropout.argtypes = [i32, i64, i64, vp, i64, f64, u64, vp, i64, vp]
+    L.gcpsl_score_workspace_bytes.argtypes = [i32, i64, i32, i32, P(size)]
+    L.gcpsl_score.argtypes = [i32, i64, i32, vp, i64, vp, i32, vp, vp, vp, vp, vp, vp, size, vp]
+    L.gcpsl_score_grad.argtypes = [i32, i64, i32, vp, i64, vp, vp, vp, vp, vp, vp, i64, vp]
     L.gcpsl_destroy.argtypes = [vp]
     L.gcpsl_destroy.restype = None
     L.gcpsl_last_error.restype = C.c_char_p
@@ -169,6 +182,234 @@ def fuse_replicas(theta, weights, stream=None):
         raise ValueError("weights must have one entry per replica")
     _check(lib().gcpsl_fuse_replicas(C.c_void_p(theta.data_ptr()), theta.shape[0], theta.shape[1], _i64p(w),
                                      _stream(stream)))
+
+
+# ------------------------------------------ operators on tensors, without a context
+#
+# Tensors are on one GPU, rows of consecutive elements (any row stride).  Every
+# function returns the tensors it wrote: those given as out, dw, db, or new
+# ones.  stream: a torch stream, the current one by default; what is newly
+# allocated for another stream is marked as used there.
+
+def _rows(t, what, dtype=None, shape=None):
+    """(address, row stride) of a [rows][cols] tensor."""
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{what} must be a [rows][cols] tensor on the GPU")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{what} must be {dtype}, is {t.dtype}")
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{what} must be {shape}, is {tuple(t.shape)}")
+    rows, cols = t.shape
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError(f"{what}: a row's elements must be consecutive")
+    return t.data_ptr(), (ld if rows > 1 else cols)
+
+
+def _type(t):
+    import torch
+    code = {torch.float32: 0, torch.bfloat16: 1}.get(t.dtype)
+    if code is None:
+        raise ValueError(f"fp32 or bf16 tensors only, not {t.dtype}")
+    return code
+
+
+def _vector(t, what, dtype, n, like):
+    """Address of a vector of n elements, 0 for None."""
+    if t is None:
+        return 0
+    if t.dtype != dtype or tuple(t.shape) != (n,) or not t.is_contiguous() or t.device != like.device:
+        raise ValueError(f"{what} must be a contiguous {dtype} vector of {n} on {like.device}")
+    return t.data_ptr()
+
+
+def _offsets(t, like):
+    import torch
+    if t.dim() != 1 or t.shape[0] < 2:
+        raise ValueError("offsets must be a vector of G + 1 entries")
+    return _vector(t, "offsets", torch.int32, t.shape[0], like), t.shape[0] - 1
+
+
+def _weights(t, what, dtype, G, n, k, like):
+    """(address, stride from group to group) of [G][n][k] weights or [G][n]
+    biases (k None), each group's consecutive."""
+    shape = (G, n) if k is None else (G, n, k)
+    if tuple(t.shape) != shape or t.dtype != dtype or t.device != like.device:
+        raise ValueError(f"{what} must be {dtype} {shape} on {like.device}")
+    st = t.stride()
+    if (st[-1] != 1 and shape[-1] > 1) or (k is not None and n > 1 and st[1] != k):
+        raise ValueError(f"{what}: a group's entries must be consecutive")
+    return t.data_ptr(), (st[0] if G > 1 else n * (k or 1))
+
+
+def _same_device(t, what, like):
+    if t.device != like.device:
+        raise ValueError(f"{what} must be on {like.device}")
+
+
+class _On:
+    """The stream of a call, and new tensors for it."""
+
+    def __init__(self, like, stream):
+        import torch
+        if not like.is_cuda or like.device.index != torch.cuda.current_device():
+            raise ValueError("tensors must be on the current GPU")
+        self.device = like.device
+        current = torch.cuda.current_stream()
+        self.other = stream if stream is not None and stream != current else None
+        self.handle = (current if stream is None else stream).cuda_stream
+
+    def empty(self, shape, dtype):
+        import torch
+        t = torch.empty(shape, dtype=dtype, device=self.device)
+        if self.other is not None:
+            t.record_stream(self.other)
+        return t
+
+
+def group_forward(x, offsets, w, bias=None, relu=False, p=0.0, seed=0, out=None, stream=None):
+    """gcpsl_group_forward: [rows][n] = dropout(relu(W_g x_r + b_g)) of x
+    [rows][k], rows offsets[g] to offsets[g + 1] through w[g] of [G][n][k]
+    and bias[g] of [G][n] (fp32)."""
+    import torch
+    on = _On(x, stream)
+    xp, ldx = _rows(x, "x")
+    off, G = _offsets(offsets, x)
+    rows, k = x.shape
+    n = w.shape[1] if w.dim() == 3 else -1
+    wp, w_gs = _weights(w, "w", x.dtype, G, n, k, x)
+    bp, b_gs = (0, 0) if bias is None else _weights(bias, "bias", torch.float32, G, n, None, x)
+    y = on.empty((rows, n), x.dtype) if out is None else out
+    _same_device(y, "out", x)
+    yp, ldy = _rows(y, "out", x.dtype, (rows, n))
+    _check(lib().gcpsl_group_forward(_type(x), G, rows, n, k, off, xp, ldx, wp, w_gs, bp, b_gs, 1 if relu else 0, p,
+                                     seed, yp, ldy, on.handle))
+    return y
+
+
+def group_input_grad(dy, offsets, w, gate=None, p=0.0, out=None, stream=None):
+    """gcpsl_group_input_grad: [rows][k] = W_g^T dy_r of dy [rows][n]; with
+    the layer's input as gate, which a ReLU and a dropout of probability p
+    made, the gradient through those."""
+    on = _On(dy, stream)
+    dp, lddy = _rows(dy, "dy")
+    off, G = _offsets(offsets, dy)
+    rows, n = dy.shape
+    k = w.shape[2] if w.dim() == 3 else -1
+    wp, w_gs = _weights(w, "w", dy.dtype, G, n, k, dy)
+    gp, ldg = 0, 0
+    if gate is not None:
+        _same_device(gate, "gate", dy)
+        gp, ldg = _rows(gate, "gate", dy.dtype, (rows, k))
+    dx = on.empty((rows, k), dy.dtype) if out is None else out
+    _same_device(dx, "out", dy)
+    xp, lddx = _rows(dx, "out", dy.dtype, (rows, k))
+    _check(lib().gcpsl_group_input_grad(_type(dy), G, rows, n, k, off, dp, lddy, wp, w_gs, gp, ldg, p, xp, lddx,
+                                        on.handle))
+    return dx
+
+
+def group_workspace_bytes(dtype, G, rows, n, k):
+    """gcpsl_group_workspace_bytes for "f32" or "bf16" tensors."""
+    b = C.c_size_t()
+    _check(lib().gcpsl_group_workspace_bytes(DTYPES[dtype], G, rows, n, k, C.byref(b)))
+    return b.value
+
+
+def _workspace(on, workspace, nbytes):
+    import torch
+    if workspace is None:
+        workspace = on.empty((nbytes,), torch.uint8)
+    elif workspace.device != on.device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous on {on.device}")
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def group_weight_grad(dy, x, offsets, dw=None, db=None, bias=True, workspace=None, stream=None):
+    """gcpsl_group_weight_grad: (dw [G][n][k], db [G][n]) in fp32 from dy
+    [rows][n] and x [rows][k]; db is None with bias=False."""
+    import torch
+    on = _On(dy, stream)
+    dp, lddy = _rows(dy, "dy")
+    off, G = _offsets(offsets, dy)
+    (rows, n), k = dy.shape, x.shape[-1]
+    _same_device(x, "x", dy)
+    xp, ldx = _rows(x, "x", dy.dtype, (rows, k))
+    dw = on.empty((G, n, k), torch.float32) if dw is None else dw
+    wp, w_gs = _weights(dw, "dw", torch.float32, G, n, k, dy)
+    db = on.empty((G, n), torch.float32) if db is None and bias else db
+    bp, b_gs = (0, 0) if db is None else _weights(db, "db", torch.float32, G, n, None, dy)
+    code, need = _type(dy), C.c_size_t()
+    _check(lib().gcpsl_group_workspace_bytes(code, G, rows, n, k, C.byref(need)))
+    workspace, ptr, size = _workspace(on, workspace, need.value)
+    _check(lib().gcpsl_group_weight_grad(code, G, rows, n, k, off, dp, lddy, xp, ldx, wp, w_gs, bp, b_gs, ptr, size,
+                                         on.handle))
+    return dw, db
+
+
+def dropout(x, p, seed, out=None, stream=None):
+    """gcpsl_dropout of x [rows][cols]; out may be x.  The same call on the
+    output's gradient is the backward pass."""
+    on = _On(x, stream)
+    xp, ldx = _rows(x, "x")
+    y = on.empty(tuple(x.shape), x.dtype) if out is None else out
+    _same_device(y, "out", x)
+    yp, ldy = _rows(y, "out", x.dtype, tuple(x.shape))
+    _check(lib().gcpsl_dropout(_type(x), x.shape[0], x.shape[1], xp, ldx, p, seed, yp, ldy, on.handle))
+    return y
+
+
+class Scores(NamedTuple):
+    logp: object       # [rows] log probability of each row's label (None without labels)
+    entropy: object    # [rows]
+    lse: object        # [rows] log sum of exponentials
+    top_logp: object   # [rows][top], in decreasing order
+    top_class: object  # [rows][top] int32
+
+
+def score_workspace_bytes(dtype, rows, L, top=0):
+    """gcpsl_score_workspace_bytes for "f32" or "bf16" logits."""
+    b = C.c_size_t()
+    _check(lib().gcpsl_score_workspace_bytes(DTYPES[dtype], rows, L, top, C.byref(b)))
+    return b.value
+
+
+def score(logits, labels=None, top=0, workspace=None, stream=None):
+    """gcpsl_score of logits [rows][L] and int32 labels [rows]."""
+    import torch
+    on = _On(logits, stream)
+    zp, ldz = _rows(logits, "logits")
+    rows, L = logits.shape
+    yp = _vector(labels, "labels", torch.int32, rows, logits)
+    code, need = _type(logits), C.c_size_t()
+    _check(lib().gcpsl_score_workspace_bytes(code, rows, L, top, C.byref(need)))
+    workspace, ptr, size = _workspace(on, workspace, need.value)
+    logp = None if labels is None else on.empty((rows,), torch.float32)
+    both = on.empty((2, rows), torch.float32)
+    top_logp, top_class = on.empty((rows, top), torch.float32), on.empty((rows, top), torch.int32)
+    entropy, lse = both[0], both[1]
+    _check(lib().gcpsl_score(code, rows, L, zp, ldz, yp, top, None if logp is None else logp.data_ptr(),
+                             entropy.data_ptr(), lse.data_ptr(), top_logp.data_ptr(), top_class.data_ptr(), ptr, size,
+                             on.handle))
+    return Scores(logp, entropy, lse, top_logp, top_class)
+
+
+def score_grad(logits, labels, lse, entropy=None, g_logp=None, g_entropy=None, out=None, stream=None):
+    """gcpsl_score_grad: the loss's gradient by the logits [rows][L], given
+    those by logp (g_logp [rows]) and by entropy (g_entropy [rows]), of which
+    one may be None; out may be the logits."""
+    import torch
+    on = _On(logits, stream)
+    zp, ldz = _rows(logits, "logits")
+    rows, L = logits.shape
+    yp = _vector(labels, "labels", torch.int32, rows, logits)
+    ptrs = [_vector(t, what, torch.float32, rows, logits) for t, what in
+            ((lse, "lse"), (entropy, "entropy"), (g_logp, "g_logp"), (g_entropy, "g_entropy"))]
+    dz = on.empty((rows, L), logits.dtype) if out is None else out
+    _same_device(dz, "out", logits)
+    dp, lddz = _rows(dz, "out", logits.dtype, (rows, L))
+    _check(lib().gcpsl_score_grad(_type(logits), rows, L, zp, ldz, yp, *ptrs, dp, lddz, on.handle))
+    return dz
 
 
 def make_desc(cfg, client_of_example, cluster_of_client, max_steps=None, max_window=1, schedule="lockstep"):

@@ -1,0 +1,223 @@
+"""Label scores and their gradient, on the GPU, against the definitions in 64 bits (tests/ops_plain.py)."""
+import numpy as np
+import pytest
+import torch
+
+import ops_plain as plain
+
+pytestmark = pytest.mark.gpu
+
+from paper_2609_29395_amd import gcpsl  # noqa: E402
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+INF = float("inf")
+
+
+def make(rows, L, dtype, seed=0, scale=2.5):
+    g = torch.Generator().manual_seed(1000 * seed + 7 * rows + L)
+    return (torch.randn(rows, L, generator=g) * scale).to(TYPES[dtype]), torch.randint(0, L, (rows,), generator=g).int()
+
+
+def same(got, want, bound):
+    """Equal where infinite or NaN, else within the bound."""
+    got = got.cpu().double()
+    ok = (got == want) | (torch.isnan(got) & torch.isnan(want)) | ((got - want).abs() <= bound)
+    assert ok.all(), (got[~ok][:4], want[~ok][:4])
+
+
+def check(z, labels, top, r=None):
+    r = gcpsl.score(z.cuda(), None if labels is None else labels.cuda(), top=top) if r is None else r
+    logp, h, lse, top_logp, top_class = plain.score(z, labels, top)
+    bl, bh = plain.score_bounds(z)
+    big = z.double().abs().masked_fill(~torch.isfinite(z.double()), 0).max(1).values
+    bl, bh = torch.nan_to_num(bl, nan=0.0), torch.nan_to_num(bh, nan=0.0)
+    same(r.lse, lse, bl)
+    same(r.entropy, h, bh)
+    if labels is not None:
+        same(r.logp, logp, bl + 4 * plain.U32 * big)
+    assert torch.equal(r.top_class.cpu(), top_class)
+    same(r.top_logp, top_logp, (bl + 4 * plain.U32 * big)[:, None])
+    return r
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,L,top", [
+    (1, 1, 1), (1, 1, 0), (5, 2, 2), (3, 10, 5), (2048, 10, 10), (70, 33, 32), (9, 64, 3), (11, 65, 32), (6, 255, 7),
+    (5, 256, 20), (4, 1000, 5), (300, 1001, 1), (2, 4096, 32), (3, 5000, 20), (1, 16384, 20), (2, 16385, 20), (1, 50021, 32),
+    (1, 131072, 8), (3, 131073, 0), (1, 300001, 20),
+])
+def test_scores(rows, L, top, dtype):
+    z, labels = make(rows, L, dtype)
+    check(z, labels, top)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("L", [10, 100, 3000, 40000])
+def test_ties_go_to_the_lower_class(L, dtype):
+    """Few distinct values, equal ones everywhere, zeros of both signs."""
+    g = torch.Generator().manual_seed(L)
+    z = torch.randint(-1, 2, (6, L), generator=g).to(TYPES[dtype])
+    z[0] = 0.5
+    z[1] = torch.where(torch.rand(L, generator=g) < 0.5, 0.0, -0.0).to(TYPES[dtype])
+    z[2] = -INF
+    z[2, L - 3:] = 1.0
+    z[3, L // 2] = 1.0
+    check(z, torch.full((6,), L - 1, dtype=torch.int32), min(L, 32))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("L", [7, 130, 2500, 33000])
+def test_masked_rows_and_values_that_are_not_finite(L, dtype):
+    T = TYPES[dtype]
+    z, labels = make(12, L, dtype, seed=1)
+    low = torch.finfo(T).min
+    z[0] = -INF                        # nothing left
+    z[1] = -INF
+    z[1, L - 1] = 2.0                  # one class left
+    z[2] = low                         # the type's lowest value everywhere: a uniform row
+    z[3, : L // 2] = low               # as a mask
+    z[4, : L // 2] = -INF
+    z[5] = -INF
+    z[5, 3] = low                      # the only class is at the lowest value
+    z[6, 2] = float("nan")
+    z[7, 5] = INF
+    z[8] = float("nan")
+    z[9, 0], z[9, 1], z[9, L - 1] = float("nan"), INF, float("nan")
+    z[10] = -INF
+    z[10, 4] = float("nan")
+    z[11, 1] = torch.finfo(T).max      # differences past the largest finite value
+    z[11, 2] = low
+    for y in (0, L - 1):
+        check(z, torch.full((12,), y, dtype=torch.int32), min(L, 20))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_labels_outside_the_classes(dtype):
+    z, _ = make(6, 50, dtype)
+    labels = torch.tensor([-1, 50, 3, 2 ** 31 - 1, -2 ** 31, 49], dtype=torch.int32)
+    r = check(z, labels, 2)
+    assert (r.logp.cpu()[[0, 1, 3, 4]] == 0).all()
+    z[0] = -INF
+    assert gcpsl.score(z.cuda(), labels.cuda()).logp[0] == 0
+    g = torch.ones(6, device="cuda")
+    d = gcpsl.score_grad(z.cuda(), labels.cuda(), r.lse, g_logp=g)
+    assert (d[[0, 1, 3, 4]] == 0).all() and (d[[2, 5]] != 0).any(1).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("first,L,ld", [(0, 64, 80), (1, 64, 71), (3, 1001, 1100), (8, 20000, 20016), (1, 9, 11)])
+def test_strides(first, L, ld, dtype):
+    z, labels = make(9, L, dtype, seed=2)
+    wide = torch.full((9, ld + 8), float("nan"), dtype=z.dtype, device="cuda")
+    v = wide[:, first:first + L]
+    v.copy_(z)
+    r = check(z, labels, min(L, 6), gcpsl.score(v, labels.cuda(), top=min(L, 6)))
+    g, gh = torch.randn(9), torch.randn(9)
+    want = gcpsl.score_grad(z.cuda(), labels.cuda(), r.lse, r.entropy, g.cuda(), gh.cuda())
+    gcpsl.score_grad(v, labels.cuda(), r.lse, r.entropy, g.cuda(), gh.cuda(), out=v)  # in place
+    assert torch.equal(v, want)
+    assert torch.isnan(wide[:, :first]).all() and torch.isnan(wide[:, first + L:]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_past_32_bits_of_elements(dtype):
+    rows, L, ld = 1200, 700, (8 << 20) // (2 if dtype == "bf16" else 4)
+    store = torch.empty(rows * ld + L, dtype=TYPES[dtype], device="cuda")
+    v = store.as_strided((rows, L), (ld, 1))
+    z, labels = make(rows, L, dtype)
+    v.copy_(z)
+    r = check(z, labels, 4, gcpsl.score(v, labels.cuda(), top=4))
+    g = torch.ones(rows, device="cuda")
+    want = gcpsl.score_grad(z.cuda(), labels.cuda(), r.lse, g_logp=g)
+    gcpsl.score_grad(v, labels.cuda(), r.lse, g_logp=g, out=v)
+    assert torch.equal(v, want)
+
+
+def grad_bound(z, labels, lse, entropy, gl, gh):
+    """p is off by (|log p| + 8) 2 U32 of itself, the terms by a few roundings each; then dz's own rounding."""
+    z, lse = z.double(), lse.double()[:, None]
+    lp = torch.where(z == -INF, 0.0, z - torch.where(torch.isinf(lse), 0.0, lse))
+    p = torch.where(z == -INF, 0.0, torch.exp(lp))
+    size = gl.double().abs()[:, None] * p + gh.double().abs()[:, None] * p * (lp.abs() + entropy.double().abs()[:, None] + 1)
+    return size * ((lp.abs() + z.abs().clamp(max=1e4) + 12) * 4 * plain.U32) + 4 * plain.U32 * gl.double().abs()[:, None]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,L", [(1, 1), (4, 2), (5, 10), (3, 63), (7, 1000), (130, 257), (2, 8192), (2, 50021)])
+@pytest.mark.parametrize("which", ["logp", "entropy", "both"])
+def test_gradient(rows, L, which, dtype):
+    z, labels = make(rows, L, dtype, seed=3)
+    if L > 2:
+        z[:, 1] = -INF
+        z[0] = -INF
+        labels[labels == 1] = 0
+    g = torch.Generator().manual_seed(L)
+    gl, gh = torch.randn(rows, generator=g), torch.randn(rows, generator=g)
+    r = gcpsl.score(z.cuda(), labels.cuda())
+    a, b = (gl if which != "entropy" else None), (gh if which != "logp" else None)
+    d = gcpsl.score_grad(z.cuda(), labels.cuda() if a is not None else None, r.lse, r.entropy if b is not None else None,
+                         None if a is None else a.cuda(), None if b is None else b.cuda())
+    lse, h = r.lse.cpu(), r.entropy.cpu()
+    want = plain.score_grad(z, labels if a is not None else None, lse, h if b is not None else None, a, b)
+    zero = torch.zeros(rows)
+    bound = grad_bound(z, labels, lse, h, zero if a is None else a, zero if b is None else b)
+    same(d, want, plain.rounded(bound, want, z.dtype))
+
+
+def test_gradient_against_differences():
+    """Central differences of the 64-bit scores: the loss's third derivative by one logit is below 8 (|g_logp| +
+    |g_entropy| (1 + H)), so a step of 1e-4 leaves less than 2e-8 of that, and 64 bits lose 1e-16 / 1e-4 of the loss."""
+    z, labels = make(4, 13, "f32", seed=4)
+    gl, gh = torch.randn(4), torch.randn(4)
+    r = gcpsl.score(z.cuda(), labels.cuda())
+    d = gcpsl.score_grad(z.cuda(), labels.cuda(), r.lse, r.entropy, gl.cuda(), gh.cuda()).cpu().double()
+
+    def loss(z):
+        logp, h, _, _, _ = plain.score(z, labels, 1)
+        return logp * gl.double() + h * gh.double()
+
+    want = torch.zeros_like(d)
+    for c in range(13):
+        e = torch.zeros(13, dtype=torch.float64)
+        e[c] = 1e-4
+        want[:, c] = (loss(z.double() + e) - loss(z.double() - e)) / 2e-4
+    size = (gl.abs() + gh.abs() * (1 + r.entropy.cpu()) + 1).double()[:, None]
+    same(d, want, 1e-7 * size + plain.rounded(grad_bound(z, labels, r.lse.cpu(), r.entropy.cpu(), gl, gh), want, z.dtype))
+
+
+@pytest.mark.parametrize("L", [9, 5000])
+def test_gradient_of_values_that_are_not_finite(L):
+    """Rows of -inf, or of the lowest value, give 0, rows with a NaN or +inf NaN, where the scores are NaN."""
+    z, labels = make(5, L, "f32", seed=5)
+    z[0] = torch.finfo(torch.float32).min
+    z[1], z[2, 3], z[3, 4] = -INF, float("nan"), INF
+    r = gcpsl.score(z.cuda(), labels.cuda())
+    one = torch.ones(5, device="cuda")
+    d = gcpsl.score_grad(z.cuda(), labels.cuda(), r.lse, r.entropy, one, one)
+    assert (d[:2] == 0).all() and torch.isnan(d[2:4]).all() and torch.isfinite(d[4]).all()
+
+
+def test_refusals():
+    z, labels = torch.zeros(4, 8, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    v = torch.zeros(4, device="cuda")
+    for call in (lambda: gcpsl.score(z.cpu()), lambda: gcpsl.score(z.t()), lambda: gcpsl.score(z.half()),
+                 lambda: gcpsl.score(z, labels.long()), lambda: gcpsl.score(z, labels[:3]), lambda: gcpsl.score(z[0]),
+                 lambda: gcpsl.score(z, labels.cpu()), lambda: gcpsl.score_grad(z, labels, v[:3], g_logp=v),
+                 lambda: gcpsl.score_grad(z, labels, v, g_logp=v.double()),
+                 lambda: gcpsl.score_grad(z, labels, v, g_logp=v, out=z[:, :7])):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: gcpsl.score(z, labels, top=9), lambda: gcpsl.score(z, labels, top=-1),
+                 lambda: gcpsl.score(torch.zeros(2, 100, device="cuda"), top=33),
+                 lambda: gcpsl.score_grad(z, labels, v), lambda: gcpsl.score_grad(z, None, v, g_logp=v),
+                 lambda: gcpsl.score_grad(z, labels, v, g_entropy=v)):
+        with pytest.raises(gcpsl.GCPSLError) as e:
+            call()
+        assert e.value.code == gcpsl.EINVAL
+    r = gcpsl.score(z[:0], labels[:0], top=2)
+    assert r.logp.shape == (0,) and r.top_class.shape == (0, 2)
+    need = gcpsl.score_workspace_bytes("bf16", 1, 131072, 20)
+    if need:
+        with pytest.raises(gcpsl.GCPSLError):
+            gcpsl.score(torch.zeros(1, 131072, dtype=torch.bfloat16, device="cuda"), top=20,
+                        workspace=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
