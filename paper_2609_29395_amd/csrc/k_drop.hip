@@ -2,34 +2,84 @@
 // [rows][cols] tensor is kept if bits [16 (j % 4), +16) of SplitMix64's output
 // number r ceil(cols / 4) + j / 4 are at least the threshold.  Nothing is
 // stored: the backward pass draws the same numbers again.
+//
+// A thread takes eight elements, two words of draws, at a time: the finaliser's
+// two 64-bit products (24 of its 40 or so lane cycles) are spread over four
+// elements, so that reading and writing bounds the kernel.  Four such pieces a
+// thread are loaded before the first is used; 16-byte accesses at any
+// alignment.
+#include <algorithm>
+
 #include "runtime.h"
 #include "ops.h"
 
 namespace {
 
-// one thread per word of four draws
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));  // global memory takes 16-byte accesses at any alignment
+
+constexpr int PER = 8, PIECES = 4;  // elements of a piece, pieces of a thread
+
 template <typename T>
-__global__ void __launch_bounds__(256) dropout_kernel(int64_t rows, int64_t cols, const T *x, int64_t ldx, T *y,
-                                                      int64_t ldy, Drop d) {
-  const int64_t words = (cols + 3) >> 2, total = rows * words;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / words, c = (i - r * words) * 4;
-    const uint64_t w = drop_word(d.key, r, words, (int)(c >> 2));
+__global__ void __launch_bounds__(256) dropout_kernel(uint32_t total, FastDiv fd_row, int64_t row0, int cols,
+                                                      const T *x, int64_t ldx, T *y, int64_t ldy, Drop d) {
+  constexpr int NW = PER * sizeof(T) / 16;  // 16-byte vectors of a piece
+  const int64_t words = (cols + 3) >> 2;
+  u32x4 w[PIECES][NW];
+  int64_t row[PIECES];
+  int col[PIECES];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (c + j < cols) {
-        const float v = ElemT<T>::to_f(x[r * ldx + c + j]);
-        y[r * ldy + c + j] = ElemT<T>::from_f(drop_keeps(w, j, d.thr) ? v * d.scale : 0.f);
+  for (int p = 0; p < PIECES; ++p) {
+    const uint32_t u = (blockIdx.x * PIECES + p) * 256 + threadIdx.x;
+    const uint32_t r = fdiv(u, fd_row);
+    row[p] = row0 + r;
+    col[p] = u < total ? (int)(u - r * fd_row.d) * PER : cols;
+    if (col[p] + PER <= cols)
+#pragma unroll
+      for (int i = 0; i < NW; ++i) w[p][i] = *(const u32x4_any *)(x + row[p] * ldx + col[p] + i * (PER / NW));
+  }
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) {
+    if (col[p] >= cols) continue;
+    const uint64_t state = d.key + (uint64_t)(row[p] * words + (col[p] >> 2) + 1) * GCPSL_GOLDEN;
+    const uint64_t draw[2] = {gc_mix64(state), gc_mix64(state + GCPSL_GOLDEN)};
+    const auto value = [&](float v, int j) { return drop_keeps(draw[j >> 2], j & 3, d.thr) ? v * d.scale : 0.f; };
+    T *out = y + row[p] * ldy + col[p];
+    if (col[p] + PER <= cols) {
+#pragma unroll
+      for (int i = 0; i < NW; ++i) {
+        u32x4 o;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t b = w[p][i][j];
+          if constexpr (sizeof(T) == 2)
+            o[j] = pack2_bf16(value(__uint_as_float(b << 16), 2 * j), value(__uint_as_float(b & 0xffff0000u), 2 * j + 1));
+          else
+            o[j] = __float_as_uint(value(__uint_as_float(b), 4 * i + j));
+        }
+        *(u32x4_any *)(out + i * (PER / NW)) = o;
       }
+    } else {
+      const T *in = x + row[p] * ldx + col[p];
+#pragma unroll
+      for (int j = 0; j < PER - 1; ++j)
+        if (col[p] + j < cols) out[j] = ElemT<T>::from_f(value(ElemT<T>::to_f(in[j]), j));
+    }
   }
 }
 
 template <typename T>
 hipError_t run(int64_t rows, int64_t cols, const void *x, int64_t ldx, void *y, int64_t ldy, const Drop &d,
                hipStream_t s) {
-  const int64_t total = rows * ((cols + 3) >> 2), blocks = (total + 255) / 256;
-  hipLaunchKernelGGL(dropout_kernel<T>, dim3((uint32_t)(blocks < 16384 ? blocks : 16384)), dim3(256), 0, s, rows, cols,
-                     (const T *)x, ldx, (T *)y, ldy, d);
+  const int64_t row_pieces = (cols + PER - 1) / PER;
+  const FastDiv fd = make_fastdiv((uint32_t)row_pieces);
+  // launches of at most 2^30 pieces, whose number is a 32-bit one
+  const int64_t slab = std::max<int64_t>(1, (1 << 30) / row_pieces);
+  for (int64_t r = 0; r < rows; r += slab) {
+    const uint32_t total = (uint32_t)(std::min(slab, rows - r) * row_pieces);
+    hipLaunchKernelGGL(dropout_kernel<T>, dim3((total + 256 * PIECES - 1) / (256 * PIECES)), dim3(256), 0, s, total, fd,
+                       r, (int)cols, (const T *)x, ldx, (T *)y, ldy, d);
+  }
   return hipGetLastError();
 }
 
