@@ -1,0 +1,187 @@
+// What the kernels of grouped products share: which rows a workgroup has, and
+// what happens to a finished sum.
+#pragma once
+
+#include <algorithm>
+#include <utility>
+
+#include "ops.h"
+#include "runtime.h"
+
+// Row stride up to which the offsets within 256 rows stay below 2^31 bytes.
+constexpr int64_t kMaxTileLd = 1 << 22;
+
+bool group_tile_ok(int dtype, const GroupArgs &a, int mode);
+hipError_t launch_group_tile(int mode, const GroupArgs &a, hipStream_t s);
+
+#define GROUP_DEVICE __device__ __forceinline__
+
+// Rows [begin, end) of group g, inside [0, rows) whatever the offsets hold.
+GROUP_DEVICE void group_rows(const int32_t *off, int g, int rows, int &begin, int &end) {
+  begin = min(max(off[g], 0), rows);
+  end = min(max(off[g + 1], begin), rows);
+}
+
+// Piece `split` of a group's rows in a weight gradient.
+GROUP_DEVICE void group_piece(const GroupArgs &a, int g, int split, int &q0, int &q1) {
+  group_rows(a.off, g, a.Q, q0, q1);
+  const int piece = ((q1 - q0 + a.splits - 1) / a.splits + 63) / 64 * 64;
+  const int64_t at = q0 + (int64_t)split * piece;  // may pass the group's end, and 31 bits
+  q0 = (int)min(at, (int64_t)q1);
+  q1 = (int)min(at + piece, (int64_t)q1);
+  q0 = __builtin_amdgcn_readfirstlane(q0);
+  q1 = __builtin_amdgcn_readfirstlane(q1);
+}
+
+// Row tiles (bm rows, none spans groups) of groups [base, base + 64), one a
+// lane: their rows, the tiles before the group (`before` are those before
+// the first) and its own.  Returns the tiles up to the last.
+struct LaneTiles {
+  int begin, end;
+  uint32_t first, tiles;
+};
+GROUP_DEVICE uint32_t lane_tiles(const int32_t *off, int G, int rows, int bm, int base, uint32_t before, LaneTiles &l) {
+  const int lane = threadIdx.x & 63;
+  l.begin = l.end = 0;
+  if (base + lane < G) group_rows(off, base + lane, rows, l.begin, l.end);
+  l.tiles = (uint32_t)(l.end - l.begin + bm - 1) / (uint32_t)bm;
+  uint32_t sum = l.tiles;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t v = __shfl_up(sum, d, 64);
+    if (lane >= d) sum += v;
+  }
+  l.first = before + sum - l.tiles;
+  return before + __shfl(sum, 63, 64);
+}
+
+// Group and rows of row tile t; false if there are not that many.  Every wave
+// scans by itself.  (A tile is checked against its group's own rows: offsets
+// that decrease can make groups overlap, but no row outside [0, rows) is
+// touched.)
+GROUP_DEVICE bool find_tile(const int32_t *off, int G, int rows, int bm, int t, int &g, int &row0, int &row1) {
+  uint32_t before = 0;
+  for (int base = 0; base < G; base += 64) {
+    LaneTiles l;
+    before = lane_tiles(off, G, rows, bm, base, before, l);
+    const uint64_t hit = __ballot((uint32_t)t - l.first < l.tiles);
+    if (hit) {
+      const int i = __ffsll((unsigned long long)hit) - 1;
+      g = __builtin_amdgcn_readfirstlane(base + i);
+      row0 = __builtin_amdgcn_readfirstlane(__shfl(l.begin, i, 64) + (t - (int)__shfl(l.first, i, 64)) * bm);
+      row1 = __builtin_amdgcn_readfirstlane(min(__shfl(l.end, i, 64), row0 + bm));
+      return true;
+    }
+  }
+  return false;
+}
+
+// Row and column tile of workgroup b, false if it has none: the tiles that the
+// offsets make, in blocks of 8 row tiles by all column tiles (rows fastest),
+// dealt to the XCDs in contiguous runs, so that the 32 workgroups of an XCD
+// work on about 8 x 4 tiles and share their operands in its L2.
+GROUP_DEVICE bool tile_of(const int32_t *off, int G, int rows, int bm, int NT, uint32_t b, int &mt, int &nt) {
+  uint32_t MT = 0;
+  for (int base = 0; base < G; base += 64) {
+    LaneTiles l;
+    MT = lane_tiles(off, G, rows, bm, base, MT, l);
+  }
+  MT = __builtin_amdgcn_readfirstlane(MT);
+  if (b >= MT * (uint32_t)NT) return false;
+  const uint32_t t = xcd_swizzle(b, MT * (uint32_t)NT);
+  const uint32_t block = t / (8u * (uint32_t)NT), in = t - block * 8u * (uint32_t)NT;
+  const uint32_t high = min(8u, MT - block * 8u);  // row tiles of this block
+  nt = __builtin_amdgcn_readfirstlane((int)(in / high));
+  mt = __builtin_amdgcn_readfirstlane((int)(block * 8u + in % high));
+  return true;
+}
+
+// Four consecutive columns c .. c + 3 of row m of the result (forward, input
+// gradient): bias, ReLU (a NaN stays one), dropout or gate.
+template <typename T, int MODE>
+GROUP_DEVICE void epilogue(const GroupArgs &a, int g, int m, int c, const float *bias, const float *gate, float (&v)[4]) {
+  if constexpr (MODE == GROUP_FWD) {
+    uint64_t word = 0;
+    if (a.drop.thr) word = drop_word(a.drop.key, m, (a.N + 3) >> 2, c >> 2);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      v[r] += bias[r];
+      if (a.relu) v[r] = v[r] <= 0.f ? 0.f : v[r];
+      if (a.drop.thr) v[r] = drop_keeps(word, r, a.drop.thr) ? v[r] * a.drop.scale : 0.f;
+    }
+  } else if (a.gate) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = gate[r] > 0.f ? v[r] * a.drop.scale : 0.f;
+  }
+}
+
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+
+// One rounding and a store, all four columns inside the result (their number
+// is a multiple of 4); any alignment.
+template <typename T, int MODE, typename V>
+GROUP_DEVICE void finish4(const GroupArgs &a, int g, int m, int c, const V &acc) {
+  float v[4] = {acc[0], acc[1], acc[2], acc[3]}, bias[4] = {0.f, 0.f, 0.f, 0.f}, gate[4];
+  if constexpr (MODE == GROUP_FWD) {
+    if (a.bias) {
+      const f32x4_any b = *(const f32x4_any *)(a.bias + g * a.bias_gs + c);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) bias[r] = b[r];
+    }
+  } else if (a.gate) {
+    const T *p = (const T *)a.gate + (int64_t)m * a.ldg + c;
+    if constexpr (sizeof(T) == 2) {
+      const u32x2_any b = *(const u32x2_any *)p;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) gate[r] = __uint_as_float(r & 1 ? b[r >> 1] & 0xffff0000u : b[r >> 1] << 16);
+    } else {
+      const f32x4_any b = *(const f32x4_any *)p;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) gate[r] = b[r];
+    }
+  }
+  epilogue<T, MODE>(a, g, m, c, bias, gate, v);
+  T *out = (T *)a.out + (int64_t)m * a.ldo + c;
+  if constexpr (sizeof(T) == 2)
+    *(u32x2_any *)out = u32x2_any{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])};
+  else
+    *(f32x4_any *)out = f32x4_any{v[0], v[1], v[2], v[3]};
+}
+
+// The same where columns may lie outside.
+template <typename T, int MODE, typename V>
+GROUP_DEVICE void finish(const GroupArgs &a, int g, int m, int c, const V &acc) {
+  if (c + 4 <= a.N) return finish4<T, MODE>(a, g, m, c, acc);
+  float v[4] = {acc[0], acc[1], acc[2], acc[3]}, bias[4] = {0.f, 0.f, 0.f, 0.f}, gate[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (c + r < a.N) {
+      if constexpr (MODE == GROUP_FWD) {
+        if (a.bias) bias[r] = a.bias[g * a.bias_gs + c + r];
+      } else {
+        if (a.gate) gate[r] = ElemT<T>::to_f(((const T *)a.gate)[(int64_t)m * a.ldg + c + r]);
+      }
+    }
+  epilogue<T, MODE>(a, g, m, c, bias, gate, v);
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (c + r < a.N) ((T *)a.out)[(int64_t)m * a.ldo + c + r] = ElemT<T>::from_f(v[r]);
+}
+
+// Four columns of a weight gradient, to its place or (pieces) to a partial.
+template <typename V> GROUP_DEVICE void store_grad(const GroupArgs &a, int g, int split, int m, int c, const V &acc) {
+  float *out = a.splits > 1 ? a.part + (((int64_t)split * a.G + g) * a.M + m) * a.N + c
+                            : (float *)a.out + g * a.out_gs + (int64_t)m * a.ldo + c;
+  if (c + 4 <= a.N) {
+    *(f32x4_any *)out = f32x4_any{acc[0], acc[1], acc[2], acc[3]};
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (c + r < a.N) out[r] = acc[r];
+  }
+}
+GROUP_DEVICE void store_bias_grad(const GroupArgs &a, int g, int split, int m, float v) {
+  if (a.splits > 1) a.part_db[((int64_t)split * a.G + g) * a.M + m] = v;
+  else a.db[g * a.db_gs + m] = v;
+}

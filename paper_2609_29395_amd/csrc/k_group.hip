@@ -5,57 +5,12 @@
 // The group offsets are read on the device, so a launch depends on the number
 // of rows and groups only: it has as many row tiles as any offsets can need,
 // and a workgroup finds its group and rows by a scan of the offsets.
-#include "runtime.h"
-#include "ops.h"
+#include "group.h"
 
 namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
-
-__device__ __forceinline__ int clampi(int v, int lo, int hi) { return min(max(v, lo), hi); }
-
-// Rows [begin, end) of group g, inside [0, rows) whatever the offsets hold.
-__device__ __forceinline__ void group_rows(const int32_t *off, int g, int rows, int &begin, int &end) {
-  begin = clampi(off[g], 0, rows);
-  end = clampi(off[g + 1], begin, rows);
-}
-
-// Group and first row of row tile t (bm rows a tile, no tile spans groups);
-// false if there are not that many.  Every wave scans by itself.  (A tile is
-// checked against its group's own rows, so offsets that decrease can make
-// groups overlap but no row outside [0, rows) is touched.)
-__device__ __forceinline__ bool find_tile(const int32_t *off, int G, int rows, int bm, int t, int &g, int &row0,
-                                          int &row1) {
-  const int lane = threadIdx.x & 63;
-  uint32_t before = 0;
-  for (int base = 0; base < G; base += 64) {
-    const int i = base + lane;
-    int b = 0, e = 0;
-    if (i < G) group_rows(off, i, rows, b, e);
-    const uint32_t tiles = (uint32_t)(e - b + bm - 1) / (uint32_t)bm;
-    uint32_t sum = tiles;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t v = __shfl_up(sum, d, 64);
-      if (lane >= d) sum += v;
-    }
-    const uint32_t first = before + sum - tiles;  // the group's first tile
-    const uint64_t hit = __ballot((uint32_t)t - first < tiles);
-    if (hit) {
-      const int l = __ffsll((unsigned long long)hit) - 1;
-      g = base + l;
-      row0 = __shfl(b, l, 64) + (t - (int)__shfl(first, l, 64)) * bm;
-      row1 = min(__shfl(e, l, 64), row0 + bm);
-      g = __builtin_amdgcn_readfirstlane(g);
-      row0 = __builtin_amdgcn_readfirstlane(row0);
-      row1 = __builtin_amdgcn_readfirstlane(row1);
-      return true;
-    }
-    before += __shfl(sum, 63, 64);
-  }
-  return false;
-}
 
 // ------------------------------------------------------------ any alignment
 // 64 x 64 outputs, four waves of 32 x 32.  A k tile is staged through
@@ -82,30 +37,6 @@ template <> struct Any<float> {
   static constexpr int PER = 4;
 };
 
-// Four consecutive columns c .. c + 3 of row m of the result (forward, input
-// gradient): bias, ReLU (a NaN stays one), dropout or gate, one rounding.
-template <typename T, int MODE>
-__device__ __forceinline__ void finish(const GroupArgs &a, int g, int m, int c, f32x4_t v) {
-  if (c >= a.N) return;
-  uint64_t word = 0;
-  if (MODE == GROUP_FWD && a.drop.thr) word = drop_word(a.drop.key, m, (a.N + 3) >> 2, c >> 2);
-  T *out = (T *)a.out + (int64_t)m * a.ldo + c;
-  const T *gate = (const T *)a.gate + (int64_t)m * a.ldg + c;
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    if (c + r >= a.N) break;
-    float x = v[r];
-    if constexpr (MODE == GROUP_FWD) {
-      if (a.bias) x += a.bias[g * a.bias_gs + c + r];
-      if (a.relu) x = x <= 0.f ? 0.f : x;
-      if (a.drop.thr) x = drop_keeps(word, r, a.drop.thr) ? x * a.drop.scale : 0.f;
-    } else {
-      if (a.gate) x = ElemT<T>::to_f(gate[r]) > 0.f ? x * a.drop.scale : 0.f;
-    }
-    out[r] = ElemT<T>::from_f(x);
-  }
-}
-
 template <typename T, int MODE>
 __global__ void __launch_bounds__(256) group_any_kernel(GroupArgs a, int NT) {
   using K = Any<T>;
@@ -123,11 +54,7 @@ __global__ void __launch_bounds__(256) group_any_kernel(GroupArgs a, int NT) {
     g = mt / MT / a.splits;
     row0 = mt % MT * BM;
     row1 = min(a.M, row0 + BM);
-    group_rows(a.off, g, a.Q, q0, q1);
-    const int piece = ((q1 - q0 + a.splits - 1) / a.splits + BQ - 1) / BQ * BQ;
-    const int64_t at = q0 + (int64_t)split * piece;  // may pass the group's end, and 31 bits
-    q0 = (int)min(at, (int64_t)q1);
-    q1 = (int)min(at + piece, (int64_t)q1);
+    group_piece(a, g, split, q0, q1);
   } else {
     if (!find_tile(a.off, a.G, a.M, BM, mt, g, row0, row1)) return;
   }
@@ -176,19 +103,13 @@ __global__ void __launch_bounds__(256) group_any_kernel(GroupArgs a, int NT) {
       const int m = row0 + wm * 32 + j * 16 + li, c = c0 + wn * 32 + i * 16 + 4 * lg;
       if (m >= row1) continue;
       if constexpr (MODE == GROUP_DW) {
-        float *out = a.splits > 1 ? a.part + (((int64_t)split * a.G + g) * a.M + m) * a.N + c
-                                  : (float *)a.out + g * a.out_gs + (int64_t)m * a.ldo + c;
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (c + r < a.N) out[r] = acc[i][j][r];
+        if (c < a.N) store_grad(a, g, split, m, c, acc[i][j]);
       } else {
-        finish<T, MODE>(a, g, m, c, acc[i][j]);
+        if (c < a.N) finish<T, MODE>(a, g, m, c, acc[i][j]);
       }
     }
-  if (MODE == GROUP_DW && a.db && nt == 0 && tid < BM && row0 + tid < row1) {
-    if (a.splits > 1) a.part_db[((int64_t)split * a.G + g) * a.M + row0 + tid] = rowsum;
-    else a.db[g * a.db_gs + row0 + tid] = rowsum;
-  }
+  if (MODE == GROUP_DW && a.db && nt == 0 && tid < BM && row0 + tid < row1)
+    store_bias_grad(a, g, split, row0 + tid, rowsum);
 }
 
 // Weight gradient in pieces: the pieces' sums, in order.
@@ -215,10 +136,6 @@ hipError_t launch_any(int mode, const GroupArgs &a, hipStream_t s) {
     const int64_t blocks = (int64_t)((a.M + 63) / 64) * NT * a.splits * a.G;
     if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((group_any_kernel<T, GROUP_DW>), dim3((uint32_t)blocks), dim3(256), 0, s, a, NT);
-    if (a.splits > 1) {
-      const int64_t n = (int64_t)a.G * a.M * (a.N + (a.db ? 1 : 0));
-      hipLaunchKernelGGL(group_join_kernel, dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, s, a);
-    }
     return hipGetLastError();
   }
   const int64_t blocks = ((int64_t)a.M / 64 + min(a.G, a.M)) * NT;
@@ -242,5 +159,13 @@ int group_splits(int dtype, int G, int64_t rows, int n, int k) {
 }
 
 hipError_t launch_group(int dtype, int mode, const GroupArgs &a, hipStream_t s) {
-  return dtype == GCPSL_BF16 ? launch_any<bf16_t>(mode, a, s) : launch_any<float>(mode, a, s);
+  hipError_t e;
+  if (group_tile_ok(dtype, a, mode)) e = launch_group_tile(mode, a, s);
+  else e = dtype == GCPSL_BF16 ? launch_any<bf16_t>(mode, a, s) : launch_any<float>(mode, a, s);
+  if (e == hipSuccess && mode == GROUP_DW && a.splits > 1) {
+    const int64_t n = (int64_t)a.G * a.M * (a.N + (a.db ? 1 : 0));
+    hipLaunchKernelGGL(group_join_kernel, dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, s, a);
+    e = hipGetLastError();
+  }
+  return e;
 }
