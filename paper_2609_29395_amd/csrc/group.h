@@ -76,10 +76,18 @@ GROUP_DEVICE bool find_tile(const int32_t *off, int G, int rows, int bm, int t, 
   return false;
 }
 
-// Row and column tile of workgroup b, false if it has none: the tiles that the
-// offsets make, in blocks of 8 row tiles by all column tiles (rows fastest),
-// dealt to the XCDs in contiguous runs, so that the 32 workgroups of an XCD
-// work on about 8 x 4 tiles and share their operands in its L2.
+// Tile t of MT x NT in blocks of 8 row tiles by all column tiles, rows
+// fastest: 32 tiles in order are about 8 x 4 and share their operands.
+GROUP_DEVICE void block_order(uint32_t t, uint32_t MT, uint32_t NT, int &mt, int &nt) {
+  const uint32_t block = t / (8u * NT), in = t - block * 8u * NT;
+  const uint32_t high = min(8u, MT - block * 8u);  // row tiles of this block
+  nt = __builtin_amdgcn_readfirstlane((int)(in / high));
+  mt = __builtin_amdgcn_readfirstlane((int)(block * 8u + in % high));
+}
+
+// Tile of workgroup b of a product whose row tiles the offsets make, false if
+// it has none: tiles are dealt to the XCDs in contiguous runs of block_order,
+// so that an XCD's 32 workgroups share their operands in its L2.
 GROUP_DEVICE bool tile_of(const int32_t *off, int G, int rows, int bm, int NT, uint32_t b, int &mt, int &nt) {
   uint32_t MT = 0;
   for (int base = 0; base < G; base += 64) {
@@ -87,12 +95,9 @@ GROUP_DEVICE bool tile_of(const int32_t *off, int G, int rows, int bm, int NT, u
     MT = lane_tiles(off, G, rows, bm, base, MT, l);
   }
   MT = __builtin_amdgcn_readfirstlane(MT);
-  if (b >= MT * (uint32_t)NT) return false;
-  const uint32_t t = xcd_swizzle(b, MT * (uint32_t)NT);
-  const uint32_t block = t / (8u * (uint32_t)NT), in = t - block * 8u * (uint32_t)NT;
-  const uint32_t high = min(8u, MT - block * 8u);  // row tiles of this block
-  nt = __builtin_amdgcn_readfirstlane((int)(in / high));
-  mt = __builtin_amdgcn_readfirstlane((int)(block * 8u + in % high));
+  const uint32_t all = MT * (uint32_t)NT;
+  if (b >= all) return false;
+  block_order(xcd_swizzle(b, all), MT, (uint32_t)NT, mt, nt);
   return true;
 }
 

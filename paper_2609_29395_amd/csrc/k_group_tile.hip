@@ -218,13 +218,13 @@ __global__ void __launch_bounds__(512, 2) group_tile_kernel(GroupArgs a, int NT)
   const char *A, *B;
   if constexpr (MODE == GROUP_DW) {
     const int MT = (a.M + BM - 1) / BM;
-    uint32_t t = xcd_swizzle(blockIdx.x, (uint32_t)(MT * NT * a.splits * a.G));
-    nt = __builtin_amdgcn_readfirstlane((int)(t % (uint32_t)NT));
-    t /= (uint32_t)NT;
-    row0 = __builtin_amdgcn_readfirstlane((int)(t % (uint32_t)MT)) * BM;
-    t /= (uint32_t)MT;
-    split = __builtin_amdgcn_readfirstlane((int)(t % (uint32_t)a.splits));
-    g = __builtin_amdgcn_readfirstlane((int)(t / (uint32_t)a.splits));
+    // a group's tiles go to all XCDs alike, so that unequal groups do not make unequal XCDs
+    const uint32_t tiles = (uint32_t)MT * (uint32_t)NT, part = blockIdx.x / tiles;
+    int mt;
+    block_order(xcd_swizzle(blockIdx.x - part * tiles, tiles), (uint32_t)MT, (uint32_t)NT, mt, nt);
+    row0 = mt * BM;
+    split = __builtin_amdgcn_readfirstlane((int)(part % (uint32_t)a.splits));
+    g = __builtin_amdgcn_readfirstlane((int)(part / (uint32_t)a.splits));
     int q0, q1;
     group_piece(a, g, split, q0, q1);
     Q = q1 - q0;
@@ -233,9 +233,8 @@ __global__ void __launch_bounds__(512, 2) group_tile_kernel(GroupArgs a, int NT)
     A = (const char *)a.a + ((int64_t)q0 * a.lda + row0) * 2;
     B = (const char *)a.b + ((int64_t)q0 * a.ldb + c0) * 2;
   } else {
-    int mt;
+    int mt, row1;
     if (!tile_of(a.off, a.G, a.M, BM, NT, blockIdx.x, mt, nt)) return;
-    int row1;
     if (!find_tile(a.off, a.G, a.M, BM, mt, g, row0, row1)) return;
     rows = row1 - row0;
     c0 = nt * BN;
