@@ -8,6 +8,7 @@ raises; there is no fallback path.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import NamedTuple
 
@@ -186,104 +187,113 @@ def fuse_replicas(theta, weights, stream=None):
 
 # ------------------------------------------ operators on tensors, without a context
 #
-# Tensors are on one GPU, rows of consecutive elements (any row stride).  Every
-# function returns the tensors it wrote: those given as out, dw, db, or new
-# ones.  stream: a torch stream, the current one by default; what is newly
-# allocated for another stream is marked as used there.
+# Tensors are on the current GPU, rows of consecutive elements (any row
+# stride).  Every function returns the tensors it wrote: those given as out,
+# dw, db, or new ones.  stream: a torch stream, the current one by default;
+# what is newly allocated for another stream is marked as used there.  The
+# smallest calls are bound by the host: checks read each attribute once, and
+# the current stream is asked for as the bare handle.
 
-def _rows(t, what, dtype=None, shape=None):
-    """(address, row stride) of a [rows][cols] tensor."""
-    if t.dim() != 2 or not t.is_cuda:
-        raise ValueError(f"{what} must be a [rows][cols] tensor on the GPU")
-    if dtype is not None and t.dtype != dtype:
-        raise ValueError(f"{what} must be {dtype}, is {t.dtype}")
-    if shape is not None and tuple(t.shape) != shape:
-        raise ValueError(f"{what} must be {shape}, is {tuple(t.shape)}")
-    rows, cols = t.shape
-    ld, step = t.stride()
-    if step != 1 and cols > 1:
-        raise ValueError(f"{what}: a row's elements must be consecutive")
-    return t.data_ptr(), (ld if rows > 1 else cols)
+_torch = None
+_types = {}
 
 
-def _type(t):
+def _load_torch():
+    global _torch
     import torch
-    code = {torch.float32: 0, torch.bfloat16: 1}.get(t.dtype)
+    _types.update({torch.float32: 0, torch.bfloat16: 1})
+    _torch = torch
+    return torch
+
+
+def _begin(t, stream):
+    """(torch, type code, stream handle, device) of a call on t's GPU."""
+    torch = _torch or _load_torch()
+    code = _types.get(t.dtype)
     if code is None:
         raise ValueError(f"fp32 or bf16 tensors only, not {t.dtype}")
-    return code
+    device = t.get_device()
+    if device < 0 or device != torch._C._cuda_getDevice():
+        raise ValueError("tensors must be on the current GPU")
+    handle = torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+    return torch, code, handle, device
 
 
-def _vector(t, what, dtype, n, like):
-    """Address of a vector of n elements, 0 for None."""
+def _empty(like, shape, dtype, stream):
+    t = like.new_empty(shape, dtype=dtype)
+    if stream is not None:
+        t.record_stream(stream)
+    return t
+
+
+def _rows(t, what, dtype, device, rows=None, cols=None):
+    """(address, row stride) of a [rows][cols] tensor."""
+    shape = t.shape
+    if len(shape) != 2 or t.dtype != dtype or t.get_device() != device:
+        raise ValueError(f"{what} must be a [rows][cols] {dtype} tensor on the same GPU")
+    r, c = shape
+    if (rows is not None and r != rows) or (cols is not None and c != cols):
+        raise ValueError(f"{what} must be ({rows}, {cols}), is {tuple(shape)}")
+    ld, step = t.stride()
+    if step != 1 and c > 1:
+        raise ValueError(f"{what}: a row's elements must be consecutive")
+    return t.data_ptr(), (ld if r > 1 else c)
+
+
+def _vector(t, what, dtype, n, device):
+    """Address of a vector of n elements, None for None."""
     if t is None:
-        return 0
-    if t.dtype != dtype or tuple(t.shape) != (n,) or not t.is_contiguous() or t.device != like.device:
-        raise ValueError(f"{what} must be a contiguous {dtype} vector of {n} on {like.device}")
+        return None
+    if t.dtype != dtype or t.shape != (n,) or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} vector of {n} on the same GPU")
     return t.data_ptr()
 
 
-def _offsets(t, like):
-    import torch
+def _offsets(t, torch, device):
     if t.dim() != 1 or t.shape[0] < 2:
         raise ValueError("offsets must be a vector of G + 1 entries")
-    return _vector(t, "offsets", torch.int32, t.shape[0], like), t.shape[0] - 1
+    G = t.shape[0] - 1
+    return _vector(t, "offsets", torch.int32, G + 1, device), G
 
 
-def _weights(t, what, dtype, G, n, k, like):
+def _weights(t, what, dtype, device, shape):
     """(address, stride from group to group) of [G][n][k] weights or [G][n]
-    biases (k None), each group's consecutive."""
-    shape = (G, n) if k is None else (G, n, k)
-    if tuple(t.shape) != shape or t.dtype != dtype or t.device != like.device:
-        raise ValueError(f"{what} must be {dtype} {shape} on {like.device}")
+    biases, each group's consecutive."""
+    if t.shape != shape or t.dtype != dtype or t.get_device() != device:
+        raise ValueError(f"{what} must be {dtype} {shape} on the same GPU, is {t.dtype} {tuple(t.shape)}")
     st = t.stride()
-    if (st[-1] != 1 and shape[-1] > 1) or (k is not None and n > 1 and st[1] != k):
+    if (st[-1] != 1 and shape[-1] > 1) or (len(shape) == 3 and shape[1] > 1 and st[1] != shape[2]):
         raise ValueError(f"{what}: a group's entries must be consecutive")
-    return t.data_ptr(), (st[0] if G > 1 else n * (k or 1))
+    return t.data_ptr(), (st[0] if shape[0] > 1 else shape[1] * (shape[2] if len(shape) == 3 else 1))
 
 
-def _same_device(t, what, like):
-    if t.device != like.device:
-        raise ValueError(f"{what} must be on {like.device}")
-
-
-class _On:
-    """The stream of a call, and new tensors for it."""
-
-    def __init__(self, like, stream):
-        import torch
-        if not like.is_cuda or like.device.index != torch.cuda.current_device():
-            raise ValueError("tensors must be on the current GPU")
-        self.device = like.device
-        current = torch.cuda.current_stream()
-        self.other = stream if stream is not None and stream != current else None
-        self.handle = (current if stream is None else stream).cuda_stream
-
-    def empty(self, shape, dtype):
-        import torch
-        t = torch.empty(shape, dtype=dtype, device=self.device)
-        if self.other is not None:
-            t.record_stream(self.other)
-        return t
+def _workspace(like, workspace, nbytes, device, stream):
+    """(address, bytes, tensor to keep) of a call's workspace."""
+    if workspace is None:
+        if nbytes == 0:
+            return None, 0, None
+        workspace = _empty(like, (nbytes,), _torch.uint8, stream)
+    elif workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous on the same GPU")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
 def group_forward(x, offsets, w, bias=None, relu=False, p=0.0, seed=0, out=None, stream=None):
     """gcpsl_group_forward: [rows][n] = dropout(relu(W_g x_r + b_g)) of x
     [rows][k], rows offsets[g] to offsets[g + 1] through w[g] of [G][n][k]
     and bias[g] of [G][n] (fp32)."""
-    import torch
-    on = _On(x, stream)
-    xp, ldx = _rows(x, "x")
-    off, G = _offsets(offsets, x)
+    torch, code, handle, device = _begin(x, stream)
+    dtype = x.dtype
+    xp, ldx = _rows(x, "x", dtype, device)
+    off, G = _offsets(offsets, torch, device)
     rows, k = x.shape
     n = w.shape[1] if w.dim() == 3 else -1
-    wp, w_gs = _weights(w, "w", x.dtype, G, n, k, x)
-    bp, b_gs = (0, 0) if bias is None else _weights(bias, "bias", torch.float32, G, n, None, x)
-    y = on.empty((rows, n), x.dtype) if out is None else out
-    _same_device(y, "out", x)
-    yp, ldy = _rows(y, "out", x.dtype, (rows, n))
-    _check(lib().gcpsl_group_forward(_type(x), G, rows, n, k, off, xp, ldx, wp, w_gs, bp, b_gs, 1 if relu else 0, p,
-                                     seed, yp, ldy, on.handle))
+    wp, w_gs = _weights(w, "w", dtype, device, (G, n, k))
+    bp, b_gs = (None, 0) if bias is None else _weights(bias, "bias", torch.float32, device, (G, n))
+    y = _empty(x, (rows, n), dtype, stream) if out is None else out
+    yp, ldy = _rows(y, "out", dtype, device, rows, n)
+    _check(lib().gcpsl_group_forward(code, G, rows, n, k, off, xp, ldx, wp, w_gs, bp, b_gs, 1 if relu else 0, p, seed,
+                                     yp, ldy, handle))
     return y
 
 
@@ -291,71 +301,60 @@ def group_input_grad(dy, offsets, w, gate=None, p=0.0, out=None, stream=None):
     """gcpsl_group_input_grad: [rows][k] = W_g^T dy_r of dy [rows][n]; with
     the layer's input as gate, which a ReLU and a dropout of probability p
     made, the gradient through those."""
-    on = _On(dy, stream)
-    dp, lddy = _rows(dy, "dy")
-    off, G = _offsets(offsets, dy)
+    torch, code, handle, device = _begin(dy, stream)
+    dtype = dy.dtype
+    dp, lddy = _rows(dy, "dy", dtype, device)
+    off, G = _offsets(offsets, torch, device)
     rows, n = dy.shape
     k = w.shape[2] if w.dim() == 3 else -1
-    wp, w_gs = _weights(w, "w", dy.dtype, G, n, k, dy)
-    gp, ldg = 0, 0
-    if gate is not None:
-        _same_device(gate, "gate", dy)
-        gp, ldg = _rows(gate, "gate", dy.dtype, (rows, k))
-    dx = on.empty((rows, k), dy.dtype) if out is None else out
-    _same_device(dx, "out", dy)
-    xp, lddx = _rows(dx, "out", dy.dtype, (rows, k))
-    _check(lib().gcpsl_group_input_grad(_type(dy), G, rows, n, k, off, dp, lddy, wp, w_gs, gp, ldg, p, xp, lddx,
-                                        on.handle))
+    wp, w_gs = _weights(w, "w", dtype, device, (G, n, k))
+    gp, ldg = (None, 0) if gate is None else _rows(gate, "gate", dtype, device, rows, k)
+    dx = _empty(dy, (rows, k), dtype, stream) if out is None else out
+    xp, lddx = _rows(dx, "out", dtype, device, rows, k)
+    _check(lib().gcpsl_group_input_grad(code, G, rows, n, k, off, dp, lddy, wp, w_gs, gp, ldg, p, xp, lddx, handle))
     return dx
+
+
+@functools.lru_cache(maxsize=1024)
+def _group_workspace_bytes(code, G, rows, n, k):
+    b = C.c_size_t()
+    _check(lib().gcpsl_group_workspace_bytes(code, G, rows, n, k, C.byref(b)))
+    return b.value
 
 
 def group_workspace_bytes(dtype, G, rows, n, k):
     """gcpsl_group_workspace_bytes for "f32" or "bf16" tensors."""
-    b = C.c_size_t()
-    _check(lib().gcpsl_group_workspace_bytes(DTYPES[dtype], G, rows, n, k, C.byref(b)))
-    return b.value
-
-
-def _workspace(on, workspace, nbytes):
-    import torch
-    if workspace is None:
-        workspace = on.empty((nbytes,), torch.uint8)
-    elif workspace.device != on.device or not workspace.is_contiguous():
-        raise ValueError(f"workspace must be contiguous on {on.device}")
-    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    return _group_workspace_bytes(DTYPES[dtype], G, rows, n, k)
 
 
 def group_weight_grad(dy, x, offsets, dw=None, db=None, bias=True, workspace=None, stream=None):
     """gcpsl_group_weight_grad: (dw [G][n][k], db [G][n]) in fp32 from dy
     [rows][n] and x [rows][k]; db is None with bias=False."""
-    import torch
-    on = _On(dy, stream)
-    dp, lddy = _rows(dy, "dy")
-    off, G = _offsets(offsets, dy)
-    (rows, n), k = dy.shape, x.shape[-1]
-    _same_device(x, "x", dy)
-    xp, ldx = _rows(x, "x", dy.dtype, (rows, k))
-    dw = on.empty((G, n, k), torch.float32) if dw is None else dw
-    wp, w_gs = _weights(dw, "dw", torch.float32, G, n, k, dy)
-    db = on.empty((G, n), torch.float32) if db is None and bias else db
-    bp, b_gs = (0, 0) if db is None else _weights(db, "db", torch.float32, G, n, None, dy)
-    code, need = _type(dy), C.c_size_t()
-    _check(lib().gcpsl_group_workspace_bytes(code, G, rows, n, k, C.byref(need)))
-    workspace, ptr, size = _workspace(on, workspace, need.value)
+    torch, code, handle, device = _begin(dy, stream)
+    dp, lddy = _rows(dy, "dy", dy.dtype, device)
+    off, G = _offsets(offsets, torch, device)
+    rows, n = dy.shape
+    xp, ldx = _rows(x, "x", dy.dtype, device, rows)
+    k = x.shape[1]
+    dw = _empty(dy, (G, n, k), torch.float32, stream) if dw is None else dw
+    wp, w_gs = _weights(dw, "dw", torch.float32, device, (G, n, k))
+    db = _empty(dy, (G, n), torch.float32, stream) if db is None and bias else db
+    bp, b_gs = (None, 0) if db is None else _weights(db, "db", torch.float32, device, (G, n))
+    ptr, size, keep = _workspace(dy, workspace, _group_workspace_bytes(code, G, rows, n, k), device, stream)
     _check(lib().gcpsl_group_weight_grad(code, G, rows, n, k, off, dp, lddy, xp, ldx, wp, w_gs, bp, b_gs, ptr, size,
-                                         on.handle))
+                                         handle))
     return dw, db
 
 
 def dropout(x, p, seed, out=None, stream=None):
     """gcpsl_dropout of x [rows][cols]; out may be x.  The same call on the
     output's gradient is the backward pass."""
-    on = _On(x, stream)
-    xp, ldx = _rows(x, "x")
-    y = on.empty(tuple(x.shape), x.dtype) if out is None else out
-    _same_device(y, "out", x)
-    yp, ldy = _rows(y, "out", x.dtype, tuple(x.shape))
-    _check(lib().gcpsl_dropout(_type(x), x.shape[0], x.shape[1], xp, ldx, p, seed, yp, ldy, on.handle))
+    torch, code, handle, device = _begin(x, stream)
+    xp, ldx = _rows(x, "x", x.dtype, device)
+    rows, cols = x.shape
+    y = _empty(x, (rows, cols), x.dtype, stream) if out is None else out
+    yp, ldy = _rows(y, "out", x.dtype, device, rows, cols)
+    _check(lib().gcpsl_dropout(code, rows, cols, xp, ldx, p, seed, yp, ldy, handle))
     return y
 
 
@@ -367,48 +366,50 @@ class Scores(NamedTuple):
     top_class: object  # [rows][top] int32
 
 
+@functools.lru_cache(maxsize=1024)
+def _score_workspace_bytes(code, rows, L, top):
+    b = C.c_size_t()
+    _check(lib().gcpsl_score_workspace_bytes(code, rows, L, top, C.byref(b)))
+    return b.value
+
+
 def score_workspace_bytes(dtype, rows, L, top=0):
     """gcpsl_score_workspace_bytes for "f32" or "bf16" logits."""
-    b = C.c_size_t()
-    _check(lib().gcpsl_score_workspace_bytes(DTYPES[dtype], rows, L, top, C.byref(b)))
-    return b.value
+    return _score_workspace_bytes(DTYPES[dtype], rows, L, top)
 
 
 def score(logits, labels=None, top=0, workspace=None, stream=None):
     """gcpsl_score of logits [rows][L] and int32 labels [rows]."""
-    import torch
-    on = _On(logits, stream)
-    zp, ldz = _rows(logits, "logits")
+    torch, code, handle, device = _begin(logits, stream)
+    zp, ldz = _rows(logits, "logits", logits.dtype, device)
     rows, L = logits.shape
-    yp = _vector(labels, "labels", torch.int32, rows, logits)
-    code, need = _type(logits), C.c_size_t()
-    _check(lib().gcpsl_score_workspace_bytes(code, rows, L, top, C.byref(need)))
-    workspace, ptr, size = _workspace(on, workspace, need.value)
-    logp = None if labels is None else on.empty((rows,), torch.float32)
-    both = on.empty((2, rows), torch.float32)
-    top_logp, top_class = on.empty((rows, top), torch.float32), on.empty((rows, top), torch.int32)
-    entropy, lse = both[0], both[1]
-    _check(lib().gcpsl_score(code, rows, L, zp, ldz, yp, top, None if logp is None else logp.data_ptr(),
-                             entropy.data_ptr(), lse.data_ptr(), top_logp.data_ptr(), top_class.data_ptr(), ptr, size,
-                             on.handle))
-    return Scores(logp, entropy, lse, top_logp, top_class)
+    yp = _vector(labels, "labels", torch.int32, rows, device)
+    ptr, size, keep = _workspace(logits, workspace, _score_workspace_bytes(code, rows, L, top), device, stream)
+    each = _empty(logits, (3, rows), torch.float32, stream)
+    top_logp = _empty(logits, (rows, top), torch.float32, stream)
+    top_class = _empty(logits, (rows, top), torch.int32, stream)
+    ep = each.data_ptr()
+    _check(lib().gcpsl_score(code, rows, L, zp, ldz, yp, top, None if labels is None else ep, ep + 4 * rows,
+                             ep + 8 * rows, top_logp.data_ptr(), top_class.data_ptr(), ptr, size, handle))
+    logp, entropy, lse = each.unbind(0)
+    return Scores(None if labels is None else logp, entropy, lse, top_logp, top_class)
 
 
 def score_grad(logits, labels, lse, entropy=None, g_logp=None, g_entropy=None, out=None, stream=None):
     """gcpsl_score_grad: the loss's gradient by the logits [rows][L], given
     those by logp (g_logp [rows]) and by entropy (g_entropy [rows]), of which
     one may be None; out may be the logits."""
-    import torch
-    on = _On(logits, stream)
-    zp, ldz = _rows(logits, "logits")
+    torch, code, handle, device = _begin(logits, stream)
+    zp, ldz = _rows(logits, "logits", logits.dtype, device)
     rows, L = logits.shape
-    yp = _vector(labels, "labels", torch.int32, rows, logits)
-    ptrs = [_vector(t, what, torch.float32, rows, logits) for t, what in
-            ((lse, "lse"), (entropy, "entropy"), (g_logp, "g_logp"), (g_entropy, "g_entropy"))]
-    dz = on.empty((rows, L), logits.dtype) if out is None else out
-    _same_device(dz, "out", logits)
-    dp, lddz = _rows(dz, "out", logits.dtype, (rows, L))
-    _check(lib().gcpsl_score_grad(_type(logits), rows, L, zp, ldz, yp, *ptrs, dp, lddz, on.handle))
+    yp = _vector(labels, "labels", torch.int32, rows, device)
+    f32 = torch.float32
+    dz = _empty(logits, (rows, L), logits.dtype, stream) if out is None else out
+    dp, lddz = _rows(dz, "out", logits.dtype, device, rows, L)
+    _check(lib().gcpsl_score_grad(code, rows, L, zp, ldz, yp, _vector(lse, "lse", f32, rows, device),
+                                  _vector(entropy, "entropy", f32, rows, device),
+                                  _vector(g_logp, "g_logp", f32, rows, device),
+                                  _vector(g_entropy, "g_entropy", f32, rows, device), dp, lddz, handle))
     return dz
 
 
