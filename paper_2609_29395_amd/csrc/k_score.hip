@@ -97,6 +97,18 @@ template <int TPR> __device__ __forceinline__ uint64_t group_max(uint64_t v, uin
   return v;
 }
 
+// The largest bound, on the upper 16 bits of an order, that at least n lanes
+// reach (n <= 64).
+__device__ __forceinline__ uint32_t bound_of(uint32_t order, int n) {
+  uint32_t at = 0;
+#pragma unroll
+  for (int bit = 15; bit >= 0; --bit) {
+    const uint32_t next = at | 1u << bit;
+    if (__popcll(__ballot((order >> 16) >= next)) >= n) at = next;
+  }
+  return at << 16;
+}
+
 // Sums of a set of logits: maximum, sum of e^d, sum of e^d d.
 struct Sums {
   float m, s, t;
@@ -220,14 +232,8 @@ __global__ void __launch_bounds__(256, 4) score_kernel(ScoreArgs a, uint32_t job
 
   float bound = -INFINITY;
   if (a.top) {
-    const uint32_t u = order_of(lmax) >> 16;
-    uint32_t at = 0;
-#pragma unroll
-    for (int bit = 15; bit >= 0; --bit) {
-      const uint32_t next = at | 1u << bit;
-      if (__popcll(__ballot(u >= next)) >= a.top) at = next;
-    }
-    if (at > (order_of(-INFINITY) >> 16)) bound = value_of(at << 16);
+    const uint32_t at = bound_of(order_of(lmax), a.top);
+    if (at > order_of(-INFINITY)) bound = value_of(at);
   }
   if (t == 0) count[0] = count[1] = 0;
   if constexpr (TPR == 256) {
@@ -314,11 +320,76 @@ __global__ void __launch_bounds__(256, 4) score_kernel(ScoreArgs a, uint32_t job
   }
 }
 
-// A row of several chunks from their sums and top keys, one workgroup a row:
-// the top classes one at a time by a maximum over the keys, held in registers
-// where 2,048 are enough.
+// A row of several chunks from their sums and top keys, at most 1,024 of them:
+// a wave a row holds the keys in registers and takes the top classes as the
+// chunks' kernel does (a maximum over all keys for each class cost 0.7 us a
+// class: 15 us for 20).
+constexpr int kHeld = 16, kCandidates = 128;
 template <typename T>
 __global__ void __launch_bounds__(256) score_join_kernel(ScoreArgs a, int chunks) {
+  __shared__ uint64_t list_[4 * kCandidates];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint64_t *list = list_ + wave * kCandidates;
+  const int64_t row = (int64_t)blockIdx.x * 4 + wave;
+  if (row >= a.rows) return;
+  const float4 *sums = part_sums(a, row, chunks);
+  const uint64_t *keys = part_keys(a, row, chunks);
+  const int n = chunks * a.top;
+  uint64_t held[kHeld], best = 0;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) held[i] = lane + i * 64 < n ? keys[lane + i * 64] : 0;
+  float m = -INFINITY;
+  for (int c = lane; c < chunks; c += 64) m = fmaxf(m, sums[c].x);
+  Sums p{wave_max(m), 0.f, 0.f};
+  for (int c = lane; c < chunks; c += 64) {
+    Sums q{sums[c].x, sums[c].y, sums[c].z};
+    rebase(q, p.m);
+    p.s += q.s;
+    p.t += q.t;
+  }
+  p.s = wave_sum(p.s);
+  p.t = wave_sum(p.t);
+  const RowScore r(p);
+  if (lane == 0) write_row<T>(a, row, r);
+  if (a.top == 0) return;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) best = max(best, held[i]);
+  const uint64_t bound = max((uint64_t)bound_of((uint32_t)(best >> 32), a.top) << 32, (uint64_t)1);
+  int count = 0;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const bool in = held[i] >= bound;
+    const uint64_t lanes = __ballot(in);
+    if (in) {
+      const int at = count + __popcll(lanes & ((1ull << lane) - 1));
+      if (at < kCandidates) list[at] = held[i];
+    }
+    count += __popcll(lanes);
+  }
+  if (count <= kCandidates) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (int i = lane; i < count; i += 64) {
+      const uint64_t key = list[i];
+      int above = 0;
+      for (int j = 0; j < count; ++j) above += list[j] > key;
+      if (above < a.top) write_top(a, row, above, key, r);
+    }
+    return;
+  }
+  uint64_t last = ~0ull;
+  for (int k = 0; k < a.top; ++k) {
+    best = 0;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+      if (held[i] < last && held[i] > best) best = held[i];
+    last = wave_max(best);
+    if (lane == 0) write_top(a, row, k, last, r);
+  }
+}
+
+// The same for more keys, a workgroup a row, one class at a time.
+template <typename T>
+__global__ void __launch_bounds__(256) score_join_many_kernel(ScoreArgs a, int chunks) {
   __shared__ float4 wsum[4];
   __shared__ uint64_t buf[4];
   const int64_t row = blockIdx.x;
@@ -326,10 +397,6 @@ __global__ void __launch_bounds__(256) score_join_kernel(ScoreArgs a, int chunks
   const float4 *sums = part_sums(a, row, chunks);
   const uint64_t *keys = part_keys(a, row, chunks);
   const int64_t n = (int64_t)chunks * a.top;
-  constexpr int HELD = 8;
-  uint64_t held[HELD];
-#pragma unroll
-  for (int i = 0; i < HELD; ++i) held[i] = t + i * 256 < n ? keys[t + i * 256] : 0;
   float m = -INFINITY;
   for (int c = t; c < chunks; c += 256) m = fmaxf(m, sums[c].x);
   m = wave_max(m);
@@ -359,10 +426,7 @@ __global__ void __launch_bounds__(256) score_join_kernel(ScoreArgs a, int chunks
   uint64_t last = ~0ull;
   for (int k = 0; k < a.top; ++k) {
     uint64_t best = 0;
-#pragma unroll
-    for (int i = 0; i < HELD; ++i)
-      if (held[i] < last && held[i] > best) best = held[i];
-    for (int64_t i = t + HELD * 256; i < n; i += 256)
+    for (int64_t i = t; i < n; i += 256)
       if (keys[i] < last && keys[i] > best) best = keys[i];
     last = group_max<256>(best, buf);
     if (t == 0) write_top(a, row, k, last, r);
@@ -508,7 +572,10 @@ template <typename T> hipError_t run(const ScoreArgs &a, hipStream_t s) {
   const FastDiv fd = make_fastdiv((uint32_t)ch.n);
   if (ch.large) hipLaunchKernelGGL((score_kernel<T, 256, kLargeNV<T>>), dim3(n), dim3(256), 0, s, a, n, fd);
   else hipLaunchKernelGGL((score_kernel<T, 256, kSmallNV>), dim3(n), dim3(256), 0, s, a, n, fd);
-  if (ch.n > 1) hipLaunchKernelGGL(score_join_kernel<T>, dim3((uint32_t)a.rows), dim3(256), 0, s, a, (int)ch.n);
+  if (ch.n > 1 && ch.n * a.top <= 64 * kHeld)
+    hipLaunchKernelGGL(score_join_kernel<T>, dim3((uint32_t)((a.rows + 3) / 4)), dim3(256), 0, s, a, (int)ch.n);
+  else if (ch.n > 1)
+    hipLaunchKernelGGL(score_join_many_kernel<T>, dim3((uint32_t)a.rows), dim3(256), 0, s, a, (int)ch.n);
   return hipGetLastError();
 }
 

@@ -45,6 +45,7 @@ def check(z, labels, top, r=None):
     (1, 1, 1), (1, 1, 0), (5, 2, 2), (3, 10, 5), (2048, 10, 10), (70, 33, 32), (9, 64, 3), (11, 65, 32), (6, 255, 7),
     (5, 256, 20), (4, 1000, 5), (300, 1001, 1), (2, 4096, 32), (3, 5000, 20), (1, 16384, 20), (2, 16385, 20), (1, 50021, 32),
     (1, 131072, 8), (3, 131073, 0), (1, 300001, 20),
+    (1, 2200001, 32), (600, 70001, 3),
 ])
 def test_scores(rows, L, top, dtype):
     z, labels = make(rows, L, dtype)
