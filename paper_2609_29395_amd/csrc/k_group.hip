@@ -150,17 +150,20 @@ hipError_t launch_any(int mode, const GroupArgs &a, hipStream_t s) {
 
 }  // namespace
 
+// Pieces of a group's rows in a weight gradient: until there are two
+// workgroups for every CU (one where it takes the CU's LDS) of 128 rows or more
+// on average.  The tile is the one that the operands most likely take.
 int group_splits(int dtype, int G, int64_t rows, int n, int k) {
-  (void)dtype;
-  // pieces of a group's rows until about two workgroups per CU have a tile each, of 128 rows or more on average
-  const int64_t tiles = (int64_t)((n + 63) / 64) * ((k + 63) / 64) * G;
-  const int64_t want = (512 + tiles - 1) / tiles, most = rows / ((int64_t)128 * G);
+  const int tile = dtype == GCPSL_F32 ? 128 : n % 8 == 0 && k % 8 == 0 ? 256 : 64;
+  const int64_t tiles = (int64_t)((n + tile - 1) / tile) * ((k + tile - 1) / tile) * G;
+  const int64_t want = ((tile == 256 ? 256 : 512) + tiles - 1) / tiles, most = rows / ((int64_t)128 * G);
   return (int)(want < most ? want : most > 1 ? most : 1);
 }
 
 hipError_t launch_group(int dtype, int mode, const GroupArgs &a, hipStream_t s) {
   hipError_t e;
   if (group_tile_ok(dtype, a, mode)) e = launch_group_tile(mode, a, s);
+  else if (dtype == GCPSL_F32 && a.N >= 64) e = launch_group_f32(mode, a, s);
   else e = dtype == GCPSL_BF16 ? launch_any<bf16_t>(mode, a, s) : launch_any<float>(mode, a, s);
   if (e == hipSuccess && mode == GROUP_DW && a.splits > 1) {
     const int64_t n = (int64_t)a.G * a.M * (a.N + (a.db ? 1 : 0));
