@@ -13,6 +13,7 @@ constexpr int64_t kMaxTileLd = 1 << 22;
 
 bool group_tile_ok(int dtype, const GroupArgs &a, int mode);
 hipError_t launch_group_tile(int mode, const GroupArgs &a, hipStream_t s);
+bool group_f32_ok(const GroupArgs &a, int mode);
 hipError_t launch_group_f32(int mode, const GroupArgs &a, hipStream_t s);
 
 #define GROUP_DEVICE __device__ __forceinline__

@@ -163,7 +163,7 @@ int group_splits(int dtype, int G, int64_t rows, int n, int k) {
 hipError_t launch_group(int dtype, int mode, const GroupArgs &a, hipStream_t s) {
   hipError_t e;
   if (group_tile_ok(dtype, a, mode)) e = launch_group_tile(mode, a, s);
-  else if (dtype == GCPSL_F32 && a.N >= 64) e = launch_group_f32(mode, a, s);
+  else if (dtype == GCPSL_F32 && a.N >= 64 && group_f32_ok(a, mode)) e = launch_group_f32(mode, a, s);
   else e = dtype == GCPSL_BF16 ? launch_any<bf16_t>(mode, a, s) : launch_any<float>(mode, a, s);
   if (e == hipSuccess && mode == GROUP_DW && a.splits > 1) {
     const int64_t n = (int64_t)a.G * a.M * (a.N + (a.db ? 1 : 0));

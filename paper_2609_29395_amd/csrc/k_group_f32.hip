@@ -18,27 +18,30 @@
 // split, and terms of opposite sign could overflow where the sum does not)
 // takes its tile again with fp32 MFMAs.  A NaN is one in every term.
 //
-// Staging: threads 0..127 take the A operand, 128..255 the B operand, 32 values
-// each of a 32-deep k tile, loaded to registers one tile ahead, split and
-// written as 16-byte pieces of 8 consecutive k.  Operands whose rows run
-// across the sum are loaded as 8 rows x 4 columns a thread, so that the 8 k of
-// a column meet in one thread.  One 48 KB buffer: two workgroups share a CU
-// and one's staging overlaps the other's MFMAs.
+// Staging: threads 0..127 take the A operand, 128..255 the B operand, 16 values
+// each of a 16-deep k tile, loaded to registers two tiles ahead, split and
+// written to LDS one tile ahead as 16-byte pieces of 8 consecutive k; a tile
+// costs one barrier.  Operands whose rows run across the sum are loaded as 8
+// rows x 2 columns a thread, so that the 8 k of a column meet in one thread.
+// Two 24 KB buffers; two workgroups share a CU and one's splitting overlaps the
+// other's MFMAs.
 #include "group.h"
 
 namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int BM = 128, BN = 128, BK = 32;
-constexpr int PLANE = 128 * 64;  // bytes of one bf16 part of an operand's tile: 128 rows of 32
+constexpr int BM = 128, BN = 128, BK = 16;
+constexpr int PLANE = 128 * 32;  // bytes of one bf16 part of an operand's tile: 128 rows of 16
+constexpr int BUFFER = 6 * PLANE;
 constexpr float kHuge = 1.125899906842624e15f;  // 2^50: products below 2^100, and any sum of them finite
 
-// 16-byte piece c (8 k) of row r in a plane; the XOR spreads the 8 rows of a
-// fragment read, and (2-way) the rows of transposed writes, over the banks.
-__device__ __forceinline__ int at(int r, int c) { return r * 64 + ((c ^ (((r >> 1) ^ (r >> 3)) & 3)) * 16); }
+// 16-byte piece c (8 k) of row r in a plane; the XOR puts the 8 rows of a
+// fragment read on all banks.
+__device__ __forceinline__ int at(int r, int c) { return r * 32 + ((c ^ ((r >> 3) & 1)) * 16); }
 
 // Two values -> their three parts, packed.
 __device__ __forceinline__ void split2(float a, float b, uint32_t (&p)[3]) {
@@ -50,56 +53,50 @@ __device__ __forceinline__ void split2(float a, float b, uint32_t (&p)[3]) {
   }
 }
 
-// One thread's share of an operand's k tiles.  T: the operand's rows run
-// across the sum (k = row); else along it.
-template <bool T> struct Stage {
-  const float *p;  // T: row k0 + 8 chunk, column 4 quad; else row t / 4, k0 + 8 (t % 4)
-  int64_t ld;
-  int n, t;        // rows or columns inside, thread of 128
-  float v[4][8];   // [row or column][k]
+typedef float f32x2_any __attribute__((ext_vector_type(2), aligned(4)));
 
-  __device__ __forceinline__ void init(const float *base, int64_t ld_, int n_, int t_) {
-    ld = ld_; n = n_; t = t_;
-    p = T ? base + (int64_t)(t >> 5) * 8 * ld + (t & 31) * 4 : base + (int64_t)(t >> 2) * ld + (t & 3) * 8;
-  }
-  // k tile at k0, `left` deep from there (all of it past the end gives zeros)
-  __device__ __forceinline__ void load(int k0, int left) {
+// One thread's share of an operand's k tiles.  T: the operand's rows run
+// across the sum (k = row): rows 8 chunk .. + 7 of a tile, two columns; else
+// along it: rows t / 2 and t / 2 + 64, k = 8 (t % 2) .. + 7 of a tile.  Rows and
+// columns past the n inside are taken as the last ones inside (what they give
+// is not stored), so that loads need no test: a thread whose columns pass the
+// end takes the last two instead.
+template <bool T> struct Stage {
+  const char *base;  // of the next tile
+  int64_t step;
+  int row, chunk;                // first row (T: column) in LDS, 16-byte piece
+  uint32_t off[T ? 1 : 2], ld;   // byte offsets of the thread's loads, bytes of a row
+  float v[2][8];                 // [row or column][k]
+
+  __device__ __forceinline__ void init(const float *p, int64_t ld_, int n, int t) {
+    base = (const char *)p;
+    ld = (uint32_t)ld_ * 4u;
+    step = T ? ld_ * (4 * BK) : 4 * BK;
     if constexpr (T) {
-      const int k = (t >> 5) * 8, c = (t & 31) * 4;
+      chunk = t >> 6;
+      row = min((t & 63) * 2, n - 2);  // -1 in a tile of one column, which is not the first
+      base -= 4;                       // offsets are not negative
+      off[0] = (uint32_t)chunk * 8u * ld + (uint32_t)(row + 1) * 4u;
+    } else {
+      chunk = t & 1;
+      row = t >> 1;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) off[j] = (uint32_t)min(row + j * 64, n - 1) * ld + (uint32_t)chunk * 32u;
+    }
+  }
+  // the next tile, all of it inside
+  __device__ __forceinline__ void load_all() {
+    if constexpr (T) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float *q = p + (int64_t)(k0 + i) * ld;
-        f32x4_any x{0.f, 0.f, 0.f, 0.f};
-        if (k + i < left) {
-          if (c + 4 <= n) {
-            x = *(const f32x4_any *)q;
-          } else {
-#pragma unroll
-            for (int j = 0; j < 3; ++j)
-              if (c + j < n) x[j] = q[j];
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j][i] = x[j];
+        const f32x2_any x = *(const f32x2_any *)(base + (off[0] + (uint32_t)i * ld));
+        v[0][i] = x[0];
+        v[1][i] = x[1];
       }
     } else {
-      const int k = (t & 3) * 8;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float *q = p + (int64_t)j * 32 * ld + k0;
-        f32x4_any x{0.f, 0.f, 0.f, 0.f}, y{0.f, 0.f, 0.f, 0.f};
-        if ((t >> 2) + j * 32 < n) {
-          if (k + 8 <= left) {
-            x = *(const f32x4_any *)q;
-            y = *(const f32x4_any *)(q + 4);
-          } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              if (k + i < left) x[i] = q[i];
-              if (k + 4 + i < left) y[i] = q[4 + i];
-            }
-          }
-        }
+      for (int j = 0; j < 2; ++j) {
+        const f32x4_any x = *(const f32x4_any *)(base + off[j]), y = *(const f32x4_any *)(base + (off[j] + 16u));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           v[j][i] = x[i];
@@ -107,12 +104,31 @@ template <bool T> struct Stage {
         }
       }
     }
+    base += step;
+  }
+  // the same with `left` values of k inside
+  __device__ __forceinline__ void load(int left) {
+    if (left >= BK) {
+      load_all();
+    } else if (left > 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int k = min(chunk * 8 + i, left - 1), d = k - chunk * 8;  // a k inside
+        const bool in = d == i;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int64_t o = T ? (int64_t)off[0] + (int64_t)d * ld + j * 4 : (int64_t)off[T ? 0 : j] + d * 4;
+          const float x = *(const float *)(base + o);
+          v[j][i] = in ? x : 0.f;
+        }
+      }
+    }
   }
   // splits the values and writes them; returns the largest magnitude so far
   __device__ __forceinline__ float write(char *planes, float top) const {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int r = T ? (t & 31) * 4 + j : (t >> 2) + j * 32, c = T ? t >> 5 : t & 3;
+    for (int j = 0; j < 2; ++j) {
+      const int r = T ? (row + j) & 127 : row + j * 64;  // (a negative row's place holds nothing of the tile)
       u32x4 w[3];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -123,23 +139,23 @@ template <bool T> struct Stage {
         for (int k = 0; k < 3; ++k) w[k][i] = s[k];
       }
 #pragma unroll
-      for (int k = 0; k < 3; ++k) *(u32x4 *)(planes + k * PLANE + at(r, c)) = w[k];
+      for (int k = 0; k < 3; ++k) *(u32x4 *)(planes + k * PLANE + at(r, chunk)) = w[k];
     }
     return top;
   }
 };
 
-__device__ __forceinline__ f32x4_t mma(const u32x4 &a, const u32x4 &b, const f32x4_t &c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0,
+__device__ __forceinline__ f32x16_t mma(const u32x4 &a, const u32x4 &b, const f32x16_t &c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0,
                                                  0, 0);
 }
 
 template <int MODE>
 __global__ void __launch_bounds__(256, 2) group_f32_kernel(GroupArgs a, int NT) {
   constexpr bool AT = MODE == GROUP_DW, BT = MODE != GROUP_FWD;
-  __shared__ __attribute__((aligned(16))) char lds[6 * PLANE];
+  __shared__ __attribute__((aligned(16))) char lds[2 * BUFFER];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave >> 1, wn = wave & 1, li = lane & 15, lg = lane >> 4;
+  const int wm = wave >> 1, wn = wave & 1, li = lane & 31, lg = lane >> 5;
   int g, row0, rows, c0, Q, split = 0, nt;
   const float *A = (const float *)a.a, *B = (const float *)a.b;
   if constexpr (MODE == GROUP_DW) {
@@ -168,55 +184,71 @@ __global__ void __launch_bounds__(256, 2) group_f32_kernel(GroupArgs a, int NT) 
   const int cols = min(BN, a.N - c0);
   const bool sums = MODE == GROUP_DW && a.db != nullptr && nt == 0;
 
-  // [column fragment][row fragment], a lane holds 4 consecutive columns of one
-  // row: the sums of h h' and of the small terms
-  f32x4_t big[4][4], small[4][4];
+  // [column fragment][row fragment] of 32 x 32: the sums of h h' and of the
+  // small terms.  A lane holds, in four groups of four, columns 8 i + 4 lg ..
+  // + 3 of row li.
+  f32x16_t big[2][2], small[2][2];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) big[i][j] = small[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  float top = 0.f, colsum[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) big[i][j][r] = small[i][j][r] = 0.f;
+  float top = 0.f, colsum[2] = {0.f, 0.f};
 
-  // the fragments' multiplication for one k tile
-  const auto multiply = [&] {
-    u32x4 x[4][3];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int k = 0; k < 3; ++k) x[j][k] = *(const u32x4 *)(lds + k * PLANE + at(wm * 64 + j * 16 + li, lg));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      u32x4 w[3];
-#pragma unroll
-      for (int k = 0; k < 3; ++k) w[k] = *(const u32x4 *)(lds + (3 + k) * PLANE + at(wn * 64 + i * 16 + li, lg));
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        small[i][j] = mma(w[2], x[j][0], small[i][j]);
-        small[i][j] = mma(w[0], x[j][2], small[i][j]);
-        small[i][j] = mma(w[1], x[j][1], small[i][j]);
-        small[i][j] = mma(w[1], x[j][0], small[i][j]);
-        small[i][j] = mma(w[0], x[j][1], small[i][j]);
-        big[i][j] = mma(w[0], x[j][0], big[i][j]);
-      }
-    }
-  };
   const auto run = [&](auto &stage, bool is_a) {
-    stage.load(0, Q);
-    for (int k0 = 0; k0 < Q; k0 += BK) {
-      __syncthreads();
-      top = stage.write(lds + (is_a ? 0 : 3 * PLANE), top);
+    char *const mine = lds + (is_a ? 0 : 3 * PLANE);
+    const auto write = [&](int p) {  // to buffer p
+      top = stage.write(mine + p * BUFFER, top);
       if constexpr (MODE == GROUP_DW) {
         if (sums && is_a) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
+          for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int i = 0; i < 8; ++i) colsum[j] += stage.v[j][i];
         }
       }
+    };
+    // k tile k0 of buffer p, the next one to LDS and the one after it to
+    // registers; `all` says that the latter is inside as a whole (the loop of
+    // such tiles has no branch, at whose end a load would be waited for)
+    const auto tile = [&](int k0, int p, auto all) {
+      u32x4 x[2][3], w[2][3];
+      const char *now = lds + p * BUFFER;
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          x[j][k] = *(const u32x4 *)(now + k * PLANE + at(wm * 64 + j * 32 + li, lg));
+          w[j][k] = *(const u32x4 *)(now + (3 + k) * PLANE + at(wn * 64 + j * 32 + li, lg));
+        }
+      if constexpr (decltype(all)::value) {
+        write(1 - p);
+        stage.load_all();
+      } else if (Q - k0 > BK) {
+        write(1 - p);
+        stage.load(Q - k0 - 2 * BK);
+      }
+      // term by term, so that a sum's next product is four MFMAs away
+      constexpr int kw[6] = {2, 0, 1, 1, 0, 0}, kx[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+      for (int k = 0; k < 6; ++k)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            if (k < 5) small[i][j] = mma(w[i][kw[k]], x[j][kx[k]], small[i][j]);
+            else big[i][j] = mma(w[i][kw[k]], x[j][kx[k]], big[i][j]);
+          }
       __syncthreads();
-      stage.load(k0 + BK, Q - k0 - BK);
-      multiply();
-    }
+    };
+    stage.load(Q);
+    if (Q > 0) write(0);
+    stage.load(Q - BK);
+    __syncthreads();
+    int k0 = 0, p = 0;
+    for (; k0 + 3 * BK <= Q; k0 += BK, p ^= 1) tile(k0, p, std::true_type{});
+    for (; k0 < Q; k0 += BK, p ^= 1) tile(k0, p, std::false_type{});
   };
   if constexpr (AT == BT) {
     Stage<AT> stage;
@@ -234,50 +266,55 @@ __global__ void __launch_bounds__(256, 2) group_f32_kernel(GroupArgs a, int NT) 
   }
 
   if (__syncthreads_or(top >= kHuge)) {
-    // again in fp32, from memory: lane (li, lg) takes k = 4 s + lg of step s
+    // again in fp32, from memory: lane (li, lg) takes k = 2 s + lg of step s
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) big[i][j] = small[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int k0 = 0; k0 < Q; k0 += 4) {
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) big[i][j][r] = small[i][j][r] = 0.f;
+    for (int k0 = 0; k0 < Q; k0 += 2) {
       const int k = k0 + lg;
-      float x[4], w[4];
+      float x[2], w[2];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int r = wm * 64 + j * 16 + li, c = wn * 64 + j * 16 + li;
+      for (int j = 0; j < 2; ++j) {
+        const int r = wm * 64 + j * 32 + li, c = wn * 64 + j * 32 + li;
         x[j] = r < rows && k < Q ? (AT ? A[(int64_t)k * a.lda + r] : A[(int64_t)r * a.lda + k]) : 0.f;
         w[j] = c < cols && k < Q ? (BT ? B[(int64_t)k * a.ldb + c] : B[(int64_t)c * a.ldb + k]) : 0.f;
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) big[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[i], x[j], big[i][j], 0, 0, 0);
+        for (int j = 0; j < 2; ++j) big[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[i], x[j], big[i][j], 0, 0, 0);
     }
   }
 
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int m = wm * 64 + j * 16 + li;
+  for (int j = 0; j < 2; ++j) {
+    const int m = wm * 64 + j * 32 + li;
     if (m >= rows) continue;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int c = c0 + wn * 64 + i * 16 + 4 * lg;
-      if (c >= a.N) continue;
-      const f32x4_t v = big[i][j] + small[i][j];
-      if constexpr (MODE == GROUP_DW) store_grad(a, g, split, row0 + m, c, v);
-      else finish<float, MODE>(a, g, row0 + m, c, v);
-    }
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int c = c0 + wn * 64 + i * 32 + 8 * q + 4 * lg;
+        if (c >= a.N) continue;
+        f32x4_t v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = big[i][j][4 * q + r] + small[i][j][4 * q + r];
+        if constexpr (MODE == GROUP_DW) store_grad(a, g, split, row0 + m, c, v);
+        else finish<float, MODE>(a, g, row0 + m, c, v);
+      }
   }
   if constexpr (MODE == GROUP_DW) {
-    if (sums) {  // each column's four shares, of 8 of every 32 rows
+    if (sums) {  // each column's two shares, of 8 of every 16 rows
       float *part = (float *)lds;
       __syncthreads();
       if (tid < 128)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) part[(tid >> 5) * 128 + (tid & 31) * 4 + j] = colsum[j];
+        for (int j = 0; j < 2; ++j) part[(tid >> 6) * 128 + ((min((tid & 63) * 2, rows - 2) + j) & 127)] = colsum[j];
       __syncthreads();
-      if (tid < rows)
-        store_bias_grad(a, g, split, row0 + tid, (part[tid] + part[128 + tid]) + (part[256 + tid] + part[384 + tid]));
+      if (tid < rows) store_bias_grad(a, g, split, row0 + tid, part[tid] + part[128 + tid]);
     }
   }
 }
@@ -292,6 +329,12 @@ template <int MODE> hipError_t run_mode(const GroupArgs &a, hipStream_t s) {
 }
 
 }  // namespace
+
+// Two columns at least wherever the operands' rows run across the sum, and
+// row strides whose offsets within a tile fit 32 bits.
+bool group_f32_ok(const GroupArgs &a, int mode) {
+  return a.lda <= kMaxTileLd && a.ldb <= kMaxTileLd && (mode == GROUP_FWD || a.N >= 2) && (mode != GROUP_DW || a.M >= 2);
+}
 
 hipError_t launch_group_f32(int mode, const GroupArgs &a, hipStream_t s) {
   return mode == GROUP_FWD ? run_mode<GROUP_FWD>(a, s)
