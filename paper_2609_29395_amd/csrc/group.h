@@ -87,20 +87,47 @@ GROUP_DEVICE void block_order(uint32_t t, uint32_t MT, uint32_t NT, int &mt, int
   mt = __builtin_amdgcn_readfirstlane((int)(block * 8u + in % high));
 }
 
-// Tile of workgroup b of a product whose row tiles the offsets make, false if
-// it has none: tiles are dealt to the XCDs in contiguous runs of block_order,
-// so that an XCD's 32 workgroups share their operands in its L2.
-GROUP_DEVICE bool tile_of(const int32_t *off, int G, int rows, int bm, int NT, uint32_t b, int &mt, int &nt) {
+// Group, rows [row0, row1) and column tile of workgroup b of a product whose
+// row tiles (bm rows) the offsets make; false if it has none.  The tiles are
+// dealt to the XCDs in contiguous runs of block_order, so that an XCD's
+// workgroups share their operands in its L2.  The tiles past the last whole
+// round of one per CU are halved if they still make no more than a round: a CU
+// that takes one tile more than the others makes them wait for half as long.
+// (What a result is the sum of, and in which order, does not depend on it.)
+constexpr uint32_t kCUs = 256;
+GROUP_DEVICE bool tile_of(const int32_t *off, int G, int rows, int bm, int NT_, uint32_t b, int &g, int &row0, int &row1,
+                          int &nt) {
   uint32_t MT = 0;
+  const uint32_t NT = (uint32_t)NT_;
   for (int base = 0; base < G; base += 64) {
     LaneTiles l;
     MT = lane_tiles(off, G, rows, bm, base, MT, l);
   }
   MT = __builtin_amdgcn_readfirstlane(MT);
-  const uint32_t all = MT * (uint32_t)NT;
-  if (b >= all) return false;
-  block_order(xcd_swizzle(b, all), MT, (uint32_t)NT, mt, nt);
-  return true;
+  const uint32_t all = MT * NT, full = all / kCUs * kCUs, rest = all - full;
+  uint32_t t = b;
+  int half = -1, mt;
+  if (b < full) {
+    t = xcd_swizzle(b, full);
+  } else if (2 * rest <= kCUs) {
+    if (b >= full + 2 * rest) return false;
+    t = xcd_swizzle(b - full, 2 * rest);
+    half = __builtin_amdgcn_readfirstlane((int)(t & 1));
+    t = full + (t >> 1);
+  } else {
+    if (b >= all) return false;
+    t = full + xcd_swizzle(b - full, rest);
+  }
+  block_order(t, MT, NT, mt, nt);
+  if (!find_tile(off, G, rows, bm, mt, g, row0, row1)) return false;
+  if (half == 0) row1 = min(row1, row0 + bm / 2);
+  if (half == 1) row0 += bm / 2;
+  return row0 < row1;
+}
+// Workgroups of such a launch: as many tiles as any offsets can make, and the
+// halves.
+inline int64_t tile_blocks(int64_t rows, int G, int bm, int64_t NT) {
+  return (rows / bm + std::min<int64_t>(G, rows)) * NT + kCUs / 2;
 }
 
 // Four consecutive columns c .. c + 3 of row m of the result (forward, input

@@ -57,16 +57,17 @@ typedef float f32x2_any __attribute__((ext_vector_type(2), aligned(4)));
 
 // One thread's share of an operand's k tiles.  T: the operand's rows run
 // across the sum (k = row): rows 8 chunk .. + 7 of a tile, two columns; else
-// along it: rows t / 2 and t / 2 + 64, k = 8 (t % 2) .. + 7 of a tile.  Rows and
+// along it: rows t / 2 and (ROWS 2) t / 2 + 64, k = 8 (t % 2) .. + 7 of a tile.  Rows and
 // columns past the n inside are taken as the last ones inside (what they give
 // is not stored), so that loads need no test: a thread whose columns pass the
 // end takes the last two instead.
-template <bool T> struct Stage {
+template <bool T, int ROWS = 2> struct Stage {
   const char *base;  // of the next tile
   int64_t step;
   int row, chunk;                // first row (T: column) in LDS, 16-byte piece
+  static constexpr int J = T ? 2 : ROWS;
   uint32_t off[T ? 1 : 2], ld;   // byte offsets of the thread's loads, bytes of a row
-  float v[2][8];                 // [row or column][k]
+  float v[J][8];                 // [row or column][k]
 
   __device__ __forceinline__ void init(const float *p, int64_t ld_, int n, int t) {
     base = (const char *)p;
@@ -95,7 +96,7 @@ template <bool T> struct Stage {
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
+      for (int j = 0; j < J; ++j) {
         const f32x4_any x = *(const f32x4_any *)(base + off[j]), y = *(const f32x4_any *)(base + (off[j] + 16u));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -116,7 +117,7 @@ template <bool T> struct Stage {
         const int k = min(chunk * 8 + i, left - 1), d = k - chunk * 8;  // a k inside
         const bool in = d == i;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < J; ++j) {
           const int64_t o = T ? (int64_t)off[0] + (int64_t)d * ld + j * 4 : (int64_t)off[T ? 0 : j] + d * 4;
           const float x = *(const float *)(base + o);
           v[j][i] = in ? x : 0.f;
@@ -127,7 +128,7 @@ template <bool T> struct Stage {
   // splits the values and writes them; returns the largest magnitude so far
   __device__ __forceinline__ float write(char *planes, float top) const {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < J; ++j) {
       const int r = T ? (row + j) & 127 : row + j * 64;  // (a negative row's place holds nothing of the tile)
       u32x4 w[3];
 #pragma unroll
@@ -150,48 +151,31 @@ __device__ __forceinline__ f32x16_t mma(const u32x4 &a, const u32x4 &b, const f3
                                                  0, 0);
 }
 
-template <int MODE>
-__global__ void __launch_bounds__(256, 2) group_f32_kernel(GroupArgs a, int NT) {
+// Where a workgroup's tile is: A and B from its first row, column and k on.
+struct Tile {
+  const float *A, *B;
+  int g, row0, rows, c0, cols, Q, split;
+  bool sums;  // of A's columns, too (the bias gradient)
+};
+
+// The tile's sums and results; waves of 32 FJ x 64 outputs.
+template <int MODE, int FJ>
+__device__ __forceinline__ void group_f32_tile(const GroupArgs &a, const Tile &t, char *lds) {
   constexpr bool AT = MODE == GROUP_DW, BT = MODE != GROUP_FWD;
-  __shared__ __attribute__((aligned(16))) char lds[2 * BUFFER];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1, li = lane & 31, lg = lane >> 5;
-  int g, row0, rows, c0, Q, split = 0, nt;
-  const float *A = (const float *)a.a, *B = (const float *)a.b;
-  if constexpr (MODE == GROUP_DW) {
-    const uint32_t MT = (uint32_t)(a.M + BM - 1) / BM, tiles = MT * (uint32_t)NT, part = blockIdx.x / tiles;
-    int mt, q0, q1;
-    block_order(xcd_swizzle(blockIdx.x - part * tiles, tiles), MT, (uint32_t)NT, mt, nt);
-    row0 = mt * BM;
-    split = __builtin_amdgcn_readfirstlane((int)(part % (uint32_t)a.splits));
-    g = __builtin_amdgcn_readfirstlane((int)(part / (uint32_t)a.splits));
-    group_piece(a, g, split, q0, q1);
-    Q = q1 - q0;
-    rows = min(BM, a.M - row0);
-    c0 = nt * BN;
-    A += (int64_t)q0 * a.lda + row0;
-    B += (int64_t)q0 * a.ldb + c0;
-  } else {
-    int mt, row1;
-    if (!tile_of(a.off, a.G, a.M, BM, NT, blockIdx.x, mt, nt)) return;
-    if (!find_tile(a.off, a.G, a.M, BM, mt, g, row0, row1)) return;
-    rows = row1 - row0;
-    c0 = nt * BN;
-    Q = a.Q;
-    A += (int64_t)row0 * a.lda;
-    B += g * a.b_gs + (BT ? (int64_t)c0 : (int64_t)c0 * a.ldb);
-  }
-  const int cols = min(BN, a.N - c0);
-  const bool sums = MODE == GROUP_DW && a.db != nullptr && nt == 0;
+  const float *const A = t.A, *const B = t.B;
+  const int g = t.g, row0 = t.row0, rows = t.rows, c0 = t.c0, cols = t.cols, Q = t.Q, split = t.split;
+  const bool sums = t.sums;
 
   // [column fragment][row fragment] of 32 x 32: the sums of h h' and of the
   // small terms.  A lane holds, in four groups of four, columns 8 i + 4 lg ..
   // + 3 of row li.
-  f32x16_t big[2][2], small[2][2];
+  f32x16_t big[2][FJ], small[2][FJ];
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < FJ; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) big[i][j][r] = small[i][j][r] = 0.f;
   float top = 0.f, colsum[2] = {0.f, 0.f};
@@ -213,13 +197,13 @@ __global__ void __launch_bounds__(256, 2) group_f32_kernel(GroupArgs a, int NT) 
     // registers; `all` says that the latter is inside as a whole (the loop of
     // such tiles has no branch, at whose end a load would be waited for)
     const auto tile = [&](int k0, int p, auto all) {
-      u32x4 x[2][3], w[2][3];
+      u32x4 x[FJ][3], w[2][3];
       const char *now = lds + p * BUFFER;
 #pragma unroll
       for (int k = 0; k < 3; ++k)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          x[j][k] = *(const u32x4 *)(now + k * PLANE + at(wm * 64 + j * 32 + li, lg));
+          if (j < FJ) x[j][k] = *(const u32x4 *)(now + k * PLANE + at(wm * 32 * FJ + j * 32 + li, lg));
           w[j][k] = *(const u32x4 *)(now + (3 + k) * PLANE + at(wn * 64 + j * 32 + li, lg));
         }
       if constexpr (decltype(all)::value) {
@@ -236,7 +220,7 @@ __global__ void __launch_bounds__(256, 2) group_f32_kernel(GroupArgs a, int NT) 
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
+          for (int j = 0; j < FJ; ++j) {
             if (k < 5) small[i][j] = mma(w[i][kw[k]], x[j][kx[k]], small[i][j]);
             else big[i][j] = mma(w[i][kw[k]], x[j][kx[k]], big[i][j]);
           }
@@ -256,7 +240,7 @@ __global__ void __launch_bounds__(256, 2) group_f32_kernel(GroupArgs a, int NT) 
     else stage.init(B, a.ldb, cols, tid - 128);
     run(stage, wave < 2);
   } else if (wave < 2) {
-    Stage<AT> stage;
+    Stage<AT, FJ> stage;
     stage.init(A, a.lda, rows, tid);
     run(stage, true);
   } else {
@@ -270,28 +254,28 @@ __global__ void __launch_bounds__(256, 2) group_f32_kernel(GroupArgs a, int NT) 
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+      for (int j = 0; j < FJ; ++j)
 #pragma unroll
         for (int r = 0; r < 16; ++r) big[i][j][r] = small[i][j][r] = 0.f;
     for (int k0 = 0; k0 < Q; k0 += 2) {
       const int k = k0 + lg;
-      float x[2], w[2];
+      float x[FJ], w[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const int r = wm * 64 + j * 32 + li, c = wn * 64 + j * 32 + li;
-        x[j] = r < rows && k < Q ? (AT ? A[(int64_t)k * a.lda + r] : A[(int64_t)r * a.lda + k]) : 0.f;
+        const int r = wm * 32 * FJ + j * 32 + li, c = wn * 64 + j * 32 + li;
+        if (j < FJ) x[j] = r < rows && k < Q ? (AT ? A[(int64_t)k * a.lda + r] : A[(int64_t)r * a.lda + k]) : 0.f;
         w[j] = c < cols && k < Q ? (BT ? B[(int64_t)k * a.ldb + c] : B[(int64_t)c * a.ldb + k]) : 0.f;
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) big[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[i], x[j], big[i][j], 0, 0, 0);
+        for (int j = 0; j < FJ; ++j) big[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[i], x[j], big[i][j], 0, 0, 0);
     }
   }
 
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int m = wm * 64 + j * 32 + li;
+  for (int j = 0; j < FJ; ++j) {
+    const int m = wm * 32 * FJ + j * 32 + li;
     if (m >= rows) continue;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -319,10 +303,43 @@ __global__ void __launch_bounds__(256, 2) group_f32_kernel(GroupArgs a, int NT) 
   }
 }
 
+template <int MODE>
+__global__ void __launch_bounds__(256, 2) group_f32_kernel(GroupArgs a, int NT) {
+  constexpr bool BT = MODE != GROUP_FWD;
+  __shared__ __attribute__((aligned(16))) char lds[2 * BUFFER];
+  Tile t{(const float *)a.a, (const float *)a.b, 0, 0, 0, 0, 0, a.Q, 0, false};
+  int nt;
+  if constexpr (MODE == GROUP_DW) {
+    const uint32_t MT = (uint32_t)(a.M + BM - 1) / BM, tiles = MT * (uint32_t)NT, part = blockIdx.x / tiles;
+    int mt, q0, q1;
+    block_order(xcd_swizzle(blockIdx.x - part * tiles, tiles), MT, (uint32_t)NT, mt, nt);
+    t.row0 = mt * BM;
+    t.split = __builtin_amdgcn_readfirstlane((int)(part % (uint32_t)a.splits));
+    t.g = __builtin_amdgcn_readfirstlane((int)(part / (uint32_t)a.splits));
+    group_piece(a, t.g, t.split, q0, q1);
+    t.Q = q1 - q0;
+    t.rows = min(BM, a.M - t.row0);
+    t.c0 = nt * BN;
+    t.A += (int64_t)q0 * a.lda + t.row0;
+    t.B += (int64_t)q0 * a.ldb + t.c0;
+  } else {
+    int row1;
+    if (!tile_of(a.off, a.G, a.M, BM, NT, blockIdx.x, t.g, t.row0, row1, nt)) return;
+    t.rows = row1 - t.row0;
+    t.c0 = nt * BN;
+    t.A += (int64_t)t.row0 * a.lda;
+    t.B += t.g * a.b_gs + (BT ? (int64_t)t.c0 : (int64_t)t.c0 * a.ldb);
+  }
+  t.cols = min(BN, a.N - t.c0);
+  t.sums = MODE == GROUP_DW && a.db != nullptr && nt == 0;
+  if (MODE != GROUP_DW && t.rows <= BM / 2) group_f32_tile<MODE, 1>(a, t, lds);
+  else group_f32_tile<MODE, 2>(a, t, lds);
+}
+
 template <int MODE> hipError_t run_mode(const GroupArgs &a, hipStream_t s) {
   const int64_t NT = (a.N + BN - 1) / BN;
   const int64_t blocks = MODE == GROUP_DW ? (int64_t)((a.M + BM - 1) / BM) * NT * a.splits * a.G
-                                          : ((int64_t)a.M / BM + std::min(a.G, a.M)) * NT;
+                                          : tile_blocks(a.M, a.G, BM, NT);
   if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(group_f32_kernel<MODE>, dim3((uint32_t)blocks), dim3(256), 0, s, a, (int)NT);
   return hipGetLastError();

@@ -37,7 +37,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int BM = 256, BN = 256, BK = 64, HALF = 128;  // rows and columns of a tile, depth, rows of a half
 constexpr int HALF_BYTES = HALF * BK * 2;               // 16 KB: two 16-byte copies a thread
 constexpr int STAGE = 4 * HALF_BYTES;                   // A's halves, B's halves
-constexpr int LDS_BYTES = 2 * STAGE;
+constexpr int LDS_BYTES = 9 * HALF_BYTES;  // two stages, or three of half a tile
 constexpr int FM = 4, FN = 2;  // 16-row and 16-column fragments of a wave in a half
 
 // XOR on the 16-byte chunk of LDS row `row`: rows of 128 bytes (8 chunks) and
@@ -233,9 +233,8 @@ __global__ void __launch_bounds__(512, 2) group_tile_kernel(GroupArgs a, int NT)
     A = (const char *)a.a + ((int64_t)q0 * a.lda + row0) * 2;
     B = (const char *)a.b + ((int64_t)q0 * a.ldb + c0) * 2;
   } else {
-    int mt, row1;
-    if (!tile_of(a.off, a.G, a.M, BM, NT, blockIdx.x, mt, nt)) return;
-    if (!find_tile(a.off, a.G, a.M, BM, mt, g, row0, row1)) return;
+    int row1;
+    if (!tile_of(a.off, a.G, a.M, BM, NT, blockIdx.x, g, row0, row1, nt)) return;
     rows = row1 - row0;
     c0 = nt * BN;
     Q = a.Q;
@@ -290,20 +289,6 @@ __global__ void __launch_bounds__(512, 2) group_tile_kernel(GroupArgs a, int NT)
 
   FragA fa;
   FragB first[2], second;  // B's halves; the first one of this tile and of the next
-  // what the phases before the first would have copied
-  copyB(0, 0);
-  copyA(0, 0);
-  copyB(0, 1);
-  copyA(0, 1);
-  copyB(1, 0);
-  copyA(1, 0);
-  copyB(1, 1);
-  wait_copies<8>();
-  barrier();
-  read_first(first[0], rb, BT);
-  barrier();
-  if (wm == 1) barrier();  // the second team is one slot behind
-
   const auto multiply = [&](int h, const FragB &b0) {
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_setprio(1);
@@ -344,6 +329,51 @@ __global__ void __launch_bounds__(512, 2) group_tile_kernel(GroupArgs a, int NT)
 #pragma unroll
     for (int i = 0; i < 2; ++i) r[i] = rb[i] + d;
   };
+  if (MODE != GROUP_DW && rows <= HALF) {
+    // Tiles of the first A half only: one phase a k tile, 32 MFMAs against 16
+    // fragment reads, in three buffers of A's half and B's two.  A k tile is
+    // copied two phases before it is read.
+    const auto copy = [&](int kt, int p) {
+      char *const d = dst + p * (3 * HALF_BYTES);
+      issue<AT>(ca, A, stepA, kt, Q, 0, d);
+      issue<BT>(cb, B, stepB, kt, Q, 0, d + HALF_BYTES);
+      issue<BT>(cb, B, stepB, kt, Q, 1, d + 2 * HALF_BYTES);
+    };
+    copy(0, 0);
+    copy(1, 1);
+    wait_copies<6>();
+    barrier();
+    if (wm == 1) barrier();
+    for (int kt = 0, p = 0; kt < nk; ++kt) {
+      copy(kt + 2, p == 0 ? 2 : p - 1);
+      uint32_t xa[NA], xb[2];
+      at_a(p * (3 * HALF_BYTES), xa);
+      at_b(p * (3 * HALF_BYTES), xb);  // (rb is past A's two halves: this is B's second one)
+      read_phase(fa, second, xa, xb, Mode{});
+      at_b(p * (3 * HALF_BYTES) - HALF_BYTES, xb);
+      read_first(first[0], xb, BT);
+      wait_copies<6>();
+      barrier();
+      multiply(0, first[0]);
+      barrier();
+      p = p == 2 ? 0 : p + 1;
+    }
+    if (wm == 0) barrier();
+  } else {
+  // what the phases before the first would have copied
+  copyB(0, 0);
+  copyA(0, 0);
+  copyB(0, 1);
+  copyA(0, 1);
+  copyB(1, 0);
+  copyA(1, 0);
+  copyB(1, 1);
+  wait_copies<8>();
+  barrier();
+  read_first(first[0], rb, BT);
+  barrier();
+  if (wm == 1) barrier();  // the second team is one slot behind
+
   const auto tile = [&](int kt, auto P) {
     constexpr int p = decltype(P)::value;  // kt % 2
     uint32_t xa[NA], xb[2];
@@ -375,6 +405,7 @@ __global__ void __launch_bounds__(512, 2) group_tile_kernel(GroupArgs a, int NT)
   }
   if (kt < nk) tile(kt, std::integral_constant<int, 0>{});
   if (wm == 0) barrier();
+  }
   wait_copies<0>();  // no copy may land in LDS after the workgroup's end
 
 #pragma unroll
@@ -415,7 +446,7 @@ template <int MODE> hipError_t run(const GroupArgs &a, hipStream_t s) {
   }
   const int64_t NT = (a.N + BN - 1) / BN;
   const int64_t blocks = MODE == GROUP_DW ? (int64_t)((a.M + BM - 1) / BM) * NT * a.splits * a.G
-                                          : ((int64_t)a.M / BM + std::min(a.G, a.M)) * NT;
+                                          : tile_blocks(a.M, a.G, BM, NT);
   if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(group_tile_kernel<MODE>, dim3((uint32_t)blocks), dim3(512), LDS_BYTES, s, a, (int)NT);
   return hipGetLastError();
