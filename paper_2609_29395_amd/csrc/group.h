@@ -24,37 +24,68 @@ GROUP_DEVICE void group_rows(const int32_t *off, int g, int rows, int &begin, in
   end = min(max(off[g + 1], begin), rows);
 }
 
-// Piece `split` of a group's rows in a weight gradient.
-GROUP_DEVICE void group_piece(const GroupArgs &a, int g, int split, int &q0, int &q1) {
-  group_rows(a.off, g, a.Q, q0, q1);
-  const int piece = ((q1 - q0 + a.splits - 1) / a.splits + 63) / 64 * 64;
-  const int64_t at = q0 + (int64_t)split * piece;  // may pass the group's end, and 31 bits
-  q0 = (int)min(at, (int64_t)q1);
-  q1 = (int)min(at + piece, (int64_t)q1);
-  q0 = __builtin_amdgcn_readfirstlane(q0);
-  q1 = __builtin_amdgcn_readfirstlane(q1);
+// A group of `count` rows in tiles of bm rows, or (pieces) in about count / bm
+// equal parts, at least one.
+template <bool PIECES> GROUP_DEVICE uint32_t parts_of(int count, int bm) {
+  return PIECES ? max(((uint32_t)count + (uint32_t)bm / 2u) / (uint32_t)bm, 1u)
+                : (uint32_t)(count + bm - 1) / (uint32_t)bm;
 }
 
-// Row tiles (bm rows, none spans groups) of groups [base, base + 64), one a
-// lane: their rows, the tiles before the group (`before` are those before
-// the first) and its own.  Returns the tiles up to the last.
+// Row tiles (bm rows, none spans groups) or pieces of groups [base, base +
+// 64), one group a lane: its rows, the parts before it (`before` are those
+// before the first) and its own.  Returns the parts up to the last.
 struct LaneTiles {
   int begin, end;
   uint32_t first, tiles;
 };
-GROUP_DEVICE uint32_t lane_tiles(const int32_t *off, int G, int rows, int bm, int base, uint32_t before, LaneTiles &l) {
-  const int lane = threadIdx.x & 63;
-  l.begin = l.end = 0;
-  if (base + lane < G) group_rows(off, base + lane, rows, l.begin, l.end);
-  l.tiles = (uint32_t)(l.end - l.begin + bm - 1) / (uint32_t)bm;
-  uint32_t sum = l.tiles;
+GROUP_DEVICE uint32_t lane_scan(uint32_t v) {  // inclusive sum over the lanes
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t v = __shfl_up(sum, d, 64);
-    if (lane >= d) sum += v;
+    const uint32_t u = __shfl_up(v, d, 64);
+    if ((threadIdx.x & 63) >= d) v += u;
   }
+  return v;
+}
+template <bool PIECES = false>
+GROUP_DEVICE uint32_t lane_tiles(const int32_t *off, int G, int rows, int bm, int base, uint32_t before, LaneTiles &l) {
+  const int i = base + (int)(threadIdx.x & 63);
+  l.begin = l.end = 0;
+  l.tiles = 0;
+  if (i < G) {
+    group_rows(off, i, rows, l.begin, l.end);
+    l.tiles = parts_of<PIECES>(l.end - l.begin, bm);
+  }
+  const uint32_t sum = lane_scan(l.tiles);
   l.first = before + sum - l.tiles;
   return before + __shfl(sum, 63, 64);
+}
+
+// Piece t of a weight gradient: its group, rows [q0, q1) and place among the
+// partials (-1 if the group is one piece); false if there are not that many.
+// (Offsets that decrease can make groups overlap and more partials than there
+// is room for: those are left out.)
+GROUP_DEVICE bool find_piece(const GroupArgs &a, int t, int &g, int &q0, int &q1, int &slot) {
+  uint32_t before = 0, slots = 0;
+  for (int base = 0; base < a.G; base += 64) {
+    LaneTiles l;
+    before = lane_tiles<true>(a.off, a.G, a.Q, a.piece, base, before, l);
+    const uint32_t own = l.tiles > 1 ? l.tiles : 0, sum = lane_scan(own);
+    const uint64_t hit = __ballot((uint32_t)t - l.first < l.tiles);
+    if (hit) {
+      const int i = __ffsll((unsigned long long)hit) - 1;
+      const int begin = __shfl(l.begin, i, 64), end = __shfl(l.end, i, 64);
+      const int n = (int)__shfl(l.tiles, i, 64), k = t - (int)__shfl(l.first, i, 64);
+      const int part = ((end - begin + n - 1) / n + 63) / 64 * 64;
+      const int64_t at = begin + (int64_t)k * part;  // may pass the group's end, and 31 bits
+      g = __builtin_amdgcn_readfirstlane(base + i);
+      q0 = __builtin_amdgcn_readfirstlane((int)min(at, (int64_t)end));
+      q1 = __builtin_amdgcn_readfirstlane((int)min(at + part, (int64_t)end));
+      slot = __builtin_amdgcn_readfirstlane(n > 1 ? (int)(slots + __shfl(sum - own, i, 64)) + k : -1);
+      return slot < a.slots;
+    }
+    slots += __shfl(sum, 63, 64);
+  }
+  return false;
 }
 
 // Group and rows of row tile t; false if there are not that many.  Every wave
@@ -203,10 +234,10 @@ GROUP_DEVICE void finish(const GroupArgs &a, int g, int m, int c, const V &acc) 
     if (c + r < a.N) ((T *)a.out)[(int64_t)m * a.ldo + c + r] = ElemT<T>::from_f(v[r]);
 }
 
-// Four columns of a weight gradient, to its place or (pieces) to a partial.
-template <typename V> GROUP_DEVICE void store_grad(const GroupArgs &a, int g, int split, int m, int c, const V &acc) {
-  float *out = a.splits > 1 ? a.part + (((int64_t)split * a.G + g) * a.M + m) * a.N + c
-                            : (float *)a.out + g * a.out_gs + (int64_t)m * a.ldo + c;
+// Four columns of a weight gradient, to its place or (slot >= 0) to a partial.
+template <typename V> GROUP_DEVICE void store_grad(const GroupArgs &a, int g, int slot, int m, int c, const V &acc) {
+  float *out = slot >= 0 ? a.part + ((int64_t)slot * a.M + m) * a.N + c
+                         : (float *)a.out + g * a.out_gs + (int64_t)m * a.ldo + c;
   if (c + 4 <= a.N) {
     *(f32x4_any *)out = f32x4_any{acc[0], acc[1], acc[2], acc[3]};
   } else {
@@ -215,7 +246,11 @@ template <typename V> GROUP_DEVICE void store_grad(const GroupArgs &a, int g, in
       if (c + r < a.N) out[r] = acc[r];
   }
 }
-GROUP_DEVICE void store_bias_grad(const GroupArgs &a, int g, int split, int m, float v) {
-  if (a.splits > 1) a.part_db[((int64_t)split * a.G + g) * a.M + m] = v;
+GROUP_DEVICE void store_bias_grad(const GroupArgs &a, int g, int slot, int m, float v) {
+  if (slot >= 0) a.part_db[(int64_t)slot * a.M + m] = v;
   else a.db[g * a.db_gs + m] = v;
 }
+
+// Workgroups of a weight gradient of `tiles` tiles a piece: as many pieces as
+// any offsets can make.
+inline int64_t piece_blocks(const GroupArgs &a, int64_t tiles) { return ((int64_t)a.Q / a.piece + a.G) * tiles; }

@@ -47,14 +47,12 @@ __global__ void __launch_bounds__(256) group_any_kernel(GroupArgs a, int NT) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int li = lane & 15, lg = lane >> 4;
   const int nt = blockIdx.x % NT;
-  int g, row0, row1, q0 = 0, q1 = a.Q, mt = blockIdx.x / NT, split = 0;
+  int g, row0, row1, q0 = 0, q1 = a.Q, mt = blockIdx.x / NT, slot = -1;
   if constexpr (MODE == GROUP_DW) {
     const int MT = (a.M + BM - 1) / BM;
-    split = mt / MT % a.splits;
-    g = mt / MT / a.splits;
+    if (!find_piece(a, mt / MT, g, q0, q1, slot)) return;
     row0 = mt % MT * BM;
     row1 = min(a.M, row0 + BM);
-    group_piece(a, g, split, q0, q1);
   } else {
     if (!find_tile(a.off, a.G, a.M, BM, mt, g, row0, row1)) return;
   }
@@ -103,29 +101,40 @@ __global__ void __launch_bounds__(256) group_any_kernel(GroupArgs a, int NT) {
       const int m = row0 + wm * 32 + j * 16 + li, c = c0 + wn * 32 + i * 16 + 4 * lg;
       if (m >= row1) continue;
       if constexpr (MODE == GROUP_DW) {
-        if (c < a.N) store_grad(a, g, split, m, c, acc[i][j]);
+        if (c < a.N) store_grad(a, g, slot, m, c, acc[i][j]);
       } else {
         if (c < a.N) finish<T, MODE>(a, g, m, c, acc[i][j]);
       }
     }
   if (MODE == GROUP_DW && a.db && nt == 0 && tid < BM && row0 + tid < row1)
-    store_bias_grad(a, g, split, row0 + tid, rowsum);
+    store_bias_grad(a, g, slot, row0 + tid, rowsum);
 }
 
-// Weight gradient in pieces: the pieces' sums, in order.
-__global__ void __launch_bounds__(256) group_join_kernel(GroupArgs a) {
-  const int64_t per = (int64_t)a.M * a.N, all = per * a.G, all_db = (int64_t)a.M * a.G;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i < all) {
-    float s = 0.f;
-    for (int k = 0; k < a.splits; ++k) s += a.part[k * all + i];
-    const int64_t g = i / per, r = i - g * per;
-    ((float *)a.out)[g * a.out_gs + r / a.N * a.ldo + r % a.N] = s;
-  } else if (a.db && i - all < all_db) {
-    const int64_t j = i - all;
-    float s = 0.f;
-    for (int k = 0; k < a.splits; ++k) s += a.part_db[k * all_db + j];
-    a.db[j / a.M * a.db_gs + j % a.M] = s;
+// Weight gradient in pieces: the pieces' sums, in order.  A workgroup takes
+// 1,024 entries of one group's weights and biases.
+__global__ void __launch_bounds__(256) group_join_kernel(GroupArgs a, uint32_t blocks) {
+  const int g = (int)(blockIdx.x / blocks);
+  uint32_t before = 0, slots = 0, n = 0, first = 0;
+  for (int base = 0; base <= g; base += 64) {
+    LaneTiles l;
+    before = lane_tiles<true>(a.off, a.G, a.Q, a.piece, base, before, l);
+    const uint32_t own = l.tiles > 1 ? l.tiles : 0, sum = lane_scan(own);
+    if (g < base + 64) {
+      n = __shfl(own, g - base, 64);
+      first = slots + __shfl(sum - own, g - base, 64);
+    }
+    slots += __shfl(sum, 63, 64);
+  }
+  if (n == 0 || first + n > (uint32_t)a.slots) return;
+  const int64_t per = (int64_t)a.M * a.N, begin = (int64_t)(blockIdx.x - g * blocks) * 1024;
+  for (int64_t i = begin + threadIdx.x; i < min(begin + 1024, per + (a.db ? a.M : 0)); i += 256) {
+    const bool bias = i >= per;
+    const float *p = bias ? a.part_db + (int64_t)first * a.M + (i - per) : a.part + first * per + i;
+    const int64_t step = bias ? a.M : per;
+    float s = p[0];
+    for (uint32_t k = 1; k < n; ++k) s += p[k * step];
+    if (bias) a.db[g * a.db_gs + (i - per)] = s;
+    else ((float *)a.out)[g * a.out_gs + i] = s;
   }
 }
 
@@ -133,7 +142,7 @@ template <typename T>
 hipError_t launch_any(int mode, const GroupArgs &a, hipStream_t s) {
   const int NT = (a.N + 63) / 64;
   if (mode == GROUP_DW) {
-    const int64_t blocks = (int64_t)((a.M + 63) / 64) * NT * a.splits * a.G;
+    const int64_t blocks = piece_blocks(a, (int64_t)((a.M + 63) / 64) * NT);
     if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((group_any_kernel<T, GROUP_DW>), dim3((uint32_t)blocks), dim3(256), 0, s, a, NT);
     return hipGetLastError();
@@ -150,14 +159,20 @@ hipError_t launch_any(int mode, const GroupArgs &a, hipStream_t s) {
 
 }  // namespace
 
-// Pieces of a group's rows in a weight gradient: until there are two
-// workgroups for every CU (one where it takes the CU's LDS) of 128 rows or more
-// on average.  The tile is the one that the operands most likely take.
-int group_splits(int dtype, int G, int64_t rows, int n, int k) {
-  const int tile = dtype == GCPSL_F32 ? 128 : n % 8 == 0 && k % 8 == 0 ? 256 : 64;
-  const int64_t tiles = (int64_t)((n + tile - 1) / tile) * ((k + tile - 1) / tile) * G;
-  const int64_t want = ((tile == 256 ? 256 : 512) + tiles - 1) / tiles, most = rows / ((int64_t)128 * G);
-  return (int)(want < most ? want : most > 1 ? most : 1);
+// A piece takes the rows that a workgroup has if they are shared evenly over
+// one round of workgroups on the chip (`per_cu` a CU), but enough of them that
+// its products take longer than its partial, written and read again: 1,024 in
+// bf16 (256 x 256 outputs: 15 us against 10), 512 in fp32 or of tiles of 64 x 64.
+// The tile is the one that the operands most likely take.
+GroupPieces group_pieces(int dtype, int G, int64_t rows, int n, int k) {
+  (void)G;
+  const bool big = dtype == GCPSL_BF16 && n % 8 == 0 && k % 8 == 0;
+  const int64_t tile = big ? 256 : dtype == GCPSL_F32 ? 128 : 64, slots = kCUs * (big ? 1 : dtype == GCPSL_F32 ? 2 : 4);
+  const int64_t tiles = ((n + tile - 1) / tile) * ((k + tile - 1) / tile);
+  const int64_t even = tiles >= slots ? rows : rows * tiles / slots;
+  const int64_t piece = std::min<int64_t>(std::max<int64_t>(even, big ? 1024 : 512), 1 << 30);
+  // a group of p > 1 pieces has more than (p - 1/2) piece >= 3/4 p piece rows
+  return {(int)piece, rows * 2 >= piece * 3 ? (int)(rows * 4 / (piece * 3)) : 0};
 }
 
 hipError_t launch_group(int dtype, int mode, const GroupArgs &a, hipStream_t s) {
@@ -165,9 +180,10 @@ hipError_t launch_group(int dtype, int mode, const GroupArgs &a, hipStream_t s) 
   if (group_tile_ok(dtype, a, mode)) e = launch_group_tile(mode, a, s);
   else if (dtype == GCPSL_F32 && a.N >= 64 && group_f32_ok(a, mode)) e = launch_group_f32(mode, a, s);
   else e = dtype == GCPSL_BF16 ? launch_any<bf16_t>(mode, a, s) : launch_any<float>(mode, a, s);
-  if (e == hipSuccess && mode == GROUP_DW && a.splits > 1) {
-    const int64_t n = (int64_t)a.G * a.M * (a.N + (a.db ? 1 : 0));
-    hipLaunchKernelGGL(group_join_kernel, dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, s, a);
+  if (e == hipSuccess && mode == GROUP_DW && a.slots > 0) {
+    const int64_t n = ((int64_t)a.M * (a.N + (a.db ? 1 : 0)) + 1023) / 1024;
+    if (n * a.G > INT32_MAX) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL(group_join_kernel, dim3((uint32_t)(n * a.G)), dim3(256), 0, s, a, (uint32_t)n);
     e = hipGetLastError();
   }
   return e;

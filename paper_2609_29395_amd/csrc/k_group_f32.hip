@@ -154,7 +154,7 @@ __device__ __forceinline__ f32x16_t mma(const u32x4 &a, const u32x4 &b, const f3
 // Where a workgroup's tile is: A and B from its first row, column and k on.
 struct Tile {
   const float *A, *B;
-  int g, row0, rows, c0, cols, Q, split;
+  int g, row0, rows, c0, cols, Q, slot;
   bool sums;  // of A's columns, too (the bias gradient)
 };
 
@@ -165,7 +165,7 @@ __device__ __forceinline__ void group_f32_tile(const GroupArgs &a, const Tile &t
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1, li = lane & 31, lg = lane >> 5;
   const float *const A = t.A, *const B = t.B;
-  const int g = t.g, row0 = t.row0, rows = t.rows, c0 = t.c0, cols = t.cols, Q = t.Q, split = t.split;
+  const int g = t.g, row0 = t.row0, rows = t.rows, c0 = t.c0, cols = t.cols, Q = t.Q, slot = t.slot;
   const bool sums = t.sums;
 
   // [column fragment][row fragment] of 32 x 32: the sums of h h' and of the
@@ -286,7 +286,7 @@ __device__ __forceinline__ void group_f32_tile(const GroupArgs &a, const Tile &t
         f32x4_t v;
 #pragma unroll
         for (int r = 0; r < 4; ++r) v[r] = big[i][j][4 * q + r] + small[i][j][4 * q + r];
-        if constexpr (MODE == GROUP_DW) store_grad(a, g, split, row0 + m, c, v);
+        if constexpr (MODE == GROUP_DW) store_grad(a, g, slot, row0 + m, c, v);
         else finish<float, MODE>(a, g, row0 + m, c, v);
       }
   }
@@ -298,7 +298,7 @@ __device__ __forceinline__ void group_f32_tile(const GroupArgs &a, const Tile &t
 #pragma unroll
         for (int j = 0; j < 2; ++j) part[(tid >> 6) * 128 + ((min((tid & 63) * 2, rows - 2) + j) & 127)] = colsum[j];
       __syncthreads();
-      if (tid < rows) store_bias_grad(a, g, split, row0 + tid, part[tid] + part[128 + tid]);
+      if (tid < rows) store_bias_grad(a, g, slot, row0 + tid, part[tid] + part[128 + tid]);
     }
   }
 }
@@ -307,16 +307,14 @@ template <int MODE>
 __global__ void __launch_bounds__(256, 2) group_f32_kernel(GroupArgs a, int NT) {
   constexpr bool BT = MODE != GROUP_FWD;
   __shared__ __attribute__((aligned(16))) char lds[2 * BUFFER];
-  Tile t{(const float *)a.a, (const float *)a.b, 0, 0, 0, 0, 0, a.Q, 0, false};
+  Tile t{(const float *)a.a, (const float *)a.b, 0, 0, 0, 0, 0, a.Q, -1, false};
   int nt;
   if constexpr (MODE == GROUP_DW) {
     const uint32_t MT = (uint32_t)(a.M + BM - 1) / BM, tiles = MT * (uint32_t)NT, part = blockIdx.x / tiles;
     int mt, q0, q1;
     block_order(xcd_swizzle(blockIdx.x - part * tiles, tiles), MT, (uint32_t)NT, mt, nt);
     t.row0 = mt * BM;
-    t.split = __builtin_amdgcn_readfirstlane((int)(part % (uint32_t)a.splits));
-    t.g = __builtin_amdgcn_readfirstlane((int)(part / (uint32_t)a.splits));
-    group_piece(a, t.g, t.split, q0, q1);
+    if (!find_piece(a, (int)part, t.g, q0, q1, t.slot)) return;
     t.Q = q1 - q0;
     t.rows = min(BM, a.M - t.row0);
     t.c0 = nt * BN;
@@ -338,7 +336,7 @@ __global__ void __launch_bounds__(256, 2) group_f32_kernel(GroupArgs a, int NT) 
 
 template <int MODE> hipError_t run_mode(const GroupArgs &a, hipStream_t s) {
   const int64_t NT = (a.N + BN - 1) / BN;
-  const int64_t blocks = MODE == GROUP_DW ? (int64_t)((a.M + BM - 1) / BM) * NT * a.splits * a.G
+  const int64_t blocks = MODE == GROUP_DW ? piece_blocks(a, (int64_t)((a.M + BM - 1) / BM) * NT)
                                           : tile_blocks(a.M, a.G, BM, NT);
   if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(group_f32_kernel<MODE>, dim3((uint32_t)blocks), dim3(256), 0, s, a, (int)NT);

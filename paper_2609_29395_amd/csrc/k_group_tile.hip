@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(512, 2) group_tile_kernel(GroupArgs a, int NT)
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 2, wn = wave & 3, li = lane & 15, lg = lane >> 4;
 
-  int g, row0, rows, c0, Q, split = 0, nt;
+  int g, row0, rows, c0, Q, slot = -1, nt;
   const char *A, *B;
   if constexpr (MODE == GROUP_DW) {
     const int MT = (a.M + BM - 1) / BM;
@@ -223,10 +223,8 @@ __global__ void __launch_bounds__(512, 2) group_tile_kernel(GroupArgs a, int NT)
     int mt;
     block_order(xcd_swizzle(blockIdx.x - part * tiles, tiles), (uint32_t)MT, (uint32_t)NT, mt, nt);
     row0 = mt * BM;
-    split = __builtin_amdgcn_readfirstlane((int)(part % (uint32_t)a.splits));
-    g = __builtin_amdgcn_readfirstlane((int)(part / (uint32_t)a.splits));
     int q0, q1;
-    group_piece(a, g, split, q0, q1);
+    if (!find_piece(a, (int)part, g, q0, q1, slot)) return;
     Q = q1 - q0;
     rows = min(BM, a.M - row0);
     c0 = nt * BN;
@@ -421,7 +419,7 @@ __global__ void __launch_bounds__(512, 2) group_tile_kernel(GroupArgs a, int NT)
           const int c = c0 + k * HALF + (wn * FN + j) * 16 + 4 * lg;
           if (c >= a.N) continue;
           if constexpr (MODE == GROUP_DW) {
-            store_grad(a, g, split, row0 + m, c, acc[h][i][k][j]);
+            store_grad(a, g, slot, row0 + m, c, acc[h][i][k][j]);
           } else {
             finish4<bf16_t, MODE>(a, g, row0 + m, c, acc[h][i][k][j]);
           }
@@ -431,7 +429,7 @@ __global__ void __launch_bounds__(512, 2) group_tile_kernel(GroupArgs a, int NT)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int m = h * HALF + (wm * FM + wn) * 16 + li;
-      if (m < rows) store_bias_grad(a, g, split, row0 + m, bacc[h][0]);
+      if (m < rows) store_bias_grad(a, g, slot, row0 + m, bacc[h][0]);
     }
   }
 }
@@ -445,7 +443,7 @@ template <int MODE> hipError_t run(const GroupArgs &a, hipStream_t s) {
     once.mark();
   }
   const int64_t NT = (a.N + BN - 1) / BN;
-  const int64_t blocks = MODE == GROUP_DW ? (int64_t)((a.M + BM - 1) / BM) * NT * a.splits * a.G
+  const int64_t blocks = MODE == GROUP_DW ? piece_blocks(a, (int64_t)((a.M + BM - 1) / BM) * NT)
                                           : tile_blocks(a.M, a.G, BM, NT);
   if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(group_tile_kernel<MODE>, dim3((uint32_t)blocks), dim3(512), LDS_BYTES, s, a, (int)NT);

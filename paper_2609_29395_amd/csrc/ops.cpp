@@ -94,7 +94,6 @@ extern "C" int gcpsl_group_forward(int32_t dtype, int32_t G, int64_t rows, int32
   a.out = y; a.ldo = ldy;
   a.bias = bias; a.bias_gs = bias_gs;
   a.relu = relu != 0;
-  a.splits = 1;
   return launched(launch_group(dtype, GROUP_FWD, a, reinterpret_cast<hipStream_t>(stream)));
 }
 
@@ -120,15 +119,12 @@ extern "C" int gcpsl_group_input_grad(int32_t dtype, int32_t G, int64_t rows, in
   a.b = w; a.ldb = k; a.b_gs = w_gs;
   a.out = dx; a.ldo = lddx;
   a.gate = gate; a.ldg = ldgate;
-  a.splits = 1;
   return launched(launch_group(dtype, GROUP_DX, a, reinterpret_cast<hipStream_t>(stream)));
 }
 
 namespace {
 // Partials of a weight gradient: the weights' and then the biases'.
-size_t partial_bytes(int splits, int G, int n, int k) {
-  return splits > 1 ? sizeof(float) * (size_t)splits * G * n * ((size_t)k + 1) : 0;
-}
+size_t partial_bytes(const GroupPieces &p, int n, int k) { return sizeof(float) * (size_t)p.slots * n * ((size_t)k + 1); }
 }  // namespace
 
 extern "C" int gcpsl_group_workspace_bytes(int32_t dtype, int32_t G, int64_t rows, int32_t n, int32_t k,
@@ -137,7 +133,7 @@ extern "C" int gcpsl_group_workspace_bytes(int32_t dtype, int32_t G, int64_t row
   if (!bytes) return fail(GCPSL_EINVAL, "null output");
   alignas(4) static const int32_t none = 0;
   CHECK(bad_groups(dtype, G, rows, n, k, &none));
-  *bytes = partial_bytes(group_splits(dtype, G, rows, n, k), G, n, k);
+  *bytes = partial_bytes(group_pieces(dtype, G, rows, n, k), n, k);
   return GCPSL_OK;
 }
 
@@ -155,10 +151,12 @@ extern "C" int gcpsl_group_weight_grad(int32_t dtype, int32_t G, int64_t rows, i
   CHECK(bad_stride(db_gs));
   if (G > 1 && (dw_gs < (int64_t)n * k || (db && db_gs < n))) return fail(GCPSL_EINVAL, "groups of an output overlap");
   GroupArgs a{};
-  a.splits = group_splits(dtype, G, rows, n, k);
-  if (partial_bytes(a.splits, G, n, k) > workspace_bytes) return fail(GCPSL_EINVAL, "workspace too small");
-  if (a.splits > 1 && (!workspace || !aligned(workspace, 16)))
+  const GroupPieces pieces = group_pieces(dtype, G, rows, n, k);
+  if (partial_bytes(pieces, n, k) > workspace_bytes) return fail(GCPSL_EINVAL, "workspace too small");
+  if (pieces.slots && (!workspace || !aligned(workspace, 16)))
     return fail(GCPSL_EINVAL, "workspace null or not 16-byte aligned");
+  a.piece = pieces.piece;
+  a.slots = pieces.slots;
   a.off = offsets;
   a.G = G; a.M = n; a.N = k; a.Q = (int)rows;
   a.a = dy; a.lda = lddy;
@@ -166,7 +164,7 @@ extern "C" int gcpsl_group_weight_grad(int32_t dtype, int32_t G, int64_t rows, i
   a.out = dw; a.ldo = k; a.out_gs = dw_gs;
   a.db = db; a.db_gs = db_gs;
   a.part = (float *)workspace;
-  a.part_db = a.part + (size_t)a.splits * G * n * k;
+  a.part_db = a.part ? a.part + (size_t)a.slots * n * k : nullptr;
   return launched(launch_group(dtype, GROUP_DW, a, reinterpret_cast<hipStream_t>(stream)));
 }
 

@@ -53,11 +53,16 @@ struct GroupArgs {
   const void *gate;         // input grad: rows of N, or null
   int64_t ldg;
   Drop drop;                // forward: applied to the result; input grad: its scale multiplies where the gate is > 0
-  int splits;               // weight grad: pieces of a group's rows
-  float *part, *part_db;    // weight grad with splits > 1: [splits][G][M][N] and [splits][G][M]
+  // weight grad: a group of c rows is summed in max(1, round(c / piece)) pieces; those of groups of more than one
+  // go to partials, [slots][M][N] and [slots][M]
+  int piece, slots;
+  float *part, *part_db;
 };
-// Splits of a weight gradient's sums (host; the workspace holds the partials).
-int group_splits(int dtype, int G, int64_t rows, int n, int k);
+// Rows of a piece of a weight gradient's sums and the partials that this can make (host).
+struct GroupPieces {
+  int piece, slots;
+};
+GroupPieces group_pieces(int dtype, int G, int64_t rows, int n, int k);
 hipError_t launch_group(int dtype, int mode, const GroupArgs &a, hipStream_t s);
 
 // ------------------------------------------------------------ label scores
