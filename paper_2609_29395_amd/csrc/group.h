@@ -60,55 +60,6 @@ GROUP_DEVICE uint32_t lane_tiles(const int32_t *off, int G, int rows, int bm, in
   return before + __shfl(sum, 63, 64);
 }
 
-// Piece t of a weight gradient: its group, rows [q0, q1) and place among the
-// partials (-1 if the group is one piece); false if there are not that many.
-// (Offsets that decrease can make groups overlap and more partials than there
-// is room for: those are left out.)
-GROUP_DEVICE bool find_piece(const GroupArgs &a, int t, int &g, int &q0, int &q1, int &slot) {
-  uint32_t before = 0, slots = 0;
-  for (int base = 0; base < a.G; base += 64) {
-    LaneTiles l;
-    before = lane_tiles<true>(a.off, a.G, a.Q, a.piece, base, before, l);
-    const uint32_t own = l.tiles > 1 ? l.tiles : 0, sum = lane_scan(own);
-    const uint64_t hit = __ballot((uint32_t)t - l.first < l.tiles);
-    if (hit) {
-      const int i = __ffsll((unsigned long long)hit) - 1;
-      const int begin = __shfl(l.begin, i, 64), end = __shfl(l.end, i, 64);
-      const int n = (int)__shfl(l.tiles, i, 64), k = t - (int)__shfl(l.first, i, 64);
-      const int part = ((end - begin + n - 1) / n + 63) / 64 * 64;
-      const int64_t at = begin + (int64_t)k * part;  // may pass the group's end, and 31 bits
-      g = __builtin_amdgcn_readfirstlane(base + i);
-      q0 = __builtin_amdgcn_readfirstlane((int)min(at, (int64_t)end));
-      q1 = __builtin_amdgcn_readfirstlane((int)min(at + part, (int64_t)end));
-      slot = __builtin_amdgcn_readfirstlane(n > 1 ? (int)(slots + __shfl(sum - own, i, 64)) + k : -1);
-      return slot < a.slots;
-    }
-    slots += __shfl(sum, 63, 64);
-  }
-  return false;
-}
-
-// Group and rows of row tile t; false if there are not that many.  Every wave
-// scans by itself.  (A tile is checked against its group's own rows: offsets
-// that decrease can make groups overlap, but no row outside [0, rows) is
-// touched.)
-GROUP_DEVICE bool find_tile(const int32_t *off, int G, int rows, int bm, int t, int &g, int &row0, int &row1) {
-  uint32_t before = 0;
-  for (int base = 0; base < G; base += 64) {
-    LaneTiles l;
-    before = lane_tiles(off, G, rows, bm, base, before, l);
-    const uint64_t hit = __ballot((uint32_t)t - l.first < l.tiles);
-    if (hit) {
-      const int i = __ffsll((unsigned long long)hit) - 1;
-      g = __builtin_amdgcn_readfirstlane(base + i);
-      row0 = __builtin_amdgcn_readfirstlane(__shfl(l.begin, i, 64) + (t - (int)__shfl(l.first, i, 64)) * bm);
-      row1 = __builtin_amdgcn_readfirstlane(min(__shfl(l.end, i, 64), row0 + bm));
-      return true;
-    }
-  }
-  return false;
-}
-
 // Tile t of MT x NT in blocks of 8 row tiles by all column tiles, rows
 // fastest: 32 tiles in order are about 8 x 4 and share their operands.
 GROUP_DEVICE void block_order(uint32_t t, uint32_t MT, uint32_t NT, int &mt, int &nt) {
@@ -116,6 +67,57 @@ GROUP_DEVICE void block_order(uint32_t t, uint32_t MT, uint32_t NT, int &mt, int
   const uint32_t high = min(8u, MT - block * 8u);  // row tiles of this block
   nt = __builtin_amdgcn_readfirstlane((int)(in / high));
   mt = __builtin_amdgcn_readfirstlane((int)(block * 8u + in % high));
+}
+
+// Lane whose group has part t, -1 if none.  (A part is checked against its
+// group's own ones: offsets that decrease can make groups overlap, but no row
+// outside [0, rows) is touched.)
+GROUP_DEVICE int lane_of(const LaneTiles &l, uint32_t t) {
+  const uint64_t hit = __ballot(t - l.first < l.tiles);
+  return __ffsll((unsigned long long)hit) - 1;
+}
+
+// Piece and tile of workgroup b of a weight gradient of `tiles` tiles: the
+// piece's group, rows [q0, q1) and place among the partials (-1 if the group is
+// one piece); false if there is none.  Every XCD has an eighth of every piece's
+// tiles, so that unequal groups do not make unequal XCDs.  (Each XCD beginning
+// with another piece, so that their writing did not coincide, cost more in
+// operands read from memory: 716 against 640 us for 16 groups of 1,024 rows.)
+// (Offsets that decrease can make more partials than there is room for: those
+// are left out.)
+GROUP_DEVICE bool piece_of(const GroupArgs &a, uint32_t tiles, uint32_t b, int &g, int &q0, int &q1, int &slot,
+                           uint32_t &tile) {
+  LaneTiles l;
+  const uint32_t first64 = lane_tiles<true>(a.off, a.G, a.Q, a.piece, 0, 0, l);
+  uint32_t P = first64;
+  for (int base = 64; base < a.G; base += 64) {
+    LaneTiles m;
+    P = lane_tiles<true>(a.off, a.G, a.Q, a.piece, base, P, m);
+  }
+  P = __builtin_amdgcn_readfirstlane(P);
+  const uint32_t t = b / tiles;
+  if (t >= P) return false;
+  tile = xcd_swizzle(b - t * tiles, tiles);
+  uint32_t before = first64, slots = 0, own = l.tiles > 1 ? l.tiles : 0, sum = lane_scan(own);
+  int base = 0, i = lane_of(l, t);
+  while (i < 0) {
+    base += 64;
+    if (base >= a.G) return false;
+    slots += __shfl(sum, 63, 64);
+    before = lane_tiles<true>(a.off, a.G, a.Q, a.piece, base, before, l);
+    own = l.tiles > 1 ? l.tiles : 0;
+    sum = lane_scan(own);
+    i = lane_of(l, t);
+  }
+  const int begin = __shfl(l.begin, i, 64), end = __shfl(l.end, i, 64);
+  const int n = (int)__shfl(l.tiles, i, 64), k = (int)(t - __shfl(l.first, i, 64));
+  const int part = ((end - begin + n - 1) / n + 63) / 64 * 64;
+  const int64_t at = begin + (int64_t)k * part;  // may pass the group's end, and 31 bits
+  g = __builtin_amdgcn_readfirstlane(base + i);
+  q0 = __builtin_amdgcn_readfirstlane((int)min(at, (int64_t)end));
+  q1 = __builtin_amdgcn_readfirstlane((int)min(at + part, (int64_t)end));
+  slot = __builtin_amdgcn_readfirstlane(n > 1 ? (int)(slots + __shfl(sum - own, i, 64)) + k : -1);
+  return slot < a.slots;
 }
 
 // Group, rows [row0, row1) and column tile of workgroup b of a product whose
@@ -128,11 +130,12 @@ GROUP_DEVICE void block_order(uint32_t t, uint32_t MT, uint32_t NT, int &mt, int
 constexpr uint32_t kCUs = 256;
 GROUP_DEVICE bool tile_of(const int32_t *off, int G, int rows, int bm, int NT_, uint32_t b, int &g, int &row0, int &row1,
                           int &nt) {
-  uint32_t MT = 0;
-  const uint32_t NT = (uint32_t)NT_;
-  for (int base = 0; base < G; base += 64) {
-    LaneTiles l;
-    MT = lane_tiles(off, G, rows, bm, base, MT, l);
+  LaneTiles l;
+  const uint32_t NT = (uint32_t)NT_, first64 = lane_tiles(off, G, rows, bm, 0, 0, l);
+  uint32_t MT = first64;
+  for (int base = 64; base < G; base += 64) {
+    LaneTiles m;
+    MT = lane_tiles(off, G, rows, bm, base, MT, m);
   }
   MT = __builtin_amdgcn_readfirstlane(MT);
   const uint32_t all = MT * NT, full = all / kCUs * kCUs, rest = all - full;
@@ -150,7 +153,17 @@ GROUP_DEVICE bool tile_of(const int32_t *off, int G, int rows, int bm, int NT_, 
     t = full + xcd_swizzle(b - full, rest);
   }
   block_order(t, MT, NT, mt, nt);
-  if (!find_tile(off, G, rows, bm, mt, g, row0, row1)) return false;
+  uint32_t before = first64;
+  int base = 0, i = lane_of(l, (uint32_t)mt);
+  while (i < 0) {
+    base += 64;
+    if (base >= G) return false;
+    before = lane_tiles(off, G, rows, bm, base, before, l);
+    i = lane_of(l, (uint32_t)mt);
+  }
+  g = __builtin_amdgcn_readfirstlane(base + i);
+  row0 = __builtin_amdgcn_readfirstlane(__shfl(l.begin, i, 64) + (mt - (int)__shfl(l.first, i, 64)) * bm);
+  row1 = __builtin_amdgcn_readfirstlane(min(__shfl(l.end, i, 64), row0 + bm));
   if (half == 0) row1 = min(row1, row0 + bm / 2);
   if (half == 1) row0 += bm / 2;
   return row0 < row1;
@@ -212,6 +225,36 @@ GROUP_DEVICE void finish4(const GroupArgs &a, int g, int m, int c, const V &acc)
     *(u32x2_any *)out = u32x2_any{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])};
   else
     *(f32x4_any *)out = f32x4_any{v[0], v[1], v[2], v[3]};
+}
+
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+// Eight columns in bf16, all inside the result (their number is a multiple of 8).
+template <int MODE> GROUP_DEVICE void finish8(const GroupArgs &a, int g, int m, int c, const float *acc) {
+  float v[2][4], bias[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}, gate[2][4];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = acc[i];
+  if constexpr (MODE == GROUP_FWD) {
+    if (a.bias) {
+      const float *p = a.bias + g * a.bias_gs + c;
+      const f32x4_any x = *(const f32x4_any *)p, y = *(const f32x4_any *)(p + 4);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        bias[0][r] = x[r];
+        bias[1][r] = y[r];
+      }
+    }
+  } else if (a.gate) {
+    const u32x4_any b = *(const u32x4_any *)((const bf16_t *)a.gate + (int64_t)m * a.ldg + c);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      gate[i >> 2][i & 3] = __uint_as_float(i & 1 ? b[i >> 1] & 0xffff0000u : b[i >> 1] << 16);
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) epilogue<bf16_t, MODE>(a, g, m, c + 4 * i, bias[i], gate[i], v[i]);
+  *(u32x4_any *)((bf16_t *)a.out + (int64_t)m * a.ldo + c) =
+      u32x4_any{pack2_bf16(v[0][0], v[0][1]), pack2_bf16(v[0][2], v[0][3]), pack2_bf16(v[1][0], v[1][1]),
+                pack2_bf16(v[1][2], v[1][3])};
 }
 
 // The same where columns may lie outside.

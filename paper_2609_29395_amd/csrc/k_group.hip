@@ -46,15 +46,17 @@ __global__ void __launch_bounds__(256) group_any_kernel(GroupArgs a, int NT) {
   __shared__ __attribute__((aligned(16))) T la[BM * LD], lb[BN * LD];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int li = lane & 15, lg = lane >> 4;
-  const int nt = blockIdx.x % NT;
-  int g, row0, row1, q0 = 0, q1 = a.Q, mt = blockIdx.x / NT, slot = -1;
+  int g, row0, row1, q0 = 0, q1 = a.Q, slot = -1, nt;
   if constexpr (MODE == GROUP_DW) {
-    const int MT = (a.M + BM - 1) / BM;
-    if (!find_piece(a, mt / MT, g, q0, q1, slot)) return;
-    row0 = mt % MT * BM;
+    const uint32_t MT = (uint32_t)(a.M + BM - 1) / BM;
+    uint32_t t;
+    int mt;
+    if (!piece_of(a, MT * (uint32_t)NT, blockIdx.x, g, q0, q1, slot, t)) return;
+    block_order(t, MT, (uint32_t)NT, mt, nt);
+    row0 = mt * BM;
     row1 = min(a.M, row0 + BM);
   } else {
-    if (!find_tile(a.off, a.G, a.M, BM, mt, g, row0, row1)) return;
+    if (!tile_of(a.off, a.G, a.M, BM, NT, blockIdx.x, g, row0, row1, nt)) return;
   }
   const int c0 = nt * BN;
   const T *A = (const T *)a.a, *B = (const T *)a.b + g * a.b_gs;
@@ -110,8 +112,9 @@ __global__ void __launch_bounds__(256) group_any_kernel(GroupArgs a, int NT) {
     store_bias_grad(a, g, slot, row0 + tid, rowsum);
 }
 
-// Weight gradient in pieces: the pieces' sums, in order.  A workgroup takes
-// 1,024 entries of one group's weights and biases.
+// Weight gradient in pieces: the pieces' sums, in order.  `blocks` workgroups
+// for each group, whose weights and biases they share; those of a group of one
+// piece end at once.
 __global__ void __launch_bounds__(256) group_join_kernel(GroupArgs a, uint32_t blocks) {
   const int g = (int)(blockIdx.x / blocks);
   uint32_t before = 0, slots = 0, n = 0, first = 0;
@@ -126,15 +129,27 @@ __global__ void __launch_bounds__(256) group_join_kernel(GroupArgs a, uint32_t b
     slots += __shfl(sum, 63, 64);
   }
   if (n == 0 || first + n > (uint32_t)a.slots) return;
-  const int64_t per = (int64_t)a.M * a.N, begin = (int64_t)(blockIdx.x - g * blocks) * 1024;
-  for (int64_t i = begin + threadIdx.x; i < min(begin + 1024, per + (a.db ? a.M : 0)); i += 256) {
-    const bool bias = i >= per;
-    const float *p = bias ? a.part_db + (int64_t)first * a.M + (i - per) : a.part + first * per + i;
-    const int64_t step = bias ? a.M : per;
-    float s = p[0];
-    for (uint32_t k = 1; k < n; ++k) s += p[k * step];
-    if (bias) a.db[g * a.db_gs + (i - per)] = s;
-    else ((float *)a.out)[g * a.out_gs + i] = s;
+  const int64_t per = (int64_t)a.M * a.N, step = (int64_t)blocks * 1024;
+  const float *p = a.part + first * per;
+  float *out = (float *)a.out + g * a.out_gs;
+  for (int64_t i = ((blockIdx.x - g * blocks) * 256 + threadIdx.x) * 4ll; i < per; i += step) {
+    if (i + 4 <= per) {
+      f32x4_any s = *(const f32x4_any *)(p + i);
+      for (uint32_t k = 1; k < n; ++k) s += *(const f32x4_any *)(p + k * per + i);
+      *(f32x4_any *)(out + i) = s;
+    } else {
+      for (int64_t j = i; j < per; ++j) {
+        float s = p[j];
+        for (uint32_t k = 1; k < n; ++k) s += p[k * per + j];
+        out[j] = s;
+      }
+    }
+  }
+  if (!a.db) return;
+  for (int m = (int)((blockIdx.x - g * blocks) * 256 + threadIdx.x); m < a.M; m += (int)(blocks * 256)) {
+    float s = a.part_db[(int64_t)first * a.M + m];
+    for (uint32_t k = 1; k < n; ++k) s += a.part_db[(int64_t)(first + k) * a.M + m];
+    a.db[g * a.db_gs + m] = s;
   }
 }
 
@@ -147,9 +162,8 @@ hipError_t launch_any(int mode, const GroupArgs &a, hipStream_t s) {
     hipLaunchKernelGGL((group_any_kernel<T, GROUP_DW>), dim3((uint32_t)blocks), dim3(256), 0, s, a, NT);
     return hipGetLastError();
   }
-  const int64_t blocks = ((int64_t)a.M / 64 + min(a.G, a.M)) * NT;
+  const int64_t blocks = tile_blocks(a.M, a.G, 64, NT);
   if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
-  if (blocks == 0) return hipSuccess;
   if (mode == GROUP_FWD)
     hipLaunchKernelGGL((group_any_kernel<T, GROUP_FWD>), dim3((uint32_t)blocks), dim3(256), 0, s, a, NT);
   else
@@ -181,9 +195,10 @@ hipError_t launch_group(int dtype, int mode, const GroupArgs &a, hipStream_t s) 
   else if (dtype == GCPSL_F32 && a.N >= 64 && group_f32_ok(a, mode)) e = launch_group_f32(mode, a, s);
   else e = dtype == GCPSL_BF16 ? launch_any<bf16_t>(mode, a, s) : launch_any<float>(mode, a, s);
   if (e == hipSuccess && mode == GROUP_DW && a.slots > 0) {
-    const int64_t n = ((int64_t)a.M * (a.N + (a.db ? 1 : 0)) + 1023) / 1024;
-    if (n * a.G > INT32_MAX) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL(group_join_kernel, dim3((uint32_t)(n * a.G)), dim3(256), 0, s, a, (uint32_t)n);
+    // about eight workgroups a CU in all, of 1,024 entries or more
+    const int64_t most = ((int64_t)a.M * a.N + 1023) / 1024, share = std::max(1, 2048 / a.G);
+    const uint32_t n = (uint32_t)std::min(most, share);
+    hipLaunchKernelGGL(group_join_kernel, dim3(n * (uint32_t)a.G), dim3(256), 0, s, a, n);
     e = hipGetLastError();
   }
   return e;

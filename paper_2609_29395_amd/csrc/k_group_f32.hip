@@ -310,11 +310,12 @@ __global__ void __launch_bounds__(256, 2) group_f32_kernel(GroupArgs a, int NT) 
   Tile t{(const float *)a.a, (const float *)a.b, 0, 0, 0, 0, 0, a.Q, -1, false};
   int nt;
   if constexpr (MODE == GROUP_DW) {
-    const uint32_t MT = (uint32_t)(a.M + BM - 1) / BM, tiles = MT * (uint32_t)NT, part = blockIdx.x / tiles;
+    const uint32_t MT = (uint32_t)(a.M + BM - 1) / BM;
+    uint32_t tile;
     int mt, q0, q1;
-    block_order(xcd_swizzle(blockIdx.x - part * tiles, tiles), MT, (uint32_t)NT, mt, nt);
+    if (!piece_of(a, MT * (uint32_t)NT, blockIdx.x, t.g, q0, q1, t.slot, tile)) return;
+    block_order(tile, MT, (uint32_t)NT, mt, nt);
     t.row0 = mt * BM;
-    if (!find_piece(a, (int)part, t.g, q0, q1, t.slot)) return;
     t.Q = q1 - q0;
     t.rows = min(BM, a.M - t.row0);
     t.c0 = nt * BN;

@@ -37,7 +37,9 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int BM = 256, BN = 256, BK = 64, HALF = 128;  // rows and columns of a tile, depth, rows of a half
 constexpr int HALF_BYTES = HALF * BK * 2;               // 16 KB: two 16-byte copies a thread
 constexpr int STAGE = 4 * HALF_BYTES;                   // A's halves, B's halves
+constexpr int OUT_ROW = BN * 4 + 16;      // bytes of a row of results in LDS (padded against bank conflicts)
 constexpr int LDS_BYTES = 9 * HALF_BYTES;  // two stages, or three of half a tile
+static_assert(HALF * OUT_ROW <= LDS_BYTES, "half a tile of results");
 constexpr int FM = 4, FN = 2;  // 16-row and 16-column fragments of a wave in a half
 
 // XOR on the 16-byte chunk of LDS row `row`: rows of 128 bytes (8 chunks) and
@@ -218,13 +220,11 @@ __global__ void __launch_bounds__(512, 2) group_tile_kernel(GroupArgs a, int NT)
   const char *A, *B;
   if constexpr (MODE == GROUP_DW) {
     const int MT = (a.M + BM - 1) / BM;
-    // a group's tiles go to all XCDs alike, so that unequal groups do not make unequal XCDs
-    const uint32_t tiles = (uint32_t)MT * (uint32_t)NT, part = blockIdx.x / tiles;
-    int mt;
-    block_order(xcd_swizzle(blockIdx.x - part * tiles, tiles), (uint32_t)MT, (uint32_t)NT, mt, nt);
+    int mt, q0, q1;
+    uint32_t t;
+    if (!piece_of(a, (uint32_t)MT * (uint32_t)NT, blockIdx.x, g, q0, q1, slot, t)) return;
+    block_order(t, (uint32_t)MT, (uint32_t)NT, mt, nt);
     row0 = mt * BM;
-    int q0, q1;
-    if (!find_piece(a, (int)part, g, q0, q1, slot)) return;
     Q = q1 - q0;
     rows = min(BM, a.M - row0);
     c0 = nt * BN;
@@ -406,25 +406,34 @@ __global__ void __launch_bounds__(512, 2) group_tile_kernel(GroupArgs a, int NT)
   }
   wait_copies<0>();  // no copy may land in LDS after the workgroup's end
 
+  // The results go through LDS, a half at a time, so that whole rows of the
+  // tile are written at once.
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+  for (int h = 0; h < 2; ++h) {
+    if (h * HALF >= rows) break;
+    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const int m = h * HALF + (wm * FM + i) * 16 + li;
-      if (m >= rows) continue;
+    for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-          const int c = c0 + k * HALF + (wn * FN + j) * 16 + 4 * lg;
-          if (c >= a.N) continue;
-          if constexpr (MODE == GROUP_DW) {
-            store_grad(a, g, slot, row0 + m, c, acc[h][i][k][j]);
-          } else {
-            finish4<bf16_t, MODE>(a, g, row0 + m, c, acc[h][i][k][j]);
-          }
-        }
+        for (int j = 0; j < FN; ++j)
+          *(f32x4_t *)(smem + ((wm * FM + i) * 16 + li) * OUT_ROW + (k * HALF + (wn * FN + j) * 16 + 4 * lg) * 4) =
+              acc[h][i][k][j];
+    __syncthreads();
+    const int high = min(HALF, rows - h * HALF);
+    if constexpr (MODE == GROUP_DW) {  // a row a wave
+      const int c = c0 + lane * 4;
+      if (c < a.N)
+        for (int r = wave; r < high; r += 8)
+          store_grad(a, g, slot, row0 + h * HALF + r, c, *(const f32x4_t *)(smem + r * OUT_ROW + lane * 16));
+    } else {  // two rows a wave, eight columns a lane
+      const int c = (lane & 31) * 8;
+      if (c0 + c < a.N)
+        for (int r = wave * 2 + (lane >> 5); r < high; r += 16)
+          finish8<MODE>(a, g, row0 + h * HALF + r, c0 + c, (const float *)(smem + r * OUT_ROW) + c);
     }
+  }
   if (sums && lg == 0) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
