@@ -18,14 +18,14 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 // of consecutive q; both operands' fragments are 16-byte LDS reads.
 template <typename T> struct Any;
 template <> struct Any<bf16_t> {
-  static constexpr int BQ = 32, LD = 40;  // q a tile; elements per LDS row (padded against bank conflicts)
+  static constexpr int BQ = 64, LD = 72;  // q a tile; elements per LDS row (padded against bank conflicts)
   static __device__ __forceinline__ void mma(f32x4_t &acc, const bf16_t *a, const bf16_t *b) {
     acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8_t *)a, *(const bf16x8_t *)b, acc, 0, 0, 0);
   }
-  static constexpr int PER = 8;  // consecutive q of one lane's fragment
+  static constexpr int PER = 8, STEP = 32;  // consecutive q of one lane's fragment, q of a product
 };
 template <> struct Any<float> {
-  static constexpr int BQ = 16, LD = 20;
+  static constexpr int BQ = 64, LD = 68;
   // four products of four q each: q = 4 (lane / 16) + j in product j, the same for both operands
   static __device__ __forceinline__ void mma(f32x4_t &acc, const float *a, const float *b) {
     const float4 x = *(const float4 *)a, y = *(const float4 *)b;
@@ -34,7 +34,7 @@ template <> struct Any<float> {
     acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x.z, y.z, acc, 0, 0, 0);
     acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x.w, y.w, acc, 0, 0, 0);
   }
-  static constexpr int PER = 4;
+  static constexpr int PER = 4, STEP = 16;
 };
 
 template <typename T, int MODE>
@@ -70,27 +70,35 @@ __global__ void __launch_bounds__(256) group_any_kernel(GroupArgs a, int NT) {
   float rowsum = 0.f;  // weight grad: this thread's row of A (threads below BM)
 
   for (int q = q0; q < q1; q += BQ) {
+    // consecutive threads take consecutive addresses of the operand; rows,
+    // columns and q outside are loaded as the last ones inside, so that all
+    // loads are in flight together
+    T va[PT], vb[PT];
+#pragma unroll
+    for (int i = 0; i < PT; ++i) {
+      const int e = i * 256 + tid;
+      const int ra = min(row0 + (AT ? e % BM : e / BQ), row1 - 1), qa = min(q + (AT ? e / BM : e % BQ), q1 - 1);
+      const int rb = min(c0 + (BT ? e % BN : e / BQ), a.N - 1), qb = min(q + (BT ? e / BN : e % BQ), q1 - 1);
+      va[i] = AT ? A[(int64_t)qa * a.lda + ra] : A[(int64_t)ra * a.lda + qa];
+      vb[i] = BT ? B[(int64_t)qb * a.ldb + rb] : B[(int64_t)rb * a.ldb + qb];
+    }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < PT; ++i) {
       const int e = i * 256 + tid;
-      // consecutive threads take consecutive addresses of the operand
       const int ra = AT ? e % BM : e / BQ, qa = AT ? e / BM : e % BQ;
       const int rb = BT ? e % BN : e / BQ, qb = BT ? e / BN : e % BQ;
-      T va = 0, vb = 0;
-      if (row0 + ra < row1 && q + qa < q1)
-        va = AT ? A[(int64_t)(q + qa) * a.lda + row0 + ra] : A[(int64_t)(row0 + ra) * a.lda + q + qa];
-      if (c0 + rb < a.N && q + qb < q1)
-        vb = BT ? B[(int64_t)(q + qb) * a.ldb + c0 + rb] : B[(int64_t)(c0 + rb) * a.ldb + q + qb];
-      la[ra * LD + qa] = va;
-      lb[rb * LD + qb] = vb;
+      la[ra * LD + qa] = q + qa < q1 ? va[i] : T(0);
+      lb[rb * LD + qb] = q + qb < q1 ? vb[i] : T(0);
     }
     __syncthreads();
+    for (int k = 0; k < min(BQ, q1 - q); k += K::STEP)
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-        K::mma(acc[i][j], lb + (wn * 32 + i * 16 + li) * LD + lg * K::PER, la + (wm * 32 + j * 16 + li) * LD + lg * K::PER);
+        for (int j = 0; j < 2; ++j)
+          K::mma(acc[i][j], lb + (wn * 32 + i * 16 + li) * LD + k + lg * K::PER,
+                 la + (wm * 32 + j * 16 + li) * LD + k + lg * K::PER);
     if (MODE == GROUP_DW && tid < BM)
       for (int i = 0; i < BQ; ++i) rowsum += ElemT<T>::to_f(la[tid * LD + i]);
   }
@@ -173,15 +181,29 @@ hipError_t launch_any(int mode, const GroupArgs &a, hipStream_t s) {
 
 }  // namespace
 
+namespace {
+
+// Whether tiles of 256 x 256 (a group's last one half full on average) give half
+// of the CUs one.  With fewer the 128 x 128 kernel's are faster: 64 tiles,
+// 4 groups of 128 rows, 4096 -> 4096, 47 against 55 us; 16, 8 groups of 256, 512
+// -> 512, 12 against 16; as fast at 128, and slower from 144 on, 8 groups of
+// 1,024, 1024 -> 1024, 32 against 27.
+bool tiles_fill_half(int64_t row_tiles, int64_t cols) { return row_tiles * ((cols + 255) / 256) >= kCUs / 2; }
+bool fills_half(const GroupArgs &a, int mode) {
+  return tiles_fill_half(mode == GROUP_DW ? (int64_t)((a.M + 255) / 256) * a.G : ((int64_t)a.M + 128 * a.G) / 256, a.N);
+}
+
+}  // namespace
+
 // A piece takes the rows that a workgroup has if they are shared evenly over
-// one round of workgroups on the chip (`per_cu` a CU), but enough of them that
-// its products take longer than its partial, written and read again: 1,024 in
-// bf16 (256 x 256 outputs: 15 us against 10), 512 in fp32 or of tiles of 64 x 64.
-// The tile is the one that the operands most likely take.
+// one round of workgroups on the chip, but enough of them that its products
+// take longer than its partial, written and read again: 1,024 for tiles of
+// 256 x 256 (15 us against 10), 512 for the others.  The tile is the one that
+// the operands most likely take.
 GroupPieces group_pieces(int dtype, int G, int64_t rows, int n, int k) {
-  (void)G;
-  const bool big = dtype == GCPSL_BF16 && n % 8 == 0 && k % 8 == 0;
-  const int64_t tile = big ? 256 : dtype == GCPSL_F32 ? 128 : 64, slots = kCUs * (big ? 1 : dtype == GCPSL_F32 ? 2 : 4);
+  const bool big = dtype == GCPSL_BF16 && n % 8 == 0 && k % 8 == 0 &&
+                   tiles_fill_half((int64_t)((n + 255) / 256) * G, k);
+  const int64_t tile = big ? 256 : 128, slots = big ? kCUs : 2 * kCUs;
   const int64_t tiles = ((n + tile - 1) / tile) * ((k + tile - 1) / tile);
   const int64_t even = tiles >= slots ? rows : rows * tiles / slots;
   const int64_t piece = std::min<int64_t>(std::max<int64_t>(even, big ? 1024 : 512), 1 << 30);
@@ -191,7 +213,8 @@ GroupPieces group_pieces(int dtype, int G, int64_t rows, int n, int k) {
 
 hipError_t launch_group(int dtype, int mode, const GroupArgs &a, hipStream_t s) {
   hipError_t e;
-  if (group_tile_ok(dtype, a, mode)) e = launch_group_tile(mode, a, s);
+  if (group_tile_ok(dtype, a, mode) && fills_half(a, mode)) e = launch_group_tile(mode, a, s);
+  else if (group_mid_ok(dtype, a, mode)) e = launch_group_mid(mode, a, s);
   else if (dtype == GCPSL_F32 && a.N >= 64 && group_f32_ok(a, mode)) e = launch_group_f32(mode, a, s);
   else e = dtype == GCPSL_BF16 ? launch_any<bf16_t>(mode, a, s) : launch_any<float>(mode, a, s);
   if (e == hipSuccess && mode == GROUP_DW && a.slots > 0) {

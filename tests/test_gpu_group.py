@@ -59,6 +59,49 @@ def test_three_products(counts, n, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rest", range(8))
+@pytest.mark.parametrize("counts,n,k", [([5, 0, 70], 128, 64), ([200, 131], 264, 136), ([129], 8, 200)])
+def test_every_remainder_of_the_vectors(counts, n, k, rest, dtype):
+    """Widths that leave every number of elements past a 16-byte piece, at the end of the sum and of the columns, next
+    to values that must not be read as theirs."""
+    T, off, G = TYPES[dtype], offsets_of(counts), len(counts)
+    rows, n, k = off[-1], n + rest, k + rest
+    w = make(102, G, n, k, dtype=T, scale=k ** -0.5)
+    wide_x, wide_d = (torch.full((rows + 1, c + 5), float("nan"), dtype=T, device="cuda") for c in (k, n))
+    x, dy = make(101, rows, k, dtype=T), make(103, rows, n, dtype=T)
+    xv, dv = wide_x[:rows, :k], wide_d[:rows, :n]
+    xv.copy_(x)
+    dv.copy_(dy)
+    o = torch.tensor(off, dtype=torch.int32).cuda()
+    check(gcpsl.group_forward(xv, o, gpu(w)), *plain.forward(x, off, w)[:2], "forward")
+    check(gcpsl.group_input_grad(dv, o, gpu(w)), *plain.input_grad(dy, off, w)[:2], "input gradient")
+    dw, db = gcpsl.group_weight_grad(dv, xv, o)
+    want_w, want_b, bound_w, bound_b = plain.weight_grad(dy, x, off)
+    check(dw, want_w, bound_w, "weight gradient")
+    check(db, want_b, bound_b, "bias gradient")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("counts,n,k", [([4000, 0, 1300, 700], 48, 40), ([9000], 136, 128), ([3, 5000, 2000], 40, 33)])
+def test_weight_gradients_in_pieces(counts, n, k, dtype):
+    """Long sums of few outputs, taken in pieces that are joined; groups of one piece and of none beside them."""
+    T, off, G = TYPES[dtype], offsets_of(counts), len(counts)
+    x, dy = make(111, off[-1], k, dtype=T), make(112, off[-1], n, dtype=T)
+    assert gcpsl.group_workspace_bytes(dtype, G, off[-1], n, k) > 0
+    o = torch.tensor(off, dtype=torch.int32).cuda()
+    dw, db = gcpsl.group_weight_grad(gpu(dy), gpu(x), o)
+    want_w, want_b, bound_w, bound_b = plain.weight_grad(dy, x, off)
+    check(dw, want_w, bound_w)
+    check(db, want_b, bound_b)
+    again = gcpsl.group_weight_grad(gpu(dy), gpu(x), o)
+    assert torch.equal(again[0], dw) and torch.equal(again[1], db)
+    need = gcpsl.group_workspace_bytes(dtype, G, off[-1], n, k)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")  # NaN throughout
+    again = gcpsl.group_weight_grad(gpu(dy), gpu(x), o, workspace=ws, bias=False)
+    assert torch.equal(again[0], dw) and again[1] is None
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("counts,n,k", [([70, 0, 33], 65, 48), ([260, 5], 264, 128), ([2, 1, 0, 1], 512, 256)])
 def test_relu_dropout_and_the_gradient_through_them(counts, n, k, dtype):
     T, off, G, p, seed = TYPES[dtype], offsets_of(counts), len(counts), 0.3, 2 ** 63 + 11
