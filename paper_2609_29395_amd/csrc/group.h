@@ -13,6 +13,8 @@ constexpr int64_t kMaxTileLd = 1 << 22;
 
 bool group_tile_ok(int dtype, const GroupArgs &a, int mode);
 hipError_t launch_group_tile(int mode, const GroupArgs &a, hipStream_t s);
+bool group_few_ok(int dtype, const GroupArgs &a, int mode);
+hipError_t launch_group_few(int dtype, const GroupArgs &a, hipStream_t s);
 bool group_mid_ok(int dtype, const GroupArgs &a, int mode);
 hipError_t launch_group_mid(int mode, const GroupArgs &a, hipStream_t s);
 bool group_f32_ok(const GroupArgs &a, int mode);
@@ -130,6 +132,7 @@ GROUP_DEVICE bool piece_of(const GroupArgs &a, uint32_t tiles, uint32_t b, int &
 // that takes one tile more than the others makes them wait for half as long.
 // (What a result is the sum of, and in which order, does not depend on it.)
 constexpr uint32_t kCUs = 256;
+template <bool HALVES = true>
 GROUP_DEVICE bool tile_of(const int32_t *off, int G, int rows, int bm, int NT_, uint32_t b, int &g, int &row0, int &row1,
                           int &nt) {
   LaneTiles l;
@@ -145,7 +148,7 @@ GROUP_DEVICE bool tile_of(const int32_t *off, int G, int rows, int bm, int NT_, 
   int half = -1, mt;
   if (b < full) {
     t = xcd_swizzle(b, full);
-  } else if (2 * rest <= kCUs) {
+  } else if (HALVES && 2 * rest <= kCUs) {
     if (b >= full + 2 * rest) return false;
     t = xcd_swizzle(b - full, 2 * rest);
     half = __builtin_amdgcn_readfirstlane((int)(t & 1));
