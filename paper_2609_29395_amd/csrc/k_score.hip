@@ -534,7 +534,11 @@ __global__ void __launch_bounds__(256) score_grad_kernel(ScoreGradArgs a, FastDi
 
 // Chunks of a long row: as much as a workgroup holds in registers (16,384
 // classes), or a quarter (bf16) or eighth (fp32) of it where the rows are too
-// few to give every CU two such chunks.
+// few to give every CU two such chunks.  But a row that one large chunk holds
+// is not cut: 1 row of 6,058 classes of bf16 takes 5.5 us so, and 8.0 as two
+// small chunks and their join.  Nor is one whose small chunks' keys are more
+// than a wave holds for the join: 1 row of 600,000, top 8, 9.7 against 15.0
+// us; below that small chunks are faster, 7.9 against 9.1 us for 17,000.
 struct Chunks {
   bool large;
   int64_t n;  // of a row
@@ -542,17 +546,18 @@ struct Chunks {
 template <typename T> constexpr int kLargeNV = sizeof(T) == 2 ? 8 : 16;
 constexpr int kSmallNV = 2;
 template <typename T> constexpr int kWaveNV = 4;  // rows that a wave holds: 4 vectors a lane
-template <typename T> Chunks chunks_of(int64_t rows, int L) {
+template <typename T> Chunks chunks_of(int64_t rows, int L, int top) {
   constexpr int64_t per = 256 * Bits<T>::VEC;
-  const int64_t n = (L + per * kLargeNV<T> - 1) / (per * kLargeNV<T>);
-  if (rows * n >= 512) return {true, n};
-  return {false, (L + per * kSmallNV - 1) / (per * kSmallNV)};
+  const int64_t large = (L + per * kLargeNV<T> - 1) / (per * kLargeNV<T>);
+  const int64_t small = (L + per * kSmallNV - 1) / (per * kSmallNV);
+  if (rows * large >= 512 || (large == 1 && small > 1) || small * top > 64 * kHeld) return {true, large};
+  return {false, small};
 }
 template <typename T> bool wave_rows(int L) { return L <= 64 * kWaveNV<T> * Bits<T>::VEC; }
 
 template <typename T> size_t work_of(int64_t rows, int L, int top) {
   if (wave_rows<T>(L)) return 0;
-  const int64_t n = chunks_of<T>(rows, L).n;
+  const int64_t n = chunks_of<T>(rows, L, top).n;
   return n > 1 ? (size_t)rows * n * (16 + 8 * (size_t)top) : 0;
 }
 
@@ -561,7 +566,7 @@ template <typename T> hipError_t run(const ScoreArgs &a, hipStream_t s) {
     hipLaunchKernelGGL(score_small_kernel<T>, dim3((uint32_t)((a.rows + 15) / 16)), dim3(256), 0, s, a);
     return hipGetLastError();
   }
-  const Chunks ch = chunks_of<T>(a.rows, a.L);
+  const Chunks ch = chunks_of<T>(a.rows, a.L, a.top);
   const int64_t jobs = wave_rows<T>(a.L) ? a.rows : a.rows * ch.n;
   if (jobs > INT32_MAX) return hipErrorInvalidConfiguration;
   const uint32_t n = (uint32_t)jobs;
