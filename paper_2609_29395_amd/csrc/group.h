@@ -14,7 +14,7 @@ constexpr int64_t kMaxTileLd = 1 << 22;
 bool group_tile_ok(int dtype, const GroupArgs &a, int mode);
 hipError_t launch_group_tile(int mode, const GroupArgs &a, hipStream_t s);
 bool group_few_ok(int dtype, const GroupArgs &a, int mode);
-hipError_t launch_group_few(int dtype, const GroupArgs &a, hipStream_t s);
+hipError_t launch_group_few(int dtype, int mode, const GroupArgs &a, hipStream_t s);
 bool group_mid_ok(int dtype, const GroupArgs &a, int mode);
 hipError_t launch_group_mid(int mode, const GroupArgs &a, hipStream_t s);
 bool group_f32_ok(const GroupArgs &a, int mode);

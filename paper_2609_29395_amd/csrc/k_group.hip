@@ -213,7 +213,7 @@ GroupPieces group_pieces(int dtype, int G, int64_t rows, int n, int k) {
 
 hipError_t launch_group(int dtype, int mode, const GroupArgs &a, hipStream_t s) {
   hipError_t e;
-  if (group_few_ok(dtype, a, mode)) e = launch_group_few(dtype, a, s);
+  if (group_few_ok(dtype, a, mode)) e = launch_group_few(dtype, mode, a, s);
   else if (group_tile_ok(dtype, a, mode) && fills_half(a, mode)) e = launch_group_tile(mode, a, s);
   else if (group_mid_ok(dtype, a, mode)) e = launch_group_mid(mode, a, s);
   else if (dtype == GCPSL_F32 && a.N >= 64 && group_f32_ok(a, mode)) e = launch_group_f32(mode, a, s);
