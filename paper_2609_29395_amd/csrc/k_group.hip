@@ -7,6 +7,9 @@
 // and a workgroup finds its group and rows by a scan of the offsets.
 #include "group.h"
 
+#include <cmath>
+#include <type_traits>
+
 namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
@@ -120,10 +123,58 @@ __global__ void __launch_bounds__(256) group_any_kernel(GroupArgs a, int NT) {
     store_bias_grad(a, g, slot, row0 + tid, rowsum);
 }
 
-// Weight gradient in pieces: the pieces' sums, in order.  `blocks` workgroups
-// for each group, whose weights and biases they share; those of a group of one
-// piece end at once.
+// out[0 .. per) = the sum of n partials of `per` entries each.  SPLIT: each wave
+// takes a quarter of the partials, eight loads in flight (1 group of 8,192
+// rows, 64 -> 64, in 27 pieces: 33 -> 18 us with the products); else a thread
+// takes all of them (pieces of large results: 57 against 68 us for 1 group of
+// 3,448 rows, 1024 -> 4096, in 2).
+template <bool SPLIT>
+__device__ __forceinline__ void join(const float *p, int64_t per, uint32_t n, float *out, uint32_t block,
+                                     uint32_t blocks, f32x4_t (&quarter)[3][64]) {
+  constexpr int ENTRIES = SPLIT ? 256 : 1024, AHEAD = SPLIT ? 8 : 4;
+  const uint32_t wave = threadIdx.x >> 6, at = SPLIT ? threadIdx.x & 63 : threadIdx.x;
+  const uint32_t k0 = SPLIT ? n * wave / 4 : 0, k1 = SPLIT ? n * (wave + 1) / 4 : n;
+  for (int64_t base = (int64_t)block * ENTRIES; base < per; base += (int64_t)blocks * ENTRIES) {
+    const int64_t i = base + at * 4;
+    f32x4_t s = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    if (i + 4 <= per) {
+      uint32_t k = k0;
+      for (; k + AHEAD <= k1; k += AHEAD) {
+        f32x4_any v[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) v[u] = *(const f32x4_any *)(p + (int64_t)(k + u) * per + i);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) s += v[u];
+      }
+#pragma unroll 2
+      for (; k < k1; ++k) s += *(const f32x4_any *)(p + (int64_t)k * per + i);
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (i + r < per)
+          for (uint32_t k = k0; k < k1; ++k) s[r] += p[(int64_t)k * per + i + r];
+    }
+    if (SPLIT) {
+      if (wave) quarter[wave - 1][at] = s;
+      __syncthreads();
+      s = (s + quarter[0][at]) + (quarter[1][at] + quarter[2][at]);
+      __syncthreads();
+    }
+    if (SPLIT && wave) continue;
+    if (i + 4 <= per) *(f32x4_any *)(out + i) = s;
+    else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (i + r < per) out[i + r] = s[r];
+    }
+  }
+}
+
+// Weight gradient in pieces: the pieces' sums, in an order of their own.
+// `blocks` workgroups for each group, whose weights and biases they share;
+// those of a group of one piece end at once.
 __global__ void __launch_bounds__(256) group_join_kernel(GroupArgs a, uint32_t blocks) {
+  __shared__ f32x4_t quarter[3][64];
   const int g = (int)(blockIdx.x / blocks);
   uint32_t before = 0, slots = 0, n = 0, first = 0;
   for (int base = 0; base <= g; base += 64) {
@@ -136,29 +187,18 @@ __global__ void __launch_bounds__(256) group_join_kernel(GroupArgs a, uint32_t b
     }
     slots += __shfl(sum, 63, 64);
   }
+  n = __builtin_amdgcn_readfirstlane(n);
+  first = __builtin_amdgcn_readfirstlane(first);
   if (n == 0 || first + n > (uint32_t)a.slots) return;
-  const int64_t per = (int64_t)a.M * a.N, step = (int64_t)blocks * 1024;
-  const float *p = a.part + first * per;
-  float *out = (float *)a.out + g * a.out_gs;
-  for (int64_t i = ((blockIdx.x - g * blocks) * 256 + threadIdx.x) * 4ll; i < per; i += step) {
-    if (i + 4 <= per) {
-      f32x4_any s = *(const f32x4_any *)(p + i);
-      for (uint32_t k = 1; k < n; ++k) s += *(const f32x4_any *)(p + k * per + i);
-      *(f32x4_any *)(out + i) = s;
-    } else {
-      for (int64_t j = i; j < per; ++j) {
-        float s = p[j];
-        for (uint32_t k = 1; k < n; ++k) s += p[k * per + j];
-        out[j] = s;
-      }
-    }
-  }
-  if (!a.db) return;
-  for (int m = (int)((blockIdx.x - g * blocks) * 256 + threadIdx.x); m < a.M; m += (int)(blocks * 256)) {
-    float s = a.part_db[(int64_t)first * a.M + m];
-    for (uint32_t k = 1; k < n; ++k) s += a.part_db[(int64_t)(first + k) * a.M + m];
-    a.db[g * a.db_gs + m] = s;
-  }
+  const int64_t per = (int64_t)a.M * a.N;
+  const uint32_t block = blockIdx.x - g * blocks;
+  const auto both = [&](auto SPLIT) {
+    join<decltype(SPLIT)::value>(a.part + first * per, per, n, (float *)a.out + g * a.out_gs, block, blocks, quarter);
+    if (a.db)
+      join<decltype(SPLIT)::value>(a.part_db + (int64_t)first * a.M, a.M, n, a.db + g * a.db_gs, block, blocks, quarter);
+  };
+  if (n > 8) both(std::true_type());
+  else both(std::false_type());
 }
 
 template <typename T>
@@ -198,15 +238,23 @@ bool fills_half(const GroupArgs &a, int mode) {
 // A piece takes the rows that a workgroup has if they are shared evenly over
 // one round of workgroups on the chip, but enough of them that its products
 // take longer than its partial, written and read again: 1,024 for tiles of
-// 256 x 256 (15 us against 10), 512 for the others.  The tile is the one that
-// the operands most likely take.
+// 256 x 256 (15 us against 10).  For the others a piece of p rows costs about
+// p a in products and, over all of the rows, rows tiles b / p in partials, the
+// sum of which is least at p = sqrt(rows tiles b / a); 128 at least (two steps
+// of the bf16 kernel; 64 are no faster) and 512 at most.  us with this and with
+// 512 throughout: 1 group of 8,192 rows, 64 -> 64, fp32 18 and 35, bf16 14 and
+// 16; 1 of 1,024, 1024 -> 1024, fp32 31 and 43.  The tile is the one that the
+// operands most likely take.
 GroupPieces group_pieces(int dtype, int G, int64_t rows, int n, int k) {
   const bool big = dtype == GCPSL_BF16 && n % 8 == 0 && k % 8 == 0 &&
                    tiles_fill_half((int64_t)((n + 255) / 256) * G, k);
   const int64_t tile = big ? 256 : 128, slots = big ? kCUs : 2 * kCUs;
   const int64_t tiles = ((n + tile - 1) / tile) * ((k + tile - 1) / tile);
   const int64_t even = tiles >= slots ? rows : rows * tiles / slots;
-  const int64_t piece = std::min<int64_t>(std::max<int64_t>(even, big ? 1024 : 512), 1 << 30);
+  const double b_by_a = dtype == GCPSL_BF16 ? 4 : 1;
+  const int64_t least =
+      big ? 1024 : std::min<int64_t>(512, std::max<int64_t>(128, (int64_t)std::sqrt(b_by_a * (double)rows * (double)tiles)));
+  const int64_t piece = std::min<int64_t>(std::max<int64_t>(even, least), 1 << 30);
   // a group of p > 1 pieces has more than (p - 1/2) piece >= 3/4 p piece rows
   return {(int)piece, rows * 2 >= piece * 3 ? (int)(rows * 4 / (piece * 3)) : 0};
 }
@@ -219,8 +267,8 @@ hipError_t launch_group(int dtype, int mode, const GroupArgs &a, hipStream_t s) 
   else if (dtype == GCPSL_F32 && a.N >= 64 && group_f32_ok(a, mode)) e = launch_group_f32(mode, a, s);
   else e = dtype == GCPSL_BF16 ? launch_any<bf16_t>(mode, a, s) : launch_any<float>(mode, a, s);
   if (e == hipSuccess && mode == GROUP_DW && a.slots > 0) {
-    // about eight workgroups a CU in all, of 1,024 entries or more
-    const int64_t most = ((int64_t)a.M * a.N + 1023) / 1024, share = std::max(1, 2048 / a.G);
+    // about eight workgroups a CU in all, of 256 entries or more
+    const int64_t most = ((int64_t)a.M * a.N + 255) / 256, share = std::max(1, 2048 / a.G);
     const uint32_t n = (uint32_t)std::min(most, share);
     hipLaunchKernelGGL(group_join_kernel, dim3(n * (uint32_t)a.G), dim3(256), 0, s, a, n);
     e = hipGetLastError();
