@@ -19,6 +19,11 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 // 64 x 64 outputs, four waves of 32 x 32.  A k tile is staged through
 // registers element by element, so any stride and size will do, into LDS rows
 // of consecutive q; both operands' fragments are 16-byte LDS reads.
+//
+// What is left to it: fp32 results of fewer than 64 columns, operands of fewer
+// elements than a vector, row strides past 2^22.  Bound by the element loads:
+// 65,536 rows of 8 groups, 128 -> 10, fp32, 20 us, 1.8 TB/s (7 us at a copy's
+// rate); the kernels of 128 columns would waste most of their products on it.
 template <typename T> struct Any;
 template <> struct Any<bf16_t> {
   static constexpr int BQ = 64, LD = 72;  // q a tile; elements per LDS row (padded against bank conflicts)

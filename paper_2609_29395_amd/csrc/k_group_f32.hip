@@ -25,6 +25,11 @@
 // rows x 2 columns a thread, so that the 8 k of a column meet in one thread.
 // Two 24 KB buffers; two workgroups share a CU and one's splitting overlaps the
 // other's MFMAs.
+//
+// Bound: the matrix cores (six bf16 products, 415 TFLOP/s at most).  8 groups of
+// 1,024 rows, 1024 -> 1024: forward 96 to 100 us (171 to 179 TFLOP/s; fp32 MFMAs
+// have a peak of 157), input gradient 97, weight gradient 105.  A workgroup
+// alone on its CU takes 0.6 us a k tile where its MFMAs take 0.35.
 #include "group.h"
 
 namespace {

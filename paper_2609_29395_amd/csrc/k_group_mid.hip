@@ -13,6 +13,14 @@
 // A piece that passes the end of the rows (the last k tile) or of the columns
 // is the row's last 8 elements shifted into place, so that nothing outside the
 // operand is read and what lies behind k is zero.
+//
+// Bound: the loads' time, which one k tile's MFMAs (0.25 us) do not cover: a
+// workgroup alone on its CU takes 0.7 us a k tile, two share one better.  8
+// groups of 512 rows, 1024 -> 1024: forward 22 us (383 TFLOP/s), input gradient
+// 20 (442); 17,450 rows of 2 groups, 551 -> 1293 (rows at
+// odd addresses): 67, 62 and 87 us (369, 399, 287 TFLOP/s).  A second set of
+// registers, for loads two k tiles ahead, brought 45 to 36 us for 512 rows, 4096
+// -> 4096, but spilled at the ends of odd sums: 67 to 82 for the latter.
 #include "group.h"
 
 namespace {

@@ -15,6 +15,11 @@
 // to a list in LDS and every one counts how many are above it.  Where the list
 // overflows (many equal values) or the chunk holds a NaN or infinity, the top
 // classes are taken one at a time by a maximum over the chunk.
+//
+// Bound: reading the logits.  4,096 rows of 131,072 classes, bf16, top 8: 203 to
+// 208 us (5.2 TB/s; reads alone reach 6.2).  One row of as many, top 20: 6 + 4.4
+// us in two kernels, launches and latency.  The gradient reads and writes once:
+// 4,096 x 50,021, fp32, 298 us (5.5 TB/s).
 #include "runtime.h"
 #include "ops.h"
 
