@@ -220,7 +220,7 @@ def _begin(t, stream):
 
 
 def _empty(like, shape, dtype, stream):
-    t = like.new_empty(shape, dtype=dtype)
+    t = like.new_empty(*shape, dtype=dtype)
     if stream is not None:
         t.record_stream(stream)
     return t
@@ -238,6 +238,14 @@ def _rows(t, what, dtype, device, rows=None, cols=None):
     if step != 1 and c > 1:
         raise ValueError(f"{what}: a row's elements must be consecutive")
     return t.data_ptr(), (ld if r > 1 else c)
+
+
+def _out(like, out, rows, cols, dtype, device, stream):
+    """(tensor, address, row stride) of a [rows][cols] result: out, or a new one."""
+    if out is None:
+        out = _empty(like, (rows, cols), dtype, stream)
+        return out, out.data_ptr(), cols
+    return out, *_rows(out, "out", dtype, device, rows, cols)
 
 
 def _vector(t, what, dtype, n, device):
@@ -290,8 +298,7 @@ def group_forward(x, offsets, w, bias=None, relu=False, p=0.0, seed=0, out=None,
     n = w.shape[1] if w.dim() == 3 else -1
     wp, w_gs = _weights(w, "w", dtype, device, (G, n, k))
     bp, b_gs = (None, 0) if bias is None else _weights(bias, "bias", torch.float32, device, (G, n))
-    y = _empty(x, (rows, n), dtype, stream) if out is None else out
-    yp, ldy = _rows(y, "out", dtype, device, rows, n)
+    y, yp, ldy = _out(x, out, rows, n, dtype, device, stream)
     _check(lib().gcpsl_group_forward(code, G, rows, n, k, off, xp, ldx, wp, w_gs, bp, b_gs, 1 if relu else 0, p, seed,
                                      yp, ldy, handle))
     return y
@@ -309,8 +316,7 @@ def group_input_grad(dy, offsets, w, gate=None, p=0.0, out=None, stream=None):
     k = w.shape[2] if w.dim() == 3 else -1
     wp, w_gs = _weights(w, "w", dtype, device, (G, n, k))
     gp, ldg = (None, 0) if gate is None else _rows(gate, "gate", dtype, device, rows, k)
-    dx = _empty(dy, (rows, k), dtype, stream) if out is None else out
-    xp, lddx = _rows(dx, "out", dtype, device, rows, k)
+    dx, xp, lddx = _out(dy, out, rows, k, dtype, device, stream)
     _check(lib().gcpsl_group_input_grad(code, G, rows, n, k, off, dp, lddy, wp, w_gs, gp, ldg, p, xp, lddx, handle))
     return dx
 
@@ -336,10 +342,18 @@ def group_weight_grad(dy, x, offsets, dw=None, db=None, bias=True, workspace=Non
     rows, n = dy.shape
     xp, ldx = _rows(x, "x", dy.dtype, device, rows)
     k = x.shape[1]
-    dw = _empty(dy, (G, n, k), torch.float32, stream) if dw is None else dw
-    wp, w_gs = _weights(dw, "dw", torch.float32, device, (G, n, k))
-    db = _empty(dy, (G, n), torch.float32, stream) if db is None and bias else db
-    bp, b_gs = (None, 0) if db is None else _weights(db, "db", torch.float32, device, (G, n))
+    if dw is None:
+        dw = _empty(dy, (G, n, k), torch.float32, stream)
+        wp, w_gs = dw.data_ptr(), n * k
+    else:
+        wp, w_gs = _weights(dw, "dw", torch.float32, device, (G, n, k))
+    if db is not None:
+        bp, b_gs = _weights(db, "db", torch.float32, device, (G, n))
+    elif bias:
+        db = _empty(dy, (G, n), torch.float32, stream)
+        bp, b_gs = db.data_ptr(), n
+    else:
+        bp, b_gs = None, 0
     ptr, size, keep = _workspace(dy, workspace, _group_workspace_bytes(code, G, rows, n, k), device, stream)
     _check(lib().gcpsl_group_weight_grad(code, G, rows, n, k, off, dp, lddy, xp, ldx, wp, w_gs, bp, b_gs, ptr, size,
                                          handle))
@@ -352,8 +366,7 @@ def dropout(x, p, seed, out=None, stream=None):
     torch, code, handle, device = _begin(x, stream)
     xp, ldx = _rows(x, "x", x.dtype, device)
     rows, cols = x.shape
-    y = _empty(x, (rows, cols), x.dtype, stream) if out is None else out
-    yp, ldy = _rows(y, "out", x.dtype, device, rows, cols)
+    y, yp, ldy = _out(x, out, rows, cols, x.dtype, device, stream)
     _check(lib().gcpsl_dropout(code, rows, cols, xp, ldx, p, seed, yp, ldy, handle))
     return y
 
@@ -385,14 +398,14 @@ def score(logits, labels=None, top=0, workspace=None, stream=None):
     rows, L = logits.shape
     yp = _vector(labels, "labels", torch.int32, rows, device)
     ptr, size, keep = _workspace(logits, workspace, _score_workspace_bytes(code, rows, L, top), device, stream)
-    each = _empty(logits, (3, rows), torch.float32, stream)
-    top_logp = _empty(logits, (rows, top), torch.float32, stream)
-    top_class = _empty(logits, (rows, top), torch.int32, stream)
-    ep = each.data_ptr()
-    _check(lib().gcpsl_score(code, rows, L, zp, ldz, yp, top, None if labels is None else ep, ep + 4 * rows,
-                             ep + 8 * rows, top_logp.data_ptr(), top_class.data_ptr(), ptr, size, handle))
-    logp, entropy, lse = each.unbind(0)
-    return Scores(None if labels is None else logp, entropy, lse, top_logp, top_class)
+    # one allocation for all results: an allocation and a view cost the host about a microsecond each
+    held = _empty(logits, (rows * (3 + 2 * top),), torch.float32, stream)
+    logp, entropy, lse, top_logp, top_class = held.split_with_sizes((rows, rows, rows, rows * top, rows * top))
+    hp = held.data_ptr()
+    _check(lib().gcpsl_score(code, rows, L, zp, ldz, yp, top, None if labels is None else hp, hp + 4 * rows,
+                             hp + 8 * rows, hp + 12 * rows, hp + (12 + 4 * top) * rows, ptr, size, handle))
+    return Scores(None if labels is None else logp, entropy, lse, top_logp.view(rows, top),
+                  top_class.view(torch.int32).view(rows, top))
 
 
 def score_grad(logits, labels, lse, entropy=None, g_logp=None, g_entropy=None, out=None, stream=None):
@@ -404,8 +417,7 @@ def score_grad(logits, labels, lse, entropy=None, g_logp=None, g_entropy=None, o
     rows, L = logits.shape
     yp = _vector(labels, "labels", torch.int32, rows, device)
     f32 = torch.float32
-    dz = _empty(logits, (rows, L), logits.dtype, stream) if out is None else out
-    dp, lddz = _rows(dz, "out", logits.dtype, device, rows, L)
+    dz, dp, lddz = _out(logits, out, rows, L, logits.dtype, device, stream)
     _check(lib().gcpsl_score_grad(code, rows, L, zp, ldz, yp, _vector(lse, "lse", f32, rows, device),
                                   _vector(entropy, "entropy", f32, rows, device),
                                   _vector(g_logp, "g_logp", f32, rows, device),
