@@ -182,7 +182,7 @@ inline int64_t tile_blocks(int64_t rows, int G, int bm, int64_t NT) {
 // Four consecutive columns c .. c + 3 of row m of the result (forward, input
 // gradient): bias, ReLU (a NaN stays one), dropout or gate.
 template <typename T, int MODE>
-GROUP_DEVICE void epilogue(const GroupArgs &a, int g, int m, int c, const float *bias, const float *gate, float (&v)[4]) {
+GROUP_DEVICE void epilogue(const GroupArgs &a, int m, int c, const float *bias, const float *gate, float (&v)[4]) {
   if constexpr (MODE == GROUP_FWD) {
     uint64_t word = 0;
     if (a.drop.thr) word = drop_word(a.drop.key, m, (a.N + 3) >> 2, c >> 2);
@@ -224,7 +224,7 @@ GROUP_DEVICE void finish4(const GroupArgs &a, int g, int m, int c, const V &acc)
       for (int r = 0; r < 4; ++r) gate[r] = b[r];
     }
   }
-  epilogue<T, MODE>(a, g, m, c, bias, gate, v);
+  epilogue<T, MODE>(a, m, c, bias, gate, v);
   T *out = (T *)a.out + (int64_t)m * a.ldo + c;
   if constexpr (sizeof(T) == 2)
     *(u32x2_any *)out = u32x2_any{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])};
@@ -234,33 +234,17 @@ GROUP_DEVICE void finish4(const GroupArgs &a, int g, int m, int c, const V &acc)
 
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 
-// Eight columns in bf16, all inside the result (their number is a multiple of 8).
-template <int MODE> GROUP_DEVICE void finish8(const GroupArgs &a, int g, int m, int c, const float *acc) {
-  float v[2][4], bias[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}, gate[2][4];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = acc[i];
-  if constexpr (MODE == GROUP_FWD) {
-    if (a.bias) {
-      const float *p = a.bias + g * a.bias_gs + c;
-      const f32x4_any x = *(const f32x4_any *)p, y = *(const f32x4_any *)(p + 4);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        bias[0][r] = x[r];
-        bias[1][r] = y[r];
-      }
-    }
-  } else if (a.gate) {
-    const u32x4_any b = *(const u32x4_any *)((const bf16_t *)a.gate + (int64_t)m * a.ldg + c);
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      gate[i >> 2][i & 3] = __uint_as_float(i & 1 ? b[i >> 1] & 0xffff0000u : b[i >> 1] << 16);
+template <typename T> struct Vec16;  // the elements of a 16-byte vector
+template <> struct Vec16<bf16_t> {
+  static constexpr int N = 8;
+  static GROUP_DEVICE float at(const u32x4_any &v, int j) {
+    return __uint_as_float(j & 1 ? v[j >> 1] & 0xffff0000u : v[j >> 1] << 16);
   }
-#pragma unroll
-  for (int i = 0; i < 2; ++i) epilogue<bf16_t, MODE>(a, g, m, c + 4 * i, bias[i], gate[i], v[i]);
-  *(u32x4_any *)((bf16_t *)a.out + (int64_t)m * a.ldo + c) =
-      u32x4_any{pack2_bf16(v[0][0], v[0][1]), pack2_bf16(v[0][2], v[0][3]), pack2_bf16(v[1][0], v[1][1]),
-                pack2_bf16(v[1][2], v[1][3])};
-}
+};
+template <> struct Vec16<float> {
+  static constexpr int N = 4;
+  static GROUP_DEVICE float at(const u32x4_any &v, int j) { return __uint_as_float(v[j]); }
+};
 
 // The same where columns may lie outside.
 template <typename T, int MODE, typename V>
@@ -276,11 +260,103 @@ GROUP_DEVICE void finish(const GroupArgs &a, int g, int m, int c, const V &acc) 
         if (a.gate) gate[r] = ElemT<T>::to_f(((const T *)a.gate)[(int64_t)m * a.ldg + c + r]);
       }
     }
-  epilogue<T, MODE>(a, g, m, c, bias, gate, v);
+  epilogue<T, MODE>(a, m, c, bias, gate, v);
 #pragma unroll
   for (int r = 0; r < 4; ++r)
     if (c + r < a.N) ((T *)a.out)[(int64_t)m * a.ldo + c + r] = ElemT<T>::from_f(v[r]);
 }
+
+// A thread's 16 bytes of columns, c on, of ROWS rows m0, m0 + step, ... below
+// m1: the bias and the gate's rows are loaded together before the sums are
+// there, so that no row waits for its own.
+template <typename T, int MODE, int ROWS> struct FinishRows {
+  static constexpr int VEC = Vec16<T>::N;
+  int m0, step, m1, c;
+  float bias[VEC];
+  u32x4_any gate[ROWS];
+  GROUP_DEVICE FinishRows(const GroupArgs &a, int g, int m0_, int step_, int m1_, int c_)
+      : m0(m0_), step(step_), m1(m1_), c(c_) {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) bias[j] = 0.f;
+    if (c >= a.N) return;
+    const bool whole = c + VEC <= a.N;  // else what is past the columns is taken as the last one
+    if constexpr (MODE == GROUP_FWD) {
+      if (!a.bias) return;
+      const float *p = a.bias + g * a.bias_gs;
+      if (whole) {
+#pragma unroll
+        for (int j = 0; j < VEC; j += 4) {
+          const f32x4_any b = *(const f32x4_any *)(p + c + j);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) bias[j + r] = b[r];
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) bias[j] = p[min(c + j, a.N - 1)];
+      }
+    } else if (a.gate) {
+#pragma unroll
+      for (int i = 0; i < ROWS; ++i) {
+        const T *p = (const T *)a.gate + (int64_t)min(m0 + i * step, m1 - 1) * a.ldg;
+        if (whole) {
+          gate[i] = *(const u32x4_any *)(p + c);
+        } else {
+          const auto bits = [&](int j) -> uint32_t {
+            const T v = p[min(c + j, a.N - 1)];
+            if constexpr (sizeof(T) == 2) return v;
+            else return __float_as_uint(v);
+          };
+#pragma unroll
+          for (int j = 0; j < 4; ++j) gate[i][j] = sizeof(T) == 2 ? bits(2 * j) | bits(2 * j + 1) << 16 : bits(j);
+        }
+      }
+    }
+  }
+  // the sums of row i, columns 4 j on, at acc(i, j)
+  template <typename F> GROUP_DEVICE void store_row(const GroupArgs &a, int i, const u32x4_any &gates, const F &acc) const {
+    const int m = m0 + i * step;
+    if (m >= m1) return;
+    u32x4_any o;
+#pragma unroll
+    for (int j = 0; j < VEC / 4; ++j) {
+      const f32x4_any v = acc(i, j);
+      float x[4], b[4], gt[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        x[r] = v[r];
+        b[r] = bias[4 * j + r];
+        gt[r] = MODE == GROUP_FWD ? 0.f : Vec16<T>::at(gates, 4 * j + r);
+      }
+      epilogue<T, MODE>(a, m, c + 4 * j, b, gt, x);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if constexpr (sizeof(T) == 4) o[r] = __float_as_uint(x[r]);
+        else if (r & 1) o[2 * j + (r >> 1)] = pack2_bf16(x[r - 1], x[r]);
+      }
+    }
+    T *out = (T *)a.out + (int64_t)m * a.ldo + c;
+    if (c + VEC <= a.N) {
+      *(u32x4_any *)out = o;
+    } else {
+#pragma unroll
+      for (int j = 0; j < VEC - 1; ++j)
+        if (c + j < a.N) {
+          if constexpr (sizeof(T) == 2) out[j] = (T)(o[j >> 1] >> (j & 1) * 16);
+          else out[j] = __uint_as_float(o[j]);
+        }
+    }
+  }
+  template <typename F> GROUP_DEVICE void store(const GroupArgs &a, const F &acc) const {
+    if (c >= a.N) return;
+    if constexpr (MODE == GROUP_FWD) {  // (copies of the draws' code for every row cost more in fetching it)
+#pragma unroll 1
+      for (int i = 0; i < ROWS; ++i) store_row(a, i, u32x4_any{}, acc);
+    } else {
+#pragma unroll
+      for (int i = 0; i < ROWS; ++i) store_row(a, i, gate[i], acc);
+    }
+  }
+};
 
 // Four columns of a weight gradient, to its place or (slot >= 0) to a partial.
 template <typename V> GROUP_DEVICE void store_grad(const GroupArgs &a, int g, int slot, int m, int c, const V &acc) {

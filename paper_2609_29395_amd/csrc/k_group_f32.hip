@@ -278,22 +278,36 @@ __device__ __forceinline__ void group_f32_tile(const GroupArgs &a, const Tile &t
     }
   }
 
+  // The results go through LDS, the rows of two waves (32 FJ of 512 bytes) at a
+  // time, so that whole rows of the tile are written at once.
+  const auto place = [&](int r, int c) { return lds + r * 512 + ((c >> 2) ^ ((r & 15) << 1)) * 16; };
 #pragma unroll
-  for (int j = 0; j < FJ; ++j) {
-    const int m = wm * 32 * FJ + j * 32 + li;
-    if (m >= rows) continue;
+  for (int h = 0; h < 2; ++h) {
+    const int m0 = h * 32 * FJ, r0 = tid >> 5, c4 = (tid & 31) * 4;
+    if (m0 >= rows) break;
+    const FinishRows<float, MODE == GROUP_DW ? GROUP_FWD : MODE, 4 * FJ> out(a, g, row0 + m0 + r0, 8, row0 + rows, c0 + c4);
+    __syncthreads();
+    if (wm == h)
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+      for (int j = 0; j < FJ; ++j)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int c = c0 + wn * 64 + i * 32 + 8 * q + 4 * lg;
-        if (c >= a.N) continue;
-        f32x4_t v;
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = big[i][j][4 * q + r] + small[i][j][4 * q + r];
-        if constexpr (MODE == GROUP_DW) store_grad(a, g, slot, row0 + m, c, v);
-        else finish<float, MODE>(a, g, row0 + m, c, v);
-      }
+          for (int q = 0; q < 4; ++q) {
+            f32x4_t v;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = big[i][j][4 * q + r] + small[i][j][4 * q + r];
+            *(f32x4_t *)place(j * 32 + li, wn * 64 + i * 32 + 8 * q + 4 * lg) = v;
+          }
+    __syncthreads();
+    const auto sum = [&](int i, int) { return *(const f32x4_t *)place(r0 + 8 * i, c4); };
+    if constexpr (MODE == GROUP_DW) {
+      if (c0 + c4 < a.N)
+        for (int i = 0; i < 4 * FJ && m0 + r0 + 8 * i < rows; ++i)
+          store_grad(a, g, slot, row0 + m0 + r0 + 8 * i, c0 + c4, sum(i, 0));
+    } else {
+      out.store(a, sum);
+    }
   }
   if constexpr (MODE == GROUP_DW) {
     if (sums) {  // each column's two shares, of 8 of every 16 rows

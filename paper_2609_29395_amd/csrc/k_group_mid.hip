@@ -206,20 +206,29 @@ __device__ __forceinline__ void group_mid_tile(const GroupArgs &a, const Tile &t
   for (; k0 + 3 * BK <= Q; k0 += BK, p ^= 1) tile(k0, p, std::true_type{});
   for (; k0 < Q; k0 += BK, p ^= 1) tile(k0, p, std::false_type{});
 
+  // The results go through LDS, 32 FM rows of 512 bytes, so that whole rows of
+  // the tile are written at once.
+  const auto place = [&](int r, int c) { return lds + r * 512 + ((c >> 2) ^ ((r & 7) << 2)) * 16; };
+  const int r0 = tid >> 4, c8 = (tid & 15) * 8;  // forward, input gradient: this thread's first row and its columns
+  const FinishRows<bf16_t, MODE == GROUP_DW ? GROUP_FWD : MODE, 2 * FM> out(a, t.g, t.row0 + r0, 16, t.row0 + t.rows,
+                                                                            t.c0 + c8);
 #pragma unroll
-  for (int i = 0; i < FM; ++i) {
-    const int m = (wm * FM + i) * 16 + li;
-    if (m >= t.rows) continue;
+  for (int i = 0; i < FM; ++i)
 #pragma unroll
-    for (int j = 0; j < FN; ++j) {
-      const int c = t.c0 + (wn * FN + j) * 16 + 4 * lg;
-      if (c >= a.N) continue;
-      if constexpr (MODE == GROUP_DW) store_grad(a, t.g, t.slot, t.row0 + m, c, acc[i][j]);
-      else finish<bf16_t, MODE>(a, t.g, t.row0 + m, c, acc[i][j]);
+    for (int j = 0; j < FN; ++j) *(f32x4_t *)place((wm * FM + i) * 16 + li, (wn * FN + j) * 16 + 4 * lg) = acc[i][j];
+  __syncthreads();
+  if constexpr (MODE == GROUP_DW) {
+    const int c = t.c0 + (tid & 31) * 4;
+    if (c < a.N)
+      for (int r = tid >> 5; r < t.rows; r += 8)
+        store_grad(a, t.g, t.slot, t.row0 + r, c, *(const f32x4_t *)place(r, (tid & 31) * 4));
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      const int m = (wm * FM + i) * 16 + li;
+      if (t.sums && lg == 0 && (i & 1) == wn && m < t.rows) store_bias_grad(a, t.g, t.slot, t.row0 + m, bacc[i >> 1][0]);
     }
-    if constexpr (MODE == GROUP_DW) {
-      if (t.sums && lg == 0 && (i & 1) == wn) store_bias_grad(a, t.g, t.slot, t.row0 + m, bacc[i >> 1][0]);
-    }
+  } else {
+    out.store(a, [&](int i, int j) { return *(const f32x4_t *)place(r0 + 16 * i, c8 + 4 * j); });
   }
 }
 

@@ -419,6 +419,10 @@ __global__ void __launch_bounds__(512, 2) group_tile_kernel(GroupArgs a, int NT)
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     if (h * HALF >= rows) break;
+    const int high = min(HALF, rows - h * HALF), m0 = row0 + h * HALF;
+    // forward, input gradient: two rows a wave, eight columns a lane
+    const int r0 = wave * 2 + (lane >> 5), c = (lane & 31) * 8;
+    const FinishRows<bf16_t, MODE == GROUP_DW ? GROUP_FWD : MODE, HALF / 16> out(a, g, m0 + r0, 16, m0 + high, c0 + c);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < FM; ++i)
@@ -429,17 +433,13 @@ __global__ void __launch_bounds__(512, 2) group_tile_kernel(GroupArgs a, int NT)
           *(f32x4_t *)(smem + ((wm * FM + i) * 16 + li) * OUT_ROW + (k * HALF + (wn * FN + j) * 16 + 4 * lg) * 4) =
               acc[h][i][k][j];
     __syncthreads();
-    const int high = min(HALF, rows - h * HALF);
     if constexpr (MODE == GROUP_DW) {  // a row a wave
-      const int c = c0 + lane * 4;
-      if (c < a.N)
+      const int c4 = c0 + lane * 4;
+      if (c4 < a.N)
         for (int r = wave; r < high; r += 8)
-          store_grad(a, g, slot, row0 + h * HALF + r, c, *(const f32x4_t *)(smem + r * OUT_ROW + lane * 16));
-    } else {  // two rows a wave, eight columns a lane
-      const int c = (lane & 31) * 8;
-      if (c0 + c < a.N)
-        for (int r = wave * 2 + (lane >> 5); r < high; r += 16)
-          finish8<MODE>(a, g, row0 + h * HALF + r, c0 + c, (const float *)(smem + r * OUT_ROW) + c);
+          store_grad(a, g, slot, m0 + r, c4, *(const f32x4_t *)(smem + r * OUT_ROW + lane * 16));
+    } else {
+      out.store(a, [&](int i, int j) { return *(const f32x4_t *)(smem + (r0 + 16 * i) * OUT_ROW + (c + 4 * j) * 4); });
     }
   }
   if (sums && lg == 0) {
