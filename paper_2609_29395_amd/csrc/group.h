@@ -42,14 +42,27 @@ struct LaneTiles {
   int begin, end;
   uint32_t first, tiles;
 };
-GROUP_DEVICE uint32_t lane_scan(uint32_t v) {  // inclusive sum over the lanes
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t u = __shfl_up(v, d, 64);
-    if ((threadIdx.x & 63) >= d) v += u;
-  }
+// v moved across lanes by DPP control CTRL, 0 where nothing arrives or the row of 16 is not in ROWS.
+template <int CTRL, int ROWS> GROUP_DEVICE uint32_t dpp(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
+// Inclusive sum over the 64 lanes, all of them active: within rows of 16 by shifts of 1, 2, 4 and 8, then the row
+// before (into rows 1 and 3) and the two before (rows 2 and 3) from their last lane.  (Shuffles go through the LDS: a
+// launch took 0.3 to 0.5 us longer with them.)
+GROUP_DEVICE uint32_t lane_scan(uint32_t v) {
+  v += dpp<0x111, 0xf>(v);
+  v += dpp<0x112, 0xf>(v);
+  v += dpp<0x114, 0xf>(v);
+  v += dpp<0x118, 0xf>(v);
+  v += dpp<0x142, 0xa>(v);
+  v += dpp<0x143, 0xc>(v);
   return v;
 }
+// Lane i's v, i the same in every lane.
+GROUP_DEVICE int of_lane(int v, int i) {
+  return __builtin_amdgcn_readlane(v, __builtin_amdgcn_readfirstlane(i));
+}
+
 template <bool PIECES = false>
 GROUP_DEVICE uint32_t lane_tiles(const int32_t *off, int G, int rows, int bm, int base, uint32_t before, LaneTiles &l) {
   const int i = base + (int)(threadIdx.x & 63);
@@ -61,7 +74,7 @@ GROUP_DEVICE uint32_t lane_tiles(const int32_t *off, int G, int rows, int bm, in
   }
   const uint32_t sum = lane_scan(l.tiles);
   l.first = before + sum - l.tiles;
-  return before + __shfl(sum, 63, 64);
+  return before + (uint32_t)of_lane((int)sum, 63);
 }
 
 // Tile t of MT x NT in blocks of 8 row tiles by all column tiles, rows
@@ -107,20 +120,20 @@ GROUP_DEVICE bool piece_of(const GroupArgs &a, uint32_t tiles, uint32_t b, int &
   while (i < 0) {
     base += 64;
     if (base >= a.G) return false;
-    slots += __shfl(sum, 63, 64);
+    slots += (uint32_t)of_lane((int)sum, 63);
     before = lane_tiles<true>(a.off, a.G, a.Q, a.piece, base, before, l);
     own = l.tiles > 1 ? l.tiles : 0;
     sum = lane_scan(own);
     i = lane_of(l, t);
   }
-  const int begin = __shfl(l.begin, i, 64), end = __shfl(l.end, i, 64);
-  const int n = (int)__shfl(l.tiles, i, 64), k = (int)(t - __shfl(l.first, i, 64));
+  const int begin = of_lane(l.begin, i), end = of_lane(l.end, i);
+  const int n = of_lane((int)l.tiles, i), k = (int)(t - (uint32_t)of_lane((int)l.first, i));
   const int part = ((end - begin + n - 1) / n + 63) / 64 * 64;
   const int64_t at = begin + (int64_t)k * part;  // may pass the group's end, and 31 bits
   g = __builtin_amdgcn_readfirstlane(base + i);
   q0 = __builtin_amdgcn_readfirstlane((int)min(at, (int64_t)end));
   q1 = __builtin_amdgcn_readfirstlane((int)min(at + part, (int64_t)end));
-  slot = __builtin_amdgcn_readfirstlane(n > 1 ? (int)(slots + __shfl(sum - own, i, 64)) + k : -1);
+  slot = __builtin_amdgcn_readfirstlane(n > 1 ? (int)(slots + (uint32_t)of_lane((int)(sum - own), i)) + k : -1);
   return slot < a.slots;
 }
 
@@ -167,8 +180,8 @@ GROUP_DEVICE bool tile_of(const int32_t *off, int G, int rows, int bm, int NT_, 
     i = lane_of(l, (uint32_t)mt);
   }
   g = __builtin_amdgcn_readfirstlane(base + i);
-  row0 = __builtin_amdgcn_readfirstlane(__shfl(l.begin, i, 64) + (mt - (int)__shfl(l.first, i, 64)) * bm);
-  row1 = __builtin_amdgcn_readfirstlane(min(__shfl(l.end, i, 64), row0 + bm));
+  row0 = __builtin_amdgcn_readfirstlane(of_lane(l.begin, i) + (mt - of_lane((int)l.first, i)) * bm);
+  row1 = __builtin_amdgcn_readfirstlane(min(of_lane(l.end, i), row0 + bm));
   if (half == 0) row1 = min(row1, row0 + bm / 2);
   if (half == 1) row0 += bm / 2;
   return row0 < row1;
@@ -266,10 +279,10 @@ GROUP_DEVICE void finish(const GroupArgs &a, int g, int m, int c, const V &acc) 
     if (c + r < a.N) ((T *)a.out)[(int64_t)m * a.ldo + c + r] = ElemT<T>::from_f(v[r]);
 }
 
-// A thread's 16 bytes of columns, c on, of ROWS rows m0, m0 + step, ... below
+// A thread's 16 bytes of columns, c on (EDGES false: all inside or all outside), of ROWS rows m0, m0 + step, ... below
 // m1: the bias and the gate's rows are loaded together before the sums are
 // there, so that no row waits for its own.
-template <typename T, int MODE, int ROWS> struct FinishRows {
+template <typename T, int MODE, int ROWS, bool EDGES = true> struct FinishRows {
   static constexpr int VEC = Vec16<T>::N;
   int m0, step, m1, c;
   float bias[VEC];
@@ -279,7 +292,7 @@ template <typename T, int MODE, int ROWS> struct FinishRows {
 #pragma unroll
     for (int j = 0; j < VEC; ++j) bias[j] = 0.f;
     if (c >= a.N) return;
-    const bool whole = c + VEC <= a.N;  // else what is past the columns is taken as the last one
+    const bool whole = !EDGES || c + VEC <= a.N;  // else what is past the columns is taken as the last one
     if constexpr (MODE == GROUP_FWD) {
       if (!a.bias) return;
       const float *p = a.bias + g * a.bias_gs;
@@ -335,7 +348,7 @@ template <typename T, int MODE, int ROWS> struct FinishRows {
       }
     }
     T *out = (T *)a.out + (int64_t)m * a.ldo + c;
-    if (c + VEC <= a.N) {
+    if (!EDGES || c + VEC <= a.N) {
       *(u32x4_any *)out = o;
     } else {
 #pragma unroll

@@ -187,10 +187,10 @@ __global__ void __launch_bounds__(256) group_join_kernel(GroupArgs a, uint32_t b
     before = lane_tiles<true>(a.off, a.G, a.Q, a.piece, base, before, l);
     const uint32_t own = l.tiles > 1 ? l.tiles : 0, sum = lane_scan(own);
     if (g < base + 64) {
-      n = __shfl(own, g - base, 64);
-      first = slots + __shfl(sum - own, g - base, 64);
+      n = (uint32_t)of_lane((int)own, g - base);
+      first = slots + (uint32_t)of_lane((int)(sum - own), g - base);
     }
-    slots += __shfl(sum, 63, 64);
+    slots += (uint32_t)of_lane((int)sum, 63);
   }
   n = __builtin_amdgcn_readfirstlane(n);
   first = __builtin_amdgcn_readfirstlane(first);

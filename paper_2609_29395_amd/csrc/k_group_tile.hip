@@ -422,7 +422,8 @@ __global__ void __launch_bounds__(512, 2) group_tile_kernel(GroupArgs a, int NT)
     const int high = min(HALF, rows - h * HALF), m0 = row0 + h * HALF;
     // forward, input gradient: two rows a wave, eight columns a lane
     const int r0 = wave * 2 + (lane >> 5), c = (lane & 31) * 8;
-    const FinishRows<bf16_t, MODE == GROUP_DW ? GROUP_FWD : MODE, HALF / 16> out(a, g, m0 + r0, 16, m0 + high, c0 + c);
+    const FinishRows<bf16_t, MODE == GROUP_DW ? GROUP_FWD : MODE, HALF / 16, false> out(a, g, m0 + r0, 16, m0 + high,
+                                                                                        c0 + c);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < FM; ++i)
