@@ -80,10 +80,11 @@ GROUP_DEVICE uint32_t lane_tiles(const int32_t *off, int G, int rows, int bm, in
 // Tile t of MT x NT in blocks of 8 row tiles by all column tiles, rows
 // fastest: 32 tiles in order are about 8 x 4 and share their operands.
 GROUP_DEVICE void block_order(uint32_t t, uint32_t MT, uint32_t NT, int &mt, int &nt) {
-  const uint32_t block = t / (8u * NT), in = t - block * 8u * NT;
+  const uint32_t block = t < 8u * NT ? 0u : t / (8u * NT), in = t - block * 8u * NT;
   const uint32_t high = min(8u, MT - block * 8u);  // row tiles of this block
-  nt = __builtin_amdgcn_readfirstlane((int)(in / high));
-  mt = __builtin_amdgcn_readfirstlane((int)(block * 8u + in % high));
+  const uint32_t n = high == 8u ? in >> 3 : in / high;
+  nt = __builtin_amdgcn_readfirstlane((int)n);
+  mt = __builtin_amdgcn_readfirstlane((int)(block * 8u + in - n * high));
 }
 
 // Lane whose group has part t, -1 if none.  (A part is checked against its
