@@ -1,6 +1,6 @@
 // Products over rows grouped by cluster, bf16, on gfx950: 128 x 128 outputs a
-// workgroup, any alignment and size from 8 on, and the launches too small for
-// tiles of 256 x 256.
+// workgroup (64 x 128 in small launches), any alignment and size from 8 on, and
+// the launches too small for tiles of 256 x 256.
 //
 // A k tile is 64 deep and goes through registers, loaded as 16-byte pieces at
 // any alignment, to LDS as it lies in memory: an operand whose rows run along
@@ -8,7 +8,7 @@
 // 256 bytes, from which ds_read_b64_tr_b16 makes fragments.  16-byte pieces are
 // XOR-swizzled within a row so that a fragment read uses every bank.  Two
 // buffers, one barrier a tile: tile t is multiplied while t + 1 is written to
-// the other buffer and t + 2 loaded to registers.
+// the other buffer and t + 2 (64 rows: and t + 3) loaded to registers.
 //
 // A piece that passes the end of the rows (the last k tile) or of the columns
 // is the row's last 8 elements shifted into place, so that nothing outside the
@@ -17,10 +17,9 @@
 // Bound: the loads' time, which one k tile's MFMAs (0.25 us) do not cover: a
 // workgroup alone on its CU takes 0.7 us a k tile, two share one better.  8
 // groups of 512 rows, 1024 -> 1024: forward 22 us (383 TFLOP/s), input gradient
-// 20 (442); 17,450 rows of 2 groups, 551 -> 1293 (rows at
-// odd addresses): 67, 62 and 87 us (369, 399, 287 TFLOP/s).  A second set of
-// registers, for loads two k tiles ahead, brought 45 to 36 us for 512 rows, 4096
-// -> 4096, but spilled at the ends of odd sums: 67 to 82 for the latter.
+// 20 (442); 17,450 rows of 2 groups, 551 -> 1293 (rows at odd addresses): 67, 62
+// and 87 us (369, 399, 287 TFLOP/s).  Tiles of 64 rows leave registers for loads
+// two k tiles ahead (with 128 rows they spilled at the ends of odd sums).
 #include "group.h"
 
 namespace {
@@ -31,7 +30,7 @@ typedef short i16x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
 
-constexpr int BM = 128, BN = 128, BK = 64;
+constexpr int BN = 128, BK = 64;
 constexpr int OPERAND = 128 * BK * 2, BUFFER = 2 * OPERAND;  // bytes of an operand's tile, of both
 
 __device__ __forceinline__ int swz_row(int row) { return (row >> 1) & 7; }
@@ -52,13 +51,14 @@ __device__ __forceinline__ u32x4 shift_down(const u32x4 &w, int n) {
 // rows run across the sum: k = tid / 16 + 16 j, columns 8 (tid % 16) .. + 7;
 // else along it: rows tid / 8 + 32 j, k = 8 (tid % 8) .. + 7.  Rows past the n
 // inside are taken as the last one inside (what they give is not stored).
-template <bool T, int PIECES = 4> struct Stage {
+// SETS: tiles whose loads may be in flight.
+template <bool T, int PIECES, int SETS> struct Stage {
   const char *base;  // of the next tile
   int64_t step;
   uint32_t off[PIECES];
   int at, shift;     // byte in LDS, elements to shift the pieces down (T, at the columns' end)
   bool edge;         // some thread shifts
-  u32x4 v[PIECES];
+  u32x4 v[SETS][PIECES];
   static constexpr int NEXT = T ? 16 * 256 : 32 * 128;  // bytes from piece to piece in LDS
 
   __device__ __forceinline__ void init(const void *p, int64_t ld, int n, int tid) {
@@ -82,34 +82,34 @@ template <bool T, int PIECES = 4> struct Stage {
         off[j] = (uint32_t)min(row + 32 * j, n - 1) * (uint32_t)ld * 2u + (uint32_t)chunk * 16u;
     }
   }
-  __device__ __forceinline__ void load_all() {
+  __device__ __forceinline__ void load_all(int set) {
 #pragma unroll
-    for (int j = 0; j < PIECES; ++j) v[j] = *(const u32x4_any *)(base + off[j]);
+    for (int j = 0; j < PIECES; ++j) v[set][j] = *(const u32x4_any *)(base + off[j]);
     base += step;
   }
   // the next tile, of which `left` values of k are inside; its pieces are whole
   // (T false: and shifted) when this returns
-  __device__ __forceinline__ void load(int left, int tid) {
-    if (left >= BK) return load_all();
+  __device__ __forceinline__ void load(int left, int tid, int set) {
+    if (left >= BK) return load_all(set);
     if (left <= 0) return;
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) {
       if constexpr (T) {
         const int k = (tid >> 4) + 16 * j, in = min(k, left - 1);
-        v[j] = *(const u32x4_any *)(base + (off[j] - (uint32_t)(k - in) * (uint32_t)(step >> 6)));
-        if (k >= left) v[j] = u32x4{0, 0, 0, 0};
+        v[set][j] = *(const u32x4_any *)(base + (off[j] - (uint32_t)(k - in) * (uint32_t)(step >> 6)));
+        if (k >= left) v[set][j] = u32x4{0, 0, 0, 0};
       } else {
         const int over = min(max((tid & 7) * 8 + 8 - left, 0), 64);  // elements past the row's end
         const u32x4 w = *(const u32x4_any *)(base + (int64_t)off[j] - over * 2);
-        v[j] = shift_down(w, min(over, 8));
+        v[set][j] = shift_down(w, min(over, 8));
       }
     }
   }
-  __device__ __forceinline__ void write(char *lds) {
+  __device__ __forceinline__ void write(char *lds, int set) {
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) {
-      if (T && edge) v[j] = shift_down(v[j], shift);
-      *(u32x4 *)(lds + at + j * NEXT) = v[j];
+      if (T && edge) v[set][j] = shift_down(v[set][j], shift);
+      *(u32x4 *)(lds + at + j * NEXT) = v[set][j];
     }
   }
 };
@@ -137,15 +137,15 @@ struct Tile {
 };
 
 // The tile's sums and results; waves of 16 FM x 64 outputs.
-template <int MODE, int FM>
+template <int MODE, int FM, int SETS>
 __device__ __forceinline__ void group_mid_tile(const GroupArgs &a, const Tile &t, char *lds) {
   constexpr bool AT = MODE == GROUP_DW, BT = MODE != GROUP_FWD;
   constexpr int FN = 4;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1, li = lane & 15, lg = lane >> 4;
   const int Q = t.Q;
-  Stage<AT, FM> sa;  // half a tile has half of A's rows
-  Stage<BT> sb;
+  Stage<AT, FM, SETS> sa;  // half a tile has half of A's rows
+  Stage<BT, 4, SETS> sb;
   sa.init(t.A, a.lda, t.rows, tid);
   sb.init(t.B, a.ldb, t.cols, tid);
   f32x4_t acc[FM][FN], bacc[2];
@@ -155,25 +155,27 @@ __device__ __forceinline__ void group_mid_tile(const GroupArgs &a, const Tile &t
     for (int j = 0; j < FN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   bacc[0] = bacc[1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-  const auto write = [&](int p) {
-    sa.write(lds + p * BUFFER);
-    sb.write(lds + p * BUFFER + OPERAND);
+  const auto write = [&](int to, int from) {
+    sa.write(lds + to * BUFFER, from);
+    sb.write(lds + to * BUFFER + OPERAND, from);
   };
-  const auto load = [&](int left) {
-    sa.load(left, tid);
-    sb.load(left, tid);
+  const auto load = [&](int left, int to) {
+    sa.load(left, tid, to);
+    sb.load(left, tid, to);
   };
-  // k tile k0 of buffer p, the next one to LDS and the one after it to
-  // registers; `all` says that the latter is inside as a whole (the loop of
-  // such tiles has no branch, at whose end a load would be waited for)
+  // k tile k0, of buffer p: the next one to LDS and the one SETS
+  // after that to the registers this frees; `all` says that the latter is
+  // inside as a whole (the loop of such tiles has no branch, at whose end a
+  // load would be waited for)
   const auto tile = [&](int k0, int p, auto all) {
+    const int set = SETS == 1 ? 0 : 1 - p;
     const char *now = lds + p * BUFFER;
-    if (Q - k0 > BK) write(1 - p);
+    if (Q - k0 > BK) write(1 - p, set);
     if constexpr (decltype(all)::value) {
-      sa.load_all();
-      sb.load_all();
+      sa.load_all(set);
+      sb.load_all(set);
     } else {
-      load(Q - k0 - 2 * BK);
+      load(Q - k0 - (SETS + 1) * BK, set);
     }
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
@@ -198,13 +200,25 @@ __device__ __forceinline__ void group_mid_tile(const GroupArgs &a, const Tile &t
     }
     __syncthreads();
   };
-  load(Q);
-  if (Q > 0) write(0);
-  load(Q - BK);
+#pragma unroll
+  for (int i = 0; i < SETS; ++i) load(Q - i * BK, i);
+  if (Q > 0) write(0, 0);
+  load(Q - SETS * BK, 0);
   __syncthreads();
   int k0 = 0, p = 0;
-  for (; k0 + 3 * BK <= Q; k0 += BK, p ^= 1) tile(k0, p, std::true_type{});
-  for (; k0 < Q; k0 += BK, p ^= 1) tile(k0, p, std::false_type{});
+  if constexpr (SETS == 1) {
+    for (; k0 + 3 * BK <= Q; k0 += BK, p ^= 1) tile(k0, p, std::true_type{});
+    for (; k0 < Q; k0 += BK, p ^= 1) tile(k0, p, std::false_type{});
+  } else {  // (registers are chosen by constants)
+    for (; k0 + 5 * BK <= Q; k0 += 2 * BK) {
+      tile(k0, 0, std::true_type{});
+      tile(k0 + BK, 1, std::true_type{});
+    }
+    for (; k0 < Q; k0 += 2 * BK) {
+      tile(k0, 0, std::false_type{});
+      if (k0 + BK < Q) tile(k0 + BK, 1, std::false_type{});
+    }
+  }
 
   // The results go through LDS, 32 FM rows of 512 bytes, so that whole rows of
   // the tile are written at once.
@@ -232,7 +246,8 @@ __device__ __forceinline__ void group_mid_tile(const GroupArgs &a, const Tile &t
   }
 }
 
-template <int MODE>
+// BM: rows of a tile, 128 or 64.
+template <int MODE, int BM>
 __global__ void __launch_bounds__(256, 2) group_mid_kernel(GroupArgs a, int NT) {
   constexpr bool BT = MODE != GROUP_FWD;
   __shared__ __attribute__((aligned(1024))) char lds[2 * BUFFER];
@@ -252,7 +267,7 @@ __global__ void __launch_bounds__(256, 2) group_mid_kernel(GroupArgs a, int NT) 
     t.B += (int64_t)q0 * a.ldb + t.c0;
   } else {
     int row1;
-    if (!tile_of(a.off, a.G, a.M, BM, NT, blockIdx.x, t.g, t.row0, row1, nt)) return;
+    if (!tile_of<BM == 128>(a.off, a.G, a.M, BM, NT, blockIdx.x, t.g, t.row0, row1, nt)) return;
     t.rows = row1 - t.row0;
     t.c0 = nt * BN;
     t.A += (int64_t)t.row0 * a.lda;
@@ -260,17 +275,32 @@ __global__ void __launch_bounds__(256, 2) group_mid_kernel(GroupArgs a, int NT) 
   }
   t.cols = min(BN, a.N - t.c0);
   t.sums = MODE == GROUP_DW && a.db != nullptr && nt == 0;
-  if (MODE != GROUP_DW && t.rows <= BM / 2) group_mid_tile<MODE, 2>(a, t, lds);
-  else group_mid_tile<MODE, 4>(a, t, lds);
+  if constexpr (BM == 64) group_mid_tile<MODE, 2, 2>(a, t, lds);
+  else if (MODE != GROUP_DW && t.rows <= BM / 2) group_mid_tile<MODE, 2, 1>(a, t, lds);
+  else group_mid_tile<MODE, 4, 1>(a, t, lds);
 }
 
-template <int MODE> hipError_t run_mode(const GroupArgs &a, hipStream_t s) {
+template <int MODE, int BM> hipError_t run_tiles(const GroupArgs &a, hipStream_t s) {
   const int64_t NT = (a.N + BN - 1) / BN;
   const int64_t blocks = MODE == GROUP_DW ? piece_blocks(a, (int64_t)((a.M + BM - 1) / BM) * NT)
                                           : tile_blocks(a.M, a.G, BM, NT);
   if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL(group_mid_kernel<MODE>, dim3((uint32_t)blocks), dim3(256), 0, s, a, (int)NT);
+  hipLaunchKernelGGL((group_mid_kernel<MODE, BM>), dim3((uint32_t)blocks), dim3(256), 0, s, a, (int)NT);
   return hipGetLastError();
+}
+
+// Tiles of 64 rows, and loads two k tiles ahead, if a CU has at most two of
+// them: us for 64 and for 128 rows, forward, 20 groups, 1,500 rows, 800 -> 700
+// (198 tiles of 64 rows), 14.9 and 20.4; 1 group, 2,000, 2048 -> 512 (124), 19.9
+// and 25.1; 6, 16,000, 646 -> 191 (506), 18.7 and 20.2; but 4, 4,096, 1024 ->
+// 1024 (528), 30.8 and 24.9.
+template <int MODE> hipError_t run_mode(const GroupArgs &a, hipStream_t s) {
+  if constexpr (MODE != GROUP_DW) {
+    // a group's last tile half full on average
+    const int64_t tiles = ((int64_t)a.M + 32 * a.G) / 64 * ((a.N + BN - 1) / BN);
+    if (tiles <= 2 * kCUs) return run_tiles<MODE, 64>(a, s);
+  }
+  return run_tiles<MODE, 128>(a, s);
 }
 
 }  // namespace
