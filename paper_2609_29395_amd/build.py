@@ -1,4 +1,4 @@
-"""Build libgcpsl.so (HIP, gfx950) in-tree with hipcc.
+"""Build libgcpsl.so (HIP, gfx950) and _ops.so (its short way from Python) in-tree.
 
 Usage: python -m paper_2609_29395_amd.build   (or build() from Python)
 """
@@ -9,11 +9,13 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJDIR = os.path.join(os.path.dirname(HERE), "_build", "gcpsl")
 LIB = os.path.join(HERE, "libgcpsl.so")
+BIND = os.path.join(HERE, "_ops.so")
 SOURCES = ["api.cpp", "assign.cpp", "k_conv.hip", "k_conv_f32.hip", "k_misc.hip", "k_wgrad_lds.hip", "k_conv_lds.hip", "k_conv_img.hip", "k_norm.hip", "k_block.hip",
            "ops.cpp", "k_group.hip", "k_group_tile.hip", "k_group_f32.hip", "k_group_mid.hip",
            "k_group_few.hip", "k_score.hip", "k_drop.hip"]
@@ -47,11 +49,30 @@ def _compile(src: str) -> str:
     return obj
 
 
+def _compile_bind() -> None:
+    """csrc/bind.cpp against torch's headers: host code only."""
+    import torch
+    root = os.path.dirname(torch.__file__)
+    include = os.path.join(root, "include")
+    tmp = BIND + ".tmp"
+    cmd = [_hipcc(), "-x", "c++", "-O2", "-fPIC", "-std=c++17", "-Wall", "-shared",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-isystem", include, "-isystem", os.path.join(include, "torch", "csrc", "api", "include"),
+           "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "bind.cpp"), "-o", tmp,
+           "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"hipcc failed for bind.cpp:\n{r.stderr}")
+    os.replace(tmp, BIND)
+
+
 def build(verbose: bool = False) -> str:
-    """Compile every HIP/C++ source for gfx950 and link libgcpsl.so."""
+    """Compile every HIP/C++ source for gfx950 and link libgcpsl.so and _ops.so."""
     os.makedirs(OBJDIR, exist_ok=True)
     with cf.ThreadPoolExecutor(max_workers=min(6, len(SOURCES))) as ex:
+        bind = ex.submit(_compile_bind)
         objs = list(ex.map(_compile, SOURCES))
+        bind.result()
     tmp = LIB + ".tmp"
     cmd = [_hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)

@@ -190,12 +190,18 @@ def fuse_replicas(theta, weights, stream=None):
 # Tensors are on the current GPU, rows of consecutive elements (any row
 # stride).  Every function returns the tensors it wrote: those given as out,
 # dw, db, or new ones.  stream: a torch stream, the current one by default;
-# what is newly allocated for another stream is marked as used there.  The
-# smallest calls are bound by the host: checks read each attribute once, and
-# the current stream is asked for as the bare handle.
+# what is newly allocated for another stream is marked as used there.
+#
+# The smallest calls are bound by the host.  A call on the current stream that
+# brings no workspace goes through csrc/bind.cpp in one native call, which
+# checks, allocates and launches; what that does not take (it answers None) and
+# every other call is checked here, by the same rules, with a message.
 
 _torch = None
 _types = {}
+_ops = None
+_ENTRIES = ["gcpsl_group_forward", "gcpsl_group_input_grad", "gcpsl_group_workspace_bytes", "gcpsl_group_weight_grad",
+            "gcpsl_dropout", "gcpsl_score_workspace_bytes", "gcpsl_score", "gcpsl_score_grad"]
 
 
 def _load_torch():
@@ -204,6 +210,28 @@ def _load_torch():
     _types.update({torch.float32: 0, torch.bfloat16: 1})
     _torch = torch
     return torch
+
+
+def _native():
+    """csrc/bind.cpp's module, on the entries of the library that lib() loaded (raises if it has not been built)."""
+    global _ops
+    if _ops is None:
+        torch = _torch or _load_torch()
+        from . import _ops as module
+        L = lib()
+        module.init(tuple(C.cast(getattr(L, name), C.c_void_p).value for name in _ENTRIES), torch._C._cuda_getDevice,
+                    torch._C._cuda_getCurrentRawStream, Scores)
+        _ops = module
+    return _ops
+
+
+def _done(result):
+    """Whether a native call made its result; raises for the library's error code."""
+    if result is None:
+        return False
+    if result.__class__ is int:
+        _check(result)
+    return True
 
 
 def _begin(t, stream):
@@ -290,6 +318,10 @@ def group_forward(x, offsets, w, bias=None, relu=False, p=0.0, seed=0, out=None,
     """gcpsl_group_forward: [rows][n] = dropout(relu(W_g x_r + b_g)) of x
     [rows][k], rows offsets[g] to offsets[g + 1] through w[g] of [G][n][k]
     and bias[g] of [G][n] (fp32)."""
+    if stream is None:
+        r = (_ops or _native()).group_forward(x, offsets, w, bias, relu, p, seed, out)
+        if _done(r):
+            return r
     torch, code, handle, device = _begin(x, stream)
     dtype = x.dtype
     xp, ldx = _rows(x, "x", dtype, device)
@@ -308,6 +340,10 @@ def group_input_grad(dy, offsets, w, gate=None, p=0.0, out=None, stream=None):
     """gcpsl_group_input_grad: [rows][k] = W_g^T dy_r of dy [rows][n]; with
     the layer's input as gate, which a ReLU and a dropout of probability p
     made, the gradient through those."""
+    if stream is None:
+        r = (_ops or _native()).group_input_grad(dy, offsets, w, gate, p, out)
+        if _done(r):
+            return r
     torch, code, handle, device = _begin(dy, stream)
     dtype = dy.dtype
     dp, lddy = _rows(dy, "dy", dtype, device)
@@ -336,6 +372,10 @@ def group_workspace_bytes(dtype, G, rows, n, k):
 def group_weight_grad(dy, x, offsets, dw=None, db=None, bias=True, workspace=None, stream=None):
     """gcpsl_group_weight_grad: (dw [G][n][k], db [G][n]) in fp32 from dy
     [rows][n] and x [rows][k]; db is None with bias=False."""
+    if stream is None and workspace is None:
+        r = (_ops or _native()).group_weight_grad(dy, x, offsets, dw, db, bias)
+        if _done(r):
+            return r
     torch, code, handle, device = _begin(dy, stream)
     dp, lddy = _rows(dy, "dy", dy.dtype, device)
     off, G = _offsets(offsets, torch, device)
@@ -363,6 +403,10 @@ def group_weight_grad(dy, x, offsets, dw=None, db=None, bias=True, workspace=Non
 def dropout(x, p, seed, out=None, stream=None):
     """gcpsl_dropout of x [rows][cols]; out may be x.  The same call on the
     output's gradient is the backward pass."""
+    if stream is None:
+        r = (_ops or _native()).dropout(x, p, seed, out)
+        if _done(r):
+            return r
     torch, code, handle, device = _begin(x, stream)
     xp, ldx = _rows(x, "x", x.dtype, device)
     rows, cols = x.shape
@@ -393,6 +437,10 @@ def score_workspace_bytes(dtype, rows, L, top=0):
 
 def score(logits, labels=None, top=0, workspace=None, stream=None):
     """gcpsl_score of logits [rows][L] and int32 labels [rows]."""
+    if stream is None and workspace is None:
+        r = (_ops or _native()).score(logits, labels, top)
+        if _done(r):
+            return r
     torch, code, handle, device = _begin(logits, stream)
     zp, ldz = _rows(logits, "logits", logits.dtype, device)
     rows, L = logits.shape
@@ -412,6 +460,10 @@ def score_grad(logits, labels, lse, entropy=None, g_logp=None, g_entropy=None, o
     """gcpsl_score_grad: the loss's gradient by the logits [rows][L], given
     those by logp (g_logp [rows]) and by entropy (g_entropy [rows]), of which
     one may be None; out may be the logits."""
+    if stream is None:
+        r = (_ops or _native()).score_grad(logits, labels, lse, entropy, g_logp, g_entropy, out)
+        if _done(r):
+            return r
     torch, code, handle, device = _begin(logits, stream)
     zp, ldz = _rows(logits, "logits", logits.dtype, device)
     rows, L = logits.shape
