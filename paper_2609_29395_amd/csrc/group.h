@@ -19,6 +19,8 @@ bool group_mid_ok(int dtype, const GroupArgs &a, int mode);
 hipError_t launch_group_mid(int mode, const GroupArgs &a, hipStream_t s);
 bool group_f32_ok(const GroupArgs &a, int mode);
 hipError_t launch_group_f32(int mode, const GroupArgs &a, hipStream_t s);
+bool group_f32_deep_ok(const GroupArgs &a, int mode);
+hipError_t launch_group_f32_deep(int mode, const GroupArgs &a, hipStream_t s);
 
 #define GROUP_DEVICE __device__ __forceinline__
 

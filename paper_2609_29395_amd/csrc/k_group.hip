@@ -20,7 +20,8 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 // registers element by element, so any stride and size will do, into LDS rows
 // of consecutive q; both operands' fragments are 16-byte LDS reads.
 //
-// What is left to it: fp32 results of fewer than 64 columns, operands of fewer
+// What is left to it: narrow fp32 results (fewer than 64 columns, 32 where there
+// are few tiles), operands of fewer
 // elements than a vector, row strides past 2^22.  Bound by the element loads:
 // 65,536 rows of 8 groups, 128 -> 10, fp32, 20 us, 1.8 TB/s (7 us at a copy's
 // rate); the kernels of 128 columns would waste most of their products on it.
@@ -277,6 +278,7 @@ hipError_t launch_group(int dtype, int mode, const GroupArgs &a, hipStream_t s) 
   if (group_few_ok(dtype, a, mode)) e = launch_group_few(dtype, mode, a, s);
   else if (group_tile_ok(dtype, a, mode) && fills_half(a, mode)) e = launch_group_tile(mode, a, s);
   else if (group_mid_ok(dtype, a, mode)) e = launch_group_mid(mode, a, s);
+  else if (dtype == GCPSL_F32 && group_f32_deep_ok(a, mode)) e = launch_group_f32_deep(mode, a, s);
   else if (dtype == GCPSL_F32 && a.N >= 64 && group_f32_ok(a, mode)) e = launch_group_f32(mode, a, s);
   else e = dtype == GCPSL_BF16 ? launch_any<bf16_t>(mode, a, s) : launch_any<float>(mode, a, s);
   if (e == hipSuccess && mode == GROUP_DW && a.slots > 0) {

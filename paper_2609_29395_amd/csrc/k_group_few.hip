@@ -260,26 +260,28 @@ template <typename T> hipError_t run(int dtype, int mode, const GroupArgs &a, hi
 }  // namespace
 
 // A vector at least in the operands' rows, and few rows or so few tiles that
-// kernels of 128 x 128 tiles, of which a CU has one or none, take longer than
-// this one, whose time goes with the tiles.  us here and there:
-//   forward, fp32   5 groups, 433 rows, 4096 -> 1024 (513 tiles)     84   150
-//                   1 group, 1,307 rows, 512 -> 640 (827)            23    26
-//                   8 groups, 1,024 rows, 1024 -> 1024 (1,152)       46    44
-//   forward, bf16   5 groups, 433 rows, 4096 -> 1024 (513)           34    43
-//                   1 group, 1,307 rows, 512 -> 640 (827)            11.3   9.8
+// the kernels of 64 x 64, 64 x 128 and 128 x 128 tiles, of which a CU has one or
+// none, take longer than this one, whose time goes with the tiles.  us here and
+// there:
+//   forward, fp32   1 group, 64 rows, 4096 -> 4096 (256 tiles)       33    56
+//                   1 group, 1,000 rows, 2000 -> 300 (310)           41    37
+//                   1 group, 1,307 rows, 512 -> 640 (827)            23    13
+//      short sums   6 groups, 4,000 rows, 128 -> 64 (254)            5.3   6.8
+//   forward, bf16   5 groups, 433 rows, 4096 -> 1024 (513)           34    40
+//                   1 group, 1,307 rows, 512 -> 640 (827)            11.1  9.7
 //   (rows at odd    1 group, 25 rows, 2013 -> 71 (3)                 13    22
-//    addresses)     33 groups, 1,236 rows, 1687 -> 396 (716)         66    25
-//   input grad.,    8 groups, 1,024 rows, 1024 -> 1024 (576)         33    40
-//      fp32         2 groups, 600 rows, 2000 -> 2000 (640)           87    70
-//   input grad.,    5 groups, 433 rows, 1024 -> 4096 (128)           21    44
-//      bf16         2 groups, 600 rows, 2000 -> 2000 (320)           26    26
+//    addresses)     33 groups, 1,236 rows, 1687 -> 396 (716)         51    29
+//   input grad.,    5 groups, 433 rows, 1024 <- 4096 (256)           46    60
+//      fp32         4 groups, 500 rows, 1024 <- 4096 (272)           106   57
+//   input grad.,    5 groups, 433 rows, 4096 <- 1024 (128)           22    42
+//      bf16         8 groups, 1,024 rows, 1024 <- 1024 (288)         14.8  15.2
 bool group_few_ok(int dtype, const GroupArgs &a, int mode) {
   const bool bf16 = dtype == GCPSL_BF16;
   const int vec = bf16 ? 8 : 4;
   if (mode == GROUP_DW || a.Q < vec) return false;
   const int64_t tiles = tiles32(dtype, a, mode);
-  if (mode == GROUP_DX) return a.N >= vec && tiles <= (bf16 ? 320 : 512);
-  return few_rows(a) || tiles <= (!bf16 ? 768 : (a.lda | a.ldb) & 1 ? 256 : 640);
+  if (mode == GROUP_DX) return a.N >= vec && tiles <= (bf16 ? 320 : a.Q < 256 ? 512 : 256);
+  return few_rows(a) || tiles <= (!bf16 ? (a.Q < 256 ? 768 : 304) : (a.lda | a.ldb) & 1 ? 256 : 640);
 }
 
 hipError_t launch_group_few(int dtype, int mode, const GroupArgs &a, hipStream_t s) {
