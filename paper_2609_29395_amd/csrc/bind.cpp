@@ -283,6 +283,15 @@ PyObject *dropout(PyObject *, PyObject *const *a, Py_ssize_t na) {
   });
 }
 
+// Entries [first, ..) of a vector of 4-byte entries as a tensor of its own (five allocations took 1.3 us longer).
+Tensor part(const Tensor &held, int64_t first, at::IntArrayRef shape, at::ScalarType type) {
+  Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(held.storage()), held.key_set(),
+                                                      c10::scalarTypeToTypeMeta(type));
+  t.unsafeGetTensorImpl()->set_storage_offset(first);
+  t.unsafeGetTensorImpl()->set_sizes_contiguous(shape);
+  return t;
+}
+
 // score(logits, labels, top)
 PyObject *score(PyObject *, PyObject *const *a, Py_ssize_t na) {
   return guarded(na, 3, [&] {
@@ -295,9 +304,11 @@ PyObject *score(PyObject *, PyObject *const *a, Py_ssize_t na) {
     size_t need = 0;
     call(entry.score_workspace_bytes, c.code, z.rows, L, top, &need);  // (refuses a top that is not a size)
     const Tensor work = need ? c.empty({(int64_t)need}, at::kByte) : Tensor();
-    const Tensor logp = given ? c.empty({z.rows}, at::kFloat) : Tensor(), entropy = c.empty({z.rows}, at::kFloat),
-                 lse = c.empty({z.rows}, at::kFloat), top_logp = c.empty({z.rows, top}, at::kFloat),
-                 top_class = c.empty({z.rows, top}, at::kInt);
+    const int64_t n = z.rows;
+    const Tensor held = c.empty({n * (3 + 2 * (int64_t)top)}, at::kFloat);
+    const Tensor logp = given ? part(held, 0, {n}, at::kFloat) : Tensor(), entropy = part(held, n, {n}, at::kFloat),
+                 lse = part(held, 2 * n, {n}, at::kFloat), top_logp = part(held, 3 * n, {n, top}, at::kFloat),
+                 top_class = part(held, (3 + top) * n, {n, top}, at::kInt);
     call(entry.score, c.code, z.rows, L, z.p, z.ld, labels, top, given ? (float *)logp.data_ptr() : nullptr,
          (float *)entropy.data_ptr(), (float *)lse.data_ptr(), (float *)top_logp.data_ptr(),
          (int32_t *)top_class.data_ptr(), need ? work.data_ptr() : nullptr, need, c.stream);

@@ -1,4 +1,5 @@
-"""ctypes binding of libgcpsl.so (include/gcpsl.h): argument marshalling only.
+"""Binding of libgcpsl.so (include/gcpsl.h), by ctypes and, for regular calls of the operators on tensors, _ops.so:
+argument marshalling only.
 
 Every computation of the hot path runs in the library's HIP kernels.  PyTorch
 is used for device memory (the caller-owned buffers the C ABI works in) and
