@@ -8,6 +8,8 @@
 #include "ops.h"
 #include "runtime.h"
 
+constexpr uint32_t kCUs = 256;
+
 // Row stride up to which the offsets within 256 rows stay below 2^31 bytes.
 constexpr int64_t kMaxTileLd = 1 << 22;
 
@@ -20,6 +22,15 @@ hipError_t launch_group_mid(int mode, const GroupArgs &a, hipStream_t s);
 bool group_f32_ok(const GroupArgs &a, int mode);
 hipError_t launch_group_f32(int mode, const GroupArgs &a, hipStream_t s);
 bool group_f32_deep_ok(const GroupArgs &a, int mode);
+// fp32 weight gradients [n][k] of G groups, `rows` in all, that tiles of 64 x 64
+// take: at most one a CU, and no more rows than that they, faster to begin and
+// end, are not passed by the larger tiles' rate.  us so and with 128 x 128: 1
+// group of 813 rows, 64 -> 256, 11 and 19; 1 of 2,000, 1024 -> 1024 (512,000
+// tiles x rows), 41 and 50; 1 of 20,000, 512 -> 512 (1,280,000), 97 and 80.
+inline bool group_f32_deep_grad(int G, int64_t rows, int n, int k) {
+  const int64_t tiles = (int64_t)((n + 63) / 64) * ((k + 63) / 64);
+  return tiles * G <= kCUs && tiles * rows <= 2560 * (int64_t)kCUs;
+}
 hipError_t launch_group_f32_deep(int mode, const GroupArgs &a, hipStream_t s);
 
 #define GROUP_DEVICE __device__ __forceinline__
@@ -147,7 +158,6 @@ GROUP_DEVICE bool piece_of(const GroupArgs &a, uint32_t tiles, uint32_t b, int &
 // round of one per CU are halved if they still make no more than a round: a CU
 // that takes one tile more than the others makes them wait for half as long.
 // (What a result is the sum of, and in which order, does not depend on it.)
-constexpr uint32_t kCUs = 256;
 template <bool HALVES = true>
 GROUP_DEVICE bool tile_of(const int32_t *off, int G, int rows, int bm, int NT_, uint32_t b, int &g, int &row0, int &row1,
                           int &nt) {

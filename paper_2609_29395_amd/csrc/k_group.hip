@@ -246,27 +246,29 @@ bool fills_half(const GroupArgs &a, int mode) {
 // take longer than its partial, written and read again: 1,024 for tiles of
 // 256 x 256 (15 us against 10).  For the others a piece of p rows costs about
 // p a in products and, over all of the rows, rows tiles b / p in partials, the
-// sum of which is least at p = sqrt(rows tiles b / a); 128 at least (two steps
-// of the bf16 kernel; 64 are no faster) and 512 at most.  us with this and with
-// 512 throughout: 1 group of 8,192 rows, 64 -> 64, fp32 18 and 35, bf16 14 and
-// 16; 1 of 1,024, 1024 -> 1024, fp32 31 and 43.  The tile is the one that the
-// operands most likely take.
+// sum of which is least at p = sqrt(rows tiles b / a), b / a about 4 for bf16, 1
+// for fp32 tiles of 128 x 128 and 0.5 for those of 64 x 64; 128 at least (two
+// steps of the bf16 kernel; 64 are no faster) and 512 at most.  us with this and
+// with 512 throughout: 1 group of 8,192 rows, 64 -> 64, bf16, 14 and 16; 1 of
+// 1,024, 1024 -> 1024, fp32 in 128 x 128, 31 and 43.  The tile is the one that
+// the operands most likely take.
 //
 // No group is cut, and the join's launch saved (1.5 to 2 us), where the largest
 // one, taken as three times the average, has no more rows than that is worth,
 // and all of them in one group would not take much longer.  With the input
-// gradient, us so and in pieces: 8 groups of 1,024 rows, 1000 -> 500, bf16 25.3
-// and 27.6; 4 of 256, 256 -> 256, fp32 17.3 and 19.1.
+// gradient, us so and in pieces, bf16: 8 groups of 1,024 rows, 1000 -> 500, 25.3
+// and 27.6; 4 of 256, 256 -> 256, 12.9 and 14.5.
 GroupPieces group_pieces(int dtype, int G, int64_t rows, int n, int k) {
   const bool big = dtype == GCPSL_BF16 && n % 8 == 0 && k % 8 == 0 &&
                    tiles_fill_half((int64_t)((n + 255) / 256) * G, k);
-  const int64_t tile = big ? 256 : 128, slots = big ? kCUs : 2 * kCUs;
+  const bool deep = dtype == GCPSL_F32 && group_f32_deep_grad(G, rows, n, k);
+  const int64_t tile = big ? 256 : deep ? 64 : 128, slots = big || deep ? kCUs : 2 * kCUs;
   const int64_t tiles = ((n + tile - 1) / tile) * ((k + tile - 1) / tile);
   const int64_t even = tiles >= slots ? rows : rows * tiles / slots;
-  const double b_by_a = dtype == GCPSL_BF16 ? 4 : 1;
+  const double b_by_a = dtype == GCPSL_BF16 ? 4 : deep ? 0.5 : 1;
   const int64_t least =
       big ? 1024 : std::min<int64_t>(512, std::max<int64_t>(128, (int64_t)std::sqrt(b_by_a * (double)rows * (double)tiles)));
-  const int64_t whole = dtype == GCPSL_BF16 ? 384 : 192;
+  const int64_t whole = dtype == GCPSL_BF16 || deep ? 384 : 192;
   const bool one = rows <= 4 * whole && std::min(rows, 3 * rows / G) <= whole;
   const int64_t piece = one ? rows + 1 : std::min<int64_t>(std::max<int64_t>(even, least), 1 << 30);
   // a group of p > 1 pieces has more than (p - 1/2) piece >= 3/4 p piece rows

@@ -1,6 +1,6 @@
-// Forward products and input gradients over rows grouped by cluster, fp32
-// (gfx950), where 128 x 128 tiles are fewer than CUs: 64 x 64 outputs a
-// workgroup, on the bf16 matrix cores (group_f32.h).
+// Products over rows grouped by cluster, fp32 (gfx950), where 128 x 128 tiles
+// are fewer than CUs: 64 x 64 outputs a workgroup, on the bf16 matrix cores
+// (group_f32.h).
 //
 // Two teams of four waves share the sum: of the k tiles, 32 deep, one takes the
 // even ones and the other the odd ones, each with two LDS buffers of its own,
@@ -28,7 +28,7 @@ constexpr int PLANE = 64 * BK * 2;  // bytes of one bf16 part of an operand's ti
 constexpr int BUFFER = 6 * PLANE;
 constexpr int LDS_BYTES = 4 * BUFFER;  // two for each team
 constexpr int SUMS = BM * BN * 4;      // bytes of a team's sums
-static_assert(2 * SUMS <= LDS_BYTES, "the teams' sums");
+static_assert(2 * SUMS + 8 * BM * 4 <= LDS_BYTES, "the teams' sums");
 
 // 16-byte piece c (8 k) of row r in a plane; the XOR puts the 16 rows that a
 // fragment read takes at a time on all banks.
@@ -93,6 +93,13 @@ template <bool T> struct Stage {
         v[set][j][i] = k < left ? x : 0.f;
       }
   }
+  // T: the sums of the thread's two columns in a set
+  __device__ __forceinline__ void sum(int set, float (&s)[2]) const {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[j] += v[set][j][i];
+  }
   // splits the values and writes them; returns the largest magnitude so far
   __device__ __forceinline__ float write(char *planes, int set, float top) const {
 #pragma unroll
@@ -116,16 +123,32 @@ template <bool T> struct Stage {
 
 template <int MODE>
 __global__ void __launch_bounds__(512, 2) group_f32_deep_kernel(GroupArgs a, int NT) {
-  constexpr bool BT = MODE != GROUP_FWD;
+  constexpr bool AT = MODE == GROUP_DW, BT = MODE != GROUP_FWD;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int tid = threadIdx.x, lane = tid & 63, t = tid & 255;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int team = wave >> 2, wm = wave >> 1 & 1, wn = wave & 1, li = lane & 31, lg = lane >> 5;
-  int g, row0, row1, nt;
-  if (!tile_of<false>(a.off, a.G, a.M, BM, NT, blockIdx.x, g, row0, row1, nt)) return;
-  const int rows = row1 - row0, c0 = nt * BN, cols = min(BN, a.N - c0), Q = a.Q;
-  const float *A = (const float *)a.a + (int64_t)row0 * a.lda;
-  const float *B = (const float *)a.b + g * a.b_gs + (BT ? (int64_t)c0 : (int64_t)c0 * a.ldb);
+  int g, row0, row1, nt, Q = a.Q, slot = -1;
+  const float *A = (const float *)a.a, *B = (const float *)a.b;
+  if constexpr (MODE == GROUP_DW) {
+    const uint32_t MT = (uint32_t)(a.M + BM - 1) / BM;
+    uint32_t tile;
+    int mt, q0, q1;
+    if (!piece_of(a, MT * (uint32_t)NT, blockIdx.x, g, q0, q1, slot, tile)) return;
+    block_order(tile, MT, (uint32_t)NT, mt, nt);
+    row0 = mt * BM;
+    row1 = min(a.M, row0 + BM);
+    Q = q1 - q0;
+    A += (int64_t)q0 * a.lda + row0;
+    B += (int64_t)q0 * a.ldb + nt * BN;
+  } else {
+    if (!tile_of<false>(a.off, a.G, a.M, BM, NT, blockIdx.x, g, row0, row1, nt)) return;
+    A += (int64_t)row0 * a.lda;
+    B += g * a.b_gs + (BT ? (int64_t)nt * BN : (int64_t)nt * BN * a.ldb);
+  }
+  const int rows = row1 - row0, c0 = nt * BN, cols = min(BN, a.N - c0);
+  const bool sums = MODE == GROUP_DW && a.db != nullptr && nt == 0;  // of A's columns, too (the bias gradient)
+  float colsum[2] = {0.f, 0.f};
 
   f32x16_t big, small[2];
 #pragma unroll
@@ -135,6 +158,12 @@ __global__ void __launch_bounds__(512, 2) group_f32_deep_kernel(GroupArgs a, int
 
   const auto run = [&](auto &stage, bool is_a) {
     char *const mine = lds + team * 2 * BUFFER, *const part = mine + (is_a ? 0 : 3 * PLANE);
+    const auto write = [&](int to) {  // from the set of the same number
+      top = stage.write(part + to * BUFFER, to, top);
+      if constexpr (MODE == GROUP_DW) {
+        if (sums && is_a) stage.sum(to, colsum);
+      }
+    };
     const auto left = [&](int i) { return Q - (2 * i + team) * BK; };
     // the team's k tile i of buffer p, the next one to LDS and the one two after
     // that to the registers this frees; `all` says that the latter is inside as a
@@ -150,10 +179,10 @@ __global__ void __launch_bounds__(512, 2) group_f32_deep_kernel(GroupArgs a, int
           w[h][k] = *(const u32x4 *)(now + (3 + k) * PLANE + at(wn * 32 + li, 2 * h + lg));
         }
       if constexpr (decltype(all)::value) {
-        top = stage.write(part + (1 - p) * BUFFER, 1 - p, top);
+        write(1 - p);
         stage.load_all(1 - p);
       } else if (i + 1 < steps) {
-        top = stage.write(part + (1 - p) * BUFFER, 1 - p, top);
+        write(1 - p);
         if (i + 3 < steps) stage.load(left(i + 3), 1 - p);
       }
       constexpr int kw[6] = {2, 0, 1, 1, 0, 0}, kx[6] = {0, 2, 1, 0, 1, 0};
@@ -176,7 +205,7 @@ __global__ void __launch_bounds__(512, 2) group_f32_deep_kernel(GroupArgs a, int
     };
     stage.load(left(0), 0);
     if (steps > 1) stage.load(left(1), 1);
-    top = stage.write(part, 0, top);
+    write(0);
     if (steps > 2) stage.load(left(2), 0);
     __syncthreads();
     int i = 0;
@@ -190,8 +219,8 @@ __global__ void __launch_bounds__(512, 2) group_f32_deep_kernel(GroupArgs a, int
     }
   };
   const bool is_a = (wave & 2) == 0;
-  if constexpr (!BT) {
-    Stage<false> stage;
+  if constexpr (AT == BT) {
+    Stage<AT> stage;
     if (is_a) stage.init(A, a.lda, rows, t, team * BK);
     else stage.init(B, a.ldb, cols, t - 128, team * BK);
     run(stage, is_a);
@@ -213,7 +242,7 @@ __global__ void __launch_bounds__(512, 2) group_f32_deep_kernel(GroupArgs a, int
     const int m = wm * 32 + li, c = wn * 32 + li;
     for (int k0 = 2 * team; k0 < Q; k0 += 4) {
       const int k = k0 + lg;
-      const float x = m < rows && k < Q ? A[(int64_t)m * a.lda + k] : 0.f;
+      const float x = m < rows && k < Q ? (AT ? A[(int64_t)k * a.lda + m] : A[(int64_t)m * a.lda + k]) : 0.f;
       const float w = c < cols && k < Q ? (BT ? B[(int64_t)k * a.ldb + c] : B[(int64_t)c * a.ldb + k]) : 0.f;
       big = __builtin_amdgcn_mfma_f32_32x32x2f32(w, x, big, 0, 0, 0);
     }
@@ -223,7 +252,7 @@ __global__ void __launch_bounds__(512, 2) group_f32_deep_kernel(GroupArgs a, int
   // in four groups of four, columns 8 q + 4 lg .. + 3 of row li.
   const auto place = [&](int which, int r, int c) { return lds + which * SUMS + r * 256 + ((c >> 2) ^ (r & 15)) * 16; };
   const int r0 = tid >> 4, c4 = (tid & 15) * 4;
-  const FinishRows<float, MODE, 2> out(a, g, row0 + r0, 32, row1, c0 + c4);
+  const FinishRows<float, MODE == GROUP_DW ? GROUP_FWD : MODE, 2> out(a, g, row0 + r0, 32, row1, c0 + c4);
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     f32x4_t v;
@@ -231,10 +260,28 @@ __global__ void __launch_bounds__(512, 2) group_f32_deep_kernel(GroupArgs a, int
     for (int r = 0; r < 4; ++r) v[r] = big[4 * q + r] + (small[0][4 * q + r] + small[1][4 * q + r]);
     *(f32x4_t *)place(team, wm * 32 + li, wn * 32 + 8 * q + 4 * lg) = v;
   }
+  // each column's shares: two teams, four pieces of 8 of their k tiles' 32
+  float *const shares = (float *)(lds + 2 * SUMS);
+  if (sums && is_a)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) shares[(team * 4 + (t >> 5)) * 64 + ((min((t & 31) * 2, rows - 2) + j) & 63)] = colsum[j];
   __syncthreads();
-  out.store(a, [&](int i, int) {
+  const auto sum = [&](int i, int) {
     return *(const f32x4_t *)place(0, r0 + 32 * i, c4) + *(const f32x4_t *)place(1, r0 + 32 * i, c4);
-  });
+  };
+  if constexpr (MODE == GROUP_DW) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (r0 + 32 * i < rows && c0 + c4 < a.N) store_grad(a, g, slot, row0 + r0 + 32 * i, c0 + c4, sum(i, 0));
+    if (sums && tid < rows) {
+      float v = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v += shares[i * 64 + tid];
+      store_bias_grad(a, g, slot, row0 + tid, v);
+    }
+  } else {
+    out.store(a, sum);
+  }
 }
 
 template <int MODE> hipError_t run_mode(const GroupArgs &a, hipStream_t s) {
@@ -245,7 +292,9 @@ template <int MODE> hipError_t run_mode(const GroupArgs &a, hipStream_t s) {
     if (e != hipSuccess) return e;
     once.mark();
   }
-  const int64_t NT = (a.N + BN - 1) / BN, blocks = tile_blocks(a.M, a.G, BM, NT);
+  const int64_t NT = (a.N + BN - 1) / BN;
+  const int64_t blocks = MODE == GROUP_DW ? piece_blocks(a, (int64_t)((a.M + BM - 1) / BM) * NT)
+                                          : tile_blocks(a.M, a.G, BM, NT);
   if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(group_f32_deep_kernel<MODE>, dim3((uint32_t)blocks), dim3(512), LDS_BYTES, s, a, (int)NT);
   return hipGetLastError();
@@ -259,10 +308,12 @@ template <int MODE> hipError_t run_mode(const GroupArgs &a, hipStream_t s) {
 // (200), 13 and 23; input gradient, 4 of 500, 1024 <- 4096 (144), 57 and 106;
 // with more, 16 of 3,000 rows, 600 -> 600 (540), 45 and 37.
 bool group_f32_deep_ok(const GroupArgs &a, int mode) {
-  if (mode == GROUP_DW || a.N < 32 || !group_f32_ok(a, mode)) return false;
+  if (a.N < 32 || !group_f32_ok(a, mode)) return false;
+  if (mode == GROUP_DW) return group_f32_deep_grad(a.G, a.Q, a.M, a.N);
   return ((int64_t)a.M + 32 * a.G) / 64 * ((a.N + BN - 1) / BN) <= kCUs;
 }
 
 hipError_t launch_group_f32_deep(int mode, const GroupArgs &a, hipStream_t s) {
-  return mode == GROUP_FWD ? run_mode<GROUP_FWD>(a, s) : run_mode<GROUP_DX>(a, s);
+  return mode == GROUP_FWD ? run_mode<GROUP_FWD>(a, s)
+                           : mode == GROUP_DX ? run_mode<GROUP_DX>(a, s) : run_mode<GROUP_DW>(a, s);
 }

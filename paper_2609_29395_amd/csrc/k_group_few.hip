@@ -280,7 +280,7 @@ bool group_few_ok(int dtype, const GroupArgs &a, int mode) {
   const int vec = bf16 ? 8 : 4;
   if (mode == GROUP_DW || a.Q < vec) return false;
   const int64_t tiles = tiles32(dtype, a, mode);
-  if (mode == GROUP_DX) return a.N >= vec && tiles <= (bf16 ? 320 : a.Q < 256 ? 512 : 256);
+  if (mode == GROUP_DX) return a.N >= vec && tiles <= (bf16 ? 320 : a.Q < 256 || !group_f32_deep_ok(a, mode) ? 512 : 256);
   return few_rows(a) || tiles <= (!bf16 ? (a.Q < 256 ? 768 : 304) : (a.lda | a.ldb) & 1 ? 256 : 640);
 }
 
