@@ -23,13 +23,14 @@ bool group_f32_ok(const GroupArgs &a, int mode);
 hipError_t launch_group_f32(int mode, const GroupArgs &a, hipStream_t s);
 bool group_f32_deep_ok(const GroupArgs &a, int mode);
 // fp32 weight gradients [n][k] of G groups, `rows` in all, that tiles of 64 x 64
-// take: at most one a CU, and no more rows than that they, faster to begin and
-// end, are not passed by the larger tiles' rate.  us so and with 128 x 128: 1
-// group of 813 rows, 64 -> 256, 11 and 19; 1 of 2,000, 1024 -> 1024 (512,000
-// tiles x rows), 41 and 50; 1 of 20,000, 512 -> 512 (1,280,000), 97 and 80.
+// take: at most one a CU, and so few rows for each of the pieces that fit beside
+// each other that the larger tiles' rate does not pass their quicker beginning
+// and end.  us so and with 128 x 128: 1 group of 813 rows, 64 -> 256, 11 and 19;
+// 1 of 2,000, 1024 -> 1024 (1 piece), 41 and 50; 1 of 10,000, 512 -> 512 (4 of
+// 2,500), 50 and 57; 1 of 20,000 (4 of 5,000), 97 and 80.
 inline bool group_f32_deep_grad(int G, int64_t rows, int n, int k) {
   const int64_t tiles = (int64_t)((n + 63) / 64) * ((k + 63) / 64);
-  return tiles * G <= kCUs && tiles * rows <= 2560 * (int64_t)kCUs;
+  return tiles * G <= kCUs && rows <= 2560 * (kCUs / tiles);
 }
 hipError_t launch_group_f32_deep(int mode, const GroupArgs &a, hipStream_t s);
 

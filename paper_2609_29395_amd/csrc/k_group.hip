@@ -264,7 +264,8 @@ GroupPieces group_pieces(int dtype, int G, int64_t rows, int n, int k) {
   const bool deep = dtype == GCPSL_F32 && group_f32_deep_grad(G, rows, n, k);
   const int64_t tile = big ? 256 : deep ? 64 : 128, slots = big || deep ? kCUs : 2 * kCUs;
   const int64_t tiles = ((n + tile - 1) / tile) * ((k + tile - 1) / tile);
-  const int64_t even = tiles >= slots ? rows : rows * tiles / slots;
+  // (a CU holds one workgroup of the 64 x 64 kernel: no more of them than CUs)
+  const int64_t even = tiles >= slots ? rows : deep ? rows / (slots / tiles) : rows * tiles / slots;
   const double b_by_a = dtype == GCPSL_BF16 ? 4 : deep ? 0.5 : 1;
   const int64_t least =
       big ? 1024 : std::min<int64_t>(512, std::max<int64_t>(128, (int64_t)std::sqrt(b_by_a * (double)rows * (double)tiles)));
