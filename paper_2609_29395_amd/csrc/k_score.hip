@@ -550,10 +550,6 @@ struct Chunks {
 };
 template <typename T> constexpr int kLargeNV = sizeof(T) == 2 ? 8 : 16;
 constexpr int kSmallNV = 2;
-template <typename T> constexpr int kWaveNV = 4;  // rows that a wave holds: 4 vectors a lane
-// (Threads that held the most vectors whatever the row's length took, for 4,096
-// rows, 28.7 us where 6 suffice for 2,048 classes of fp32, and 7.7 for 100 of bf16
-// where 6.0 do now.)
 template <typename T> Chunks chunks_of(int64_t rows, int L, int top) {
   constexpr int64_t per = 256 * Bits<T>::VEC;
   const int64_t large = (L + per * kLargeNV<T> - 1) / (per * kLargeNV<T>);
@@ -561,10 +557,16 @@ template <typename T> Chunks chunks_of(int64_t rows, int L, int top) {
   if (rows * large >= 512 || (large == 1 && small > 1) || small * top > 64 * kHeld) return {true, large};
   return {false, small};
 }
-template <typename T> bool wave_rows(int L) { return L <= 64 * kWaveNV<T> * Bits<T>::VEC; }
+// Rows that one wave each takes: those it holds in 4 vectors a lane, and in 8
+// where there are rows enough for all SIMDs: us so and by four waves a row, 4,096
+// rows of 4,096 classes, bf16, 10.0 and 13.8, of 2,048, fp32, 8.1 and 12.6; 1,024
+// rows 6.5 and 6.3, 5.8 and 6.0.
+template <typename T> bool wave_rows(int64_t rows, int L) {
+  return L <= 64 * (rows >= 1024 ? 8 : 4) * Bits<T>::VEC;
+}
 
 template <typename T> size_t work_of(int64_t rows, int L, int top) {
-  if (wave_rows<T>(L)) return 0;
+  if (wave_rows<T>(rows, L)) return 0;
   const int64_t n = chunks_of<T>(rows, L, top).n;
   return n > 1 ? (size_t)rows * n * (16 + 8 * (size_t)top) : 0;
 }
@@ -574,7 +576,7 @@ template <typename T> hipError_t run(const ScoreArgs &a, hipStream_t s) {
     hipLaunchKernelGGL(score_small_kernel<T>, dim3((uint32_t)((a.rows + 15) / 16)), dim3(256), 0, s, a);
     return hipGetLastError();
   }
-  const bool wave = wave_rows<T>(a.L);
+  const bool wave = wave_rows<T>(a.rows, a.L);
   const Chunks ch = wave ? Chunks{false, 1} : chunks_of<T>(a.rows, a.L, a.top);
   const int64_t jobs = a.rows * ch.n;
   if (jobs > INT32_MAX) return hipErrorInvalidConfiguration;
@@ -582,12 +584,14 @@ template <typename T> hipError_t run(const ScoreArgs &a, hipStream_t s) {
   const auto launch = [&](auto kernel, uint32_t groups) {
     hipLaunchKernelGGL(kernel, dim3(groups), dim3(256), 0, s, a, n, make_fastdiv((uint32_t)ch.n));
   };
-  // a row that is not cut: as many vectors a thread as it needs
+  // a row that is not cut: as many vectors a thread as it needs (the most, always:
+  // 4,096 rows of 3,000 classes, fp32, 28 us where 15 do, of 100, bf16, 7.6 and 6.0)
   const int vectors = (a.L + Bits<T>::VEC - 1) / Bits<T>::VEC;
   if (wave) {
     if (vectors <= 64) launch(score_kernel<T, 64, 1>, (n + 3) / 4);
     else if (vectors <= 128) launch(score_kernel<T, 64, 2>, (n + 3) / 4);
-    else launch(score_kernel<T, 64, kWaveNV<T>>, (n + 3) / 4);
+    else if (vectors <= 256) launch(score_kernel<T, 64, 4>, (n + 3) / 4);
+    else launch(score_kernel<T, 64, 8>, (n + 3) / 4);
   } else if (ch.n > 1 ? !ch.large : vectors <= 256 * kSmallNV) {
     launch(score_kernel<T, 256, kSmallNV>, n);
   } else if (ch.n == 1 && vectors <= 1024) {
