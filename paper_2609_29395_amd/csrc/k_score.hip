@@ -31,6 +31,7 @@ typedef u32x4 u32x4_any __attribute__((aligned(2)));  // global memory takes 16-
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 __device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
 __device__ __forceinline__ float log_of(float s) { return __builtin_amdgcn_logf(s) * kLn2; }
+constexpr float kNear = 1048576.f;  // 2^20: maxima up to which differences come from products with log2e
 constexpr float kFar = -1e4f;  // e^kFar is 0: stands for any smaller difference where that is multiplied by e^d = 0
 
 // Largest of three values; a NaN may or may not show.
@@ -206,7 +207,10 @@ __global__ void __launch_bounds__(256, 4) score_kernel(ScoreArgs a, uint32_t job
   }
   // In units of log 2, d = x log2e - base log2e with the second product
   // rounded: what that rounding is off by (`off`) is the same for every
-  // element and is taken out of the sums.
+  // element and is taken out of the sums.  It is at most 2^-24 of the product,
+  // below 0.1 up to kNear; further out, from 10^9 on, 2^off would pass fp32's
+  // range.  (`base` is that of the wave: of a finite fill, where its classes
+  // are all ruled out.)
   Sums p{wave_max(lmax), 0.f, 0.f};
   const float base = base_of(p.m), prod = base * kLog2e, off = fmaf(base, kLog2e, -prod);
   float s2[2] = {0.f, 0.f}, t2[2] = {0.f, 0.f};
@@ -222,7 +226,7 @@ __global__ void __launch_bounds__(256, 4) score_kernel(ScoreArgs a, uint32_t job
   p.s = wave_sum(s2[0] + s2[1]);
   p.t = kLn2 * f * fmaf(-off, p.s, wave_sum(t2[0] + t2[1]));
   p.s *= f;
-  if (fabsf(base) > 1e37f) {  // the products pass fp32's range
+  if (fabsf(base) > kNear) {  // the difference first, which is exact near the maximum
     p.s = p.t = 0.f;
     for (int k = 0; k < NV * VEC; ++k) {  // the thread's own elements, again from memory
       const int i = i0 + k / VEC * TPR * VEC + k % VEC;
