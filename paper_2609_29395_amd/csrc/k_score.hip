@@ -20,6 +20,8 @@
 // 208 us (5.2 TB/s; reads alone reach 6.2).  One row of as many, top 20: 6 + 4.4
 // us in two kernels, launches and latency.  The gradient reads and writes once:
 // 4,096 x 50,021, fp32, 298 us (5.5 TB/s).
+#include <algorithm>
+
 #include "runtime.h"
 #include "ops.h"
 
@@ -575,16 +577,13 @@ template <typename T> size_t work_of(int64_t rows, int L, int top) {
   return n > 1 ? (size_t)rows * n * (16 + 8 * (size_t)top) : 0;
 }
 
-template <typename T> hipError_t run(const ScoreArgs &a, hipStream_t s) {
+// Rows of one launch; `wave` and `ch` are chosen by all the rows of the call.
+template <typename T> hipError_t run_rows(const ScoreArgs &a, bool wave, const Chunks &ch, hipStream_t s) {
   if (a.L <= 64) {
     hipLaunchKernelGGL(score_small_kernel<T>, dim3((uint32_t)((a.rows + 15) / 16)), dim3(256), 0, s, a);
     return hipGetLastError();
   }
-  const bool wave = wave_rows<T>(a.rows, a.L);
-  const Chunks ch = wave ? Chunks{false, 1} : chunks_of<T>(a.rows, a.L, a.top);
-  const int64_t jobs = a.rows * ch.n;
-  if (jobs > INT32_MAX) return hipErrorInvalidConfiguration;
-  const uint32_t n = (uint32_t)jobs;
+  const uint32_t n = (uint32_t)(a.rows * ch.n);
   const auto launch = [&](auto kernel, uint32_t groups) {
     hipLaunchKernelGGL(kernel, dim3(groups), dim3(256), 0, s, a, n, make_fastdiv((uint32_t)ch.n));
   };
@@ -612,13 +611,48 @@ template <typename T> hipError_t run(const ScoreArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// p's entry r, or null.
+template <typename P> P *entry_at(P *p, int64_t r) { return p ? p + r : nullptr; }
+
+template <typename T> hipError_t run(const ScoreArgs &a, hipStream_t s) {
+  const bool wave = wave_rows<T>(a.rows, a.L);
+  const Chunks ch = wave || a.L <= 64 ? Chunks{false, 1} : chunks_of<T>(a.rows, a.L, a.top);
+  const int64_t slab = kMaxBlocks / ch.n;  // (launches of less than a workgroup a row would hold more)
+  for (int64_t r = 0; r < a.rows; r += slab) {
+    ScoreArgs b = a;
+    b.z = (const T *)a.z + r * a.ldz;
+    b.rows = std::min(slab, a.rows - r);
+    b.labels = entry_at(a.labels, r);
+    b.logp = entry_at(a.logp, r);
+    b.entropy = entry_at(a.entropy, r);
+    b.lse = entry_at(a.lse, r);
+    b.top_logp = entry_at(a.top_logp, r * a.top);
+    b.top_class = entry_at(a.top_class, r * a.top);
+    const hipError_t e = run_rows<T>(b, wave, ch, s);  // (one after another on the stream: the workspace serves each)
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 template <typename T> hipError_t run_grad(const ScoreGradArgs &a, hipStream_t s) {
   constexpr int NV = 4;
-  const int64_t per = 256 * NV * Bits<T>::VEC, n = (a.L + per - 1) / per;
-  if (a.rows * n > INT32_MAX) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL((score_grad_kernel<T, NV>), dim3((uint32_t)(a.rows * n)), dim3(256), 0, s, a,
-                     make_fastdiv((uint32_t)n));
-  return hipGetLastError();
+  const int64_t per = 256 * NV * Bits<T>::VEC, n = (a.L + per - 1) / per, slab = kMaxBlocks / n;
+  for (int64_t r = 0; r < a.rows; r += slab) {
+    ScoreGradArgs b = a;
+    b.z = (const T *)a.z + r * a.ldz;
+    b.rows = std::min(slab, a.rows - r);
+    b.labels = entry_at(a.labels, r);
+    b.lse = a.lse + r;
+    b.entropy = entry_at(a.entropy, r);
+    b.g_logp = entry_at(a.g_logp, r);
+    b.g_entropy = entry_at(a.g_entropy, r);
+    b.dz = (T *)a.dz + r * a.lddz;
+    hipLaunchKernelGGL((score_grad_kernel<T, NV>), dim3((uint32_t)(b.rows * n)), dim3(256), 0, s, b,
+                       make_fastdiv((uint32_t)n));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace

@@ -8,6 +8,10 @@
 #include "common.h"
 #include "rng.h"
 
+// Workgroups of 256 threads that one launch may have.  A launch has fewer than
+// 2^32 threads: the runtime takes their number modulo that, without an error.
+constexpr int64_t kMaxBlocks = ((int64_t)1 << 32) / 256 - 1;
+
 // ---------------------------------------------------------------- dropout
 // Threshold and factor of a dropout probability: an element is kept when its
 // 16-bit draw is at least `thr`, which has probability 1 - thr / 65536.
