@@ -452,8 +452,9 @@ int gcpsl_timing_read(gcpsl_ctx *ctx, gcpsl_kernel_stat *out, int32_t cap, int32
  * overlap inputs unless said otherwise.  Every call is asynchronous on
  * `stream`, allocates nothing and reads nothing on the host but its
  * arguments, so that it may be captured in a graph.  No rows is a valid
- * call.  EINVAL on a bad argument, EUNSUPPORTED where one launch would need
- * more than 2^31 workgroups, EHIP on a failed launch.
+ * call.  EINVAL on a bad argument, EHIP on a failed launch, EUNSUPPORTED where
+ * a grouped product's one launch would need 2^32 threads (256 or 512 for every
+ * tile that any offsets can make).
  *
  * Grouped rows: offsets is a device array [G + 1], 1 <= G <= 1024; rows
  * [offsets[g], offsets[g + 1]) belong to group g, 0 <= offsets[0] <= ... <=

@@ -212,12 +212,12 @@ hipError_t launch_any(int mode, const GroupArgs &a, hipStream_t s) {
   const int NT = (a.N + 63) / 64;
   if (mode == GROUP_DW) {
     const int64_t blocks = piece_blocks(a, (int64_t)((a.M + 63) / 64) * NT);
-    if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (blocks > kMaxBlocks) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((group_any_kernel<T, GROUP_DW>), dim3((uint32_t)blocks), dim3(256), 0, s, a, NT);
     return hipGetLastError();
   }
   const int64_t blocks = tile_blocks(a.M, a.G, 64, NT);
-  if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
+  if (blocks > kMaxBlocks) return hipErrorInvalidConfiguration;
   if (mode == GROUP_FWD)
     hipLaunchKernelGGL((group_any_kernel<T, GROUP_FWD>), dim3((uint32_t)blocks), dim3(256), 0, s, a, NT);
   else

@@ -320,7 +320,7 @@ template <int MODE> hipError_t run_mode(const GroupArgs &a, hipStream_t s) {
   const int64_t NT = (a.N + BN - 1) / BN;
   const int64_t blocks = MODE == GROUP_DW ? piece_blocks(a, (int64_t)((a.M + BM - 1) / BM) * NT)
                                           : tile_blocks(a.M, a.G, BM, NT);
-  if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
+  if (blocks > kMaxBlocks) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(group_f32_kernel<MODE>, dim3((uint32_t)blocks), dim3(256), 0, s, a, (int)NT);
   return hipGetLastError();
 }

@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(64 * WAVES) group_few_kernel(GroupArgs a, int 
 
 template <typename T, int MODE, int FR, int FC> hipError_t run(const GroupArgs &a, hipStream_t s) {
   const int64_t NT = (a.N + 16 * FC - 1) / (16 * FC), blocks = tile_blocks(a.M, a.G, 16 * FR, NT);
-  if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
+  if (blocks > kMaxBlocks) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((group_few_kernel<T, MODE, FR, FC>), dim3((uint32_t)blocks), dim3(64 * WAVES), 0, s, a, (int)NT);
   return hipGetLastError();
 }

@@ -284,7 +284,7 @@ template <int MODE, int BM> hipError_t run_tiles(const GroupArgs &a, hipStream_t
   const int64_t NT = (a.N + BN - 1) / BN;
   const int64_t blocks = MODE == GROUP_DW ? piece_blocks(a, (int64_t)((a.M + BM - 1) / BM) * NT)
                                           : tile_blocks(a.M, a.G, BM, NT);
-  if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
+  if (blocks > kMaxBlocks) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((group_mid_kernel<MODE, BM>), dim3((uint32_t)blocks), dim3(256), 0, s, a, (int)NT);
   return hipGetLastError();
 }

@@ -463,7 +463,7 @@ template <int MODE> hipError_t run(const GroupArgs &a, hipStream_t s) {
   const int64_t NT = (a.N + BN - 1) / BN;
   const int64_t blocks = MODE == GROUP_DW ? piece_blocks(a, (int64_t)((a.M + BM - 1) / BM) * NT)
                                           : tile_blocks(a.M, a.G, BM, NT);
-  if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
+  if (blocks > kMaxBlocks / 2) return hipErrorInvalidConfiguration;  // (of 512 threads)
   hipLaunchKernelGGL(group_tile_kernel<MODE>, dim3((uint32_t)blocks), dim3(512), LDS_BYTES, s, a, (int)NT);
   return hipGetLastError();
 }
