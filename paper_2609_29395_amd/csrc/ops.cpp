@@ -29,6 +29,9 @@ int launched(hipError_t e) noexcept {
 }
 
 constexpr int64_t kMaxRows = INT32_MAX, kMaxLd = INT32_MAX, kMaxStride = (int64_t)1 << 40;
+// Grouped rows: a row of the last tile (256 rows at most), or a group's rows and
+// the pieces that they are cut into (513 at most), stay below 2^31 in sum.
+constexpr int64_t kMaxGroupRows = ((int64_t)1 << 31) - 1024;
 constexpr int kMaxGroups = 1024, kMaxCols = 1 << 28;  // column counters and their tile sums stay below 2^31
 
 bool is_type(int dtype) { return dtype == GCPSL_F32 || dtype == GCPSL_BF16; }
@@ -69,6 +72,12 @@ const char *bad_stride(int64_t s) { return s < 0 || s > kMaxStride ? "group stri
     if (const char *why_ = (expr)) return fail(GCPSL_EINVAL, why_); \
   } while (0)
 
+#define CHECK_GROUPS(...)                                                                            \
+  do {                                                                                               \
+    CHECK(bad_groups(__VA_ARGS__));                                                                  \
+    if (rows > kMaxGroupRows) return fail(GCPSL_EUNSUPPORTED, "more than 2^31 - 1024 grouped rows"); \
+  } while (0)
+
 }  // namespace
 
 extern "C" int gcpsl_group_forward(int32_t dtype, int32_t G, int64_t rows, int32_t n, int32_t k,
@@ -76,7 +85,7 @@ extern "C" int gcpsl_group_forward(int32_t dtype, int32_t G, int64_t rows, int32
                                    const float *bias, int64_t bias_gs, int32_t relu, double p, uint64_t seed, void *y,
                                    int64_t ldy, void *stream) {
   gcpsl_clear_error();
-  CHECK(bad_groups(dtype, G, rows, n, k, offsets));
+  CHECK_GROUPS(dtype, G, rows, n, k, offsets);
   const size_t e = elem_bytes(dtype);
   CHECK(bad_tensor(x, e, rows, k, ldx, false));
   CHECK(bad_tensor(w, e, G, k, k, false));
@@ -102,7 +111,7 @@ extern "C" int gcpsl_group_input_grad(int32_t dtype, int32_t G, int64_t rows, in
                                       int64_t w_gs, const void *gate, int64_t ldgate, double p, void *dx, int64_t lddx,
                                       void *stream) {
   gcpsl_clear_error();
-  CHECK(bad_groups(dtype, G, rows, n, k, offsets));
+  CHECK_GROUPS(dtype, G, rows, n, k, offsets);
   const size_t e = elem_bytes(dtype);
   CHECK(bad_tensor(dy, e, rows, n, lddy, false));
   CHECK(bad_tensor(w, e, G, k, k, false));
@@ -132,7 +141,7 @@ extern "C" int gcpsl_group_workspace_bytes(int32_t dtype, int32_t G, int64_t row
   gcpsl_clear_error();
   if (!bytes) return fail(GCPSL_EINVAL, "null output");
   alignas(4) static const int32_t none = 0;
-  CHECK(bad_groups(dtype, G, rows, n, k, &none));
+  CHECK_GROUPS(dtype, G, rows, n, k, &none);
   *bytes = partial_bytes(group_pieces(dtype, G, rows, n, k), n, k);
   return GCPSL_OK;
 }
@@ -142,7 +151,7 @@ extern "C" int gcpsl_group_weight_grad(int32_t dtype, int32_t G, int64_t rows, i
                                        int64_t ldx, float *dw, int64_t dw_gs, float *db, int64_t db_gs,
                                        void *workspace, size_t workspace_bytes, void *stream) {
   gcpsl_clear_error();
-  CHECK(bad_groups(dtype, G, rows, n, k, offsets));
+  CHECK_GROUPS(dtype, G, rows, n, k, offsets);
   const size_t e = elem_bytes(dtype);
   CHECK(bad_tensor(dy, e, rows, n, lddy, false));
   CHECK(bad_tensor(x, e, rows, k, ldx, false));

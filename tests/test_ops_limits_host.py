@@ -1,7 +1,9 @@
 """The largest calls of the operators on caller-owned tensors, refused on the host (no GPU needed)."""
+import ctypes as C
+
 import pytest
 
-from test_ops_host import FORWARD, INPUT, WEIGHT, built, call, g
+from test_ops_host import FAR, FORWARD, INPUT, WEIGHT, built, call, g
 
 
 # The launch's threads pass 2^32, which the runtime would take modulo that: tiles of 64 x 64 by 256 threads (fp32 rows of
@@ -16,3 +18,17 @@ from test_ops_host import FORWARD, INPUT, WEIGHT, built, call, g
 ])
 def test_launches_of_too_many_threads(name, good, change):
     assert call(name, good, **change) == g.EUNSUPPORTED
+
+
+# The last rows of such tensors would pass 2^31 in a tile's or a piece's row numbers.
+@built
+@pytest.mark.parametrize("rows", [2 ** 31 - 1023, 2 ** 31 - 1])
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_grouped_rows_next_to_two_to_the_31st(rows, dtype):
+    size = C.c_size_t()
+    assert call("gcpsl_group_forward", FORWARD, dtype=dtype, rows=rows, n=1, k=1, ldx=0, ldy=1) == g.EUNSUPPORTED
+    assert call("gcpsl_group_input_grad", INPUT, dtype=dtype, rows=rows, n=1, k=1, lddy=0, lddx=1) == g.EUNSUPPORTED
+    assert call("gcpsl_group_weight_grad", WEIGHT, dtype=dtype, rows=rows, n=1, k=1, lddy=0, ldx=0, workspace=FAR,
+                workspace_bytes=1 << 30) == g.EUNSUPPORTED
+    assert g.lib().gcpsl_group_workspace_bytes(dtype, 2, rows, 1, 1, C.byref(size)) == g.EUNSUPPORTED
+    assert g.lib().gcpsl_group_workspace_bytes(dtype, 2, 2 ** 31 - 1024, 1, 1, C.byref(size)) == g.OK and size.value > 0
