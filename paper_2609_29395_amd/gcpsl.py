@@ -190,8 +190,11 @@ def fuse_replicas(theta, weights, stream=None):
 #
 # Tensors are on the current GPU, rows of consecutive elements (any row
 # stride).  Every function returns the tensors it wrote: those given as out,
-# dw, db, or new ones.  stream: a torch stream, the current one by default;
-# what is newly allocated for another stream is marked as used there.
+# dw, db, or new ones.  stream: a torch stream, the current one by default.
+# What is newly allocated for another stream comes from that stream's memory and
+# is marked as used on the current one too; as with any work of two streams, the
+# caller makes `stream` wait for inputs made elsewhere, and whoever reads the
+# results wait for `stream`.
 #
 # The smallest calls are bound by the host.  A call on the current stream that
 # brings no workspace goes through csrc/bind.cpp in one native call, which
@@ -249,9 +252,12 @@ def _begin(t, stream):
 
 
 def _empty(like, shape, dtype, stream):
-    t = like.new_empty(*shape, dtype=dtype)
-    if stream is not None:
-        t.record_stream(stream)
+    if stream is None:
+        return like.new_empty(*shape, dtype=dtype)
+    # from that stream's memory: a block freed on the current stream may still be in use by work queued there
+    with _torch.cuda.stream(stream):
+        t = like.new_empty(*shape, dtype=dtype)
+    t.record_stream(_torch.cuda.current_stream(t.device))  # where the caller may go on with it
     return t
 
 
