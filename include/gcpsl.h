@@ -533,9 +533,11 @@ int gcpsl_score(int32_t dtype, int64_t rows, int32_t L, const void *z, int64_t l
  * loss's gradients by logp and entropy (either may be NULL),
  *   dz_c = g_logp (1[c = y] - p_c) - g_entropy p_c (log p_c + entropy),
  * p_c = exp(z_c - lse), lse and entropy as gcpsl_score gave them (entropy
- * only where g_entropy is given).  A row without a label takes no gradient
- * from logp.  A row whose lse is below -1e30, all its classes ruled out by
- * -inf or the type's lowest values, has gradient 0.  dz may be z (lddz = ldz).
+ * only where g_entropy is given); lse's rounding makes p_c off by up to 2^-24
+ * |lse| of itself.  A row without a label takes no gradient from logp.  A row
+ * whose lse is -2^23 (-8388608) or less has gradient 0: all its classes are
+ * ruled out, by -inf or by a finite value, and lse no longer holds how many.
+ * dz may be z (lddz = ldz).
  */
 int gcpsl_score_grad(int32_t dtype, int64_t rows, int32_t L, const void *z, int64_t ldz, const int32_t *labels,
                      const float *lse, const float *entropy, const float *g_logp, const float *g_entropy, void *dz,

@@ -494,6 +494,11 @@ __global__ void __launch_bounds__(256) score_small_kernel(ScoreArgs a) {
     if (live && i * 16 + lane < a.L && above[i] < a.top) write_top(a, row, above[i], key[i], r);
 }
 
+// A row's lse from which on its classes count as ruled out: -2^23, where fp32's
+// steps are 1 and lse no longer holds the logarithm of how many share it, so that
+// z - lse would make e^0 of every class.
+constexpr float kRuledOut = -8388608.f;
+
 // dz: NV 16-byte vectors a thread, chunks of 256 NV vectors of a row.
 template <typename T, int NV>
 __global__ void __launch_bounds__(256) score_grad_kernel(ScoreGradArgs a, FastDiv fd_chunks) {
@@ -515,7 +520,7 @@ __global__ void __launch_bounds__(256) score_grad_kernel(ScoreGradArgs a, FastDi
   const int y = a.g_logp ? a.labels[row] : -1;
   const float gl = (unsigned)y < (unsigned)L ? a.g_logp[row] : 0.f;
   const float gh = a.g_entropy ? a.g_entropy[row] : 0.f, H = a.g_entropy ? a.entropy[row] : 0.f;
-  const bool empty = lse < -1e30f;
+  const bool empty = lse <= kRuledOut;
   const float g0 = -gl - gh * H;  // dz = p (g0 - gh log p) off the label
   const auto grad = [&](float x, int i) {
     if (empty) return 0.f;
