@@ -109,7 +109,12 @@ __global__ void __launch_bounds__(256) group_any_kernel(GroupArgs a, int NT) {
           K::mma(acc[i][j], lb + (wn * 32 + i * 16 + li) * LD + k + lg * K::PER,
                  la + (wm * 32 + j * 16 + li) * LD + k + lg * K::PER);
     if (MODE == GROUP_DW && tid < BM)
-      for (int i = 0; i < BQ; ++i) rowsum += ElemT<T>::to_f(la[tid * LD + i]);
+      for (int i = 0; i < BQ; i += 8) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = ElemT<T>::to_f(la[tid * LD + i + j]);
+        rowsum += sum8(v);
+      }
   }
 
   // lane (li, lg) holds columns 4 lg .. 4 lg + 3 of row li of each fragment

@@ -154,9 +154,7 @@ __device__ __forceinline__ void group_f32_tile(const GroupArgs &a, const Tile &t
       if constexpr (MODE == GROUP_DW) {
         if (sums && is_a) {
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) colsum[j] += stage.v[j][i];
+          for (int j = 0; j < 2; ++j) colsum[j] += sum8(stage.v[j]);
         }
       }
     };

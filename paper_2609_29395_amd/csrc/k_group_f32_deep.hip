@@ -96,9 +96,7 @@ template <bool T> struct Stage {
   // T: the sums of the thread's two columns in a set
   __device__ __forceinline__ void sum(int set, float (&s)[2]) const {
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s[j] += v[set][j][i];
+    for (int j = 0; j < 2; ++j) s[j] += sum8(v[set][j]);
   }
   // splits the values and writes them; returns the largest magnitude so far
   __device__ __forceinline__ float write(char *planes, int set, float top) const {
