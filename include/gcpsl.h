@@ -448,7 +448,10 @@ int gcpsl_timing_read(gcpsl_ctx *ctx, gcpsl_kernel_stat *out, int32_t cap, int32
  * row's elements are consecutive and any element alignment will do (16-byte
  * aligned rows are read fastest).  dtype GCPSL_F32 or GCPSL_BF16 is the type
  * of the activations and weights; biases, weight gradients and scores are
- * fp32, and so are all sums; a result is rounded once.  Outputs must not
+ * fp32, and so are all sums; a result is rounded once.  (fp32 products may be
+ * taken from three bf16 parts of every value, which hold all its bits down to
+ * 2^-110 and steps of 2^-133 below: whether they are goes by the call's sizes
+ * and strides.)  Outputs must not
  * overlap inputs unless said otherwise.  Every call is asynchronous on
  * `stream`, allocates nothing and reads nothing on the host but its
  * arguments, so that it may be captured in a graph.  No rows is a valid
