@@ -495,10 +495,12 @@ int gcpsl_group_input_grad(int32_t dtype, int32_t G, int64_t rows, int32_t n, in
 /* dW_g = sum over the rows r of group g of dy_r x_r^T, [n][k] fp32 at dw + g
  * dw_gs; db_g = sum of dy_r, [n] at db + g db_gs (db may be NULL); both zero
  * for a group without rows (dw_gs >= n k and db_gs >= n if G > 1).  The
- * summation order depends on G, rows, n, k and the group's count only: the
- * same call gives the same bits.  workspace: gcpsl_group_workspace_bytes()
- * bytes on the device, 16-byte aligned (NULL if that is 0), used until the
- * call's work on the stream is done. */
+ * summation order depends on dtype, G, rows, n, k, the group's count, the
+ * operands' row strides and alignment, and in fp32 on whether a value of a tile
+ * reaches 2^50: the same call gives the same bits, equal values in another
+ * layout may not.  workspace: gcpsl_group_workspace_bytes() bytes on the device,
+ * 16-byte aligned (NULL if that is 0), used until the call's work on the stream
+ * is done. */
 int gcpsl_group_workspace_bytes(int32_t dtype, int32_t G, int64_t rows, int32_t n, int32_t k, size_t *bytes);
 int gcpsl_group_weight_grad(int32_t dtype, int32_t G, int64_t rows, int32_t n, int32_t k, const int32_t *offsets,
                             const void *dy, int64_t lddy, const void *x, int64_t ldx, float *dw, int64_t dw_gs,
