@@ -196,6 +196,10 @@ def fuse_replicas(theta, weights, stream=None):
 # caller makes `stream` wait for inputs made elsewhere, and whoever reads the
 # results wait for `stream`.
 #
+# Autograd does not see these calls: tensors that require a gradient are taken as
+# plain ones, results never require one, and what is written (out, dw, db) does
+# not count as changed.  The backward passes are the functions for them here.
+#
 # The smallest calls are bound by the host.  A call on the current stream that
 # brings no workspace goes through csrc/bind.cpp in one native call, which
 # checks, allocates and launches; what that does not take (it answers None) and
