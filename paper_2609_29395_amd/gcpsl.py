@@ -256,12 +256,13 @@ def _begin(t, stream):
 
 
 def _empty(like, shape, dtype, stream):
-    if stream is None:
+    current = None if stream is None else _torch.cuda.current_stream(like.device)
+    if stream == current:
         return like.new_empty(*shape, dtype=dtype)
     # from that stream's memory: a block freed on the current stream may still be in use by work queued there
     with _torch.cuda.stream(stream):
         t = like.new_empty(*shape, dtype=dtype)
-    t.record_stream(_torch.cuda.current_stream(t.device))  # where the caller may go on with it
+    t.record_stream(current)  # where the caller may go on with it
     return t
 
 
