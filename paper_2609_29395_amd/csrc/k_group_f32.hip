@@ -11,10 +11,13 @@
 // Two 24 KB buffers; two workgroups share a CU and one's splitting overlaps the
 // other's MFMAs.
 //
-// Bound: the matrix cores (six bf16 products, 415 TFLOP/s at most).  8 groups of
-// 1,024 rows, 1024 -> 1024: forward 96 to 100 us (171 to 179 TFLOP/s; fp32 MFMAs
-// have a peak of 157), input gradient 97, weight gradient 105.  A workgroup
-// alone on its CU takes 0.6 us a k tile where its MFMAs take 0.35.
+// Bound: what a k tile costs beside its MFMAs, which the matrix cores are busy
+// with 32 to 35 % of a launch: every value is split by each tile that reads it,
+// and every 16 of the sum take fragment reads and a barrier.  8 groups of 1,024
+// rows, 1024 -> 1024: forward 96 to 100 us (171 to 179 TFLOP/s, 42 % of what six
+// bf16 products allow; fp32 MFMAs have a peak of 157), input gradient 97, weight
+// gradient 105.  A workgroup alone on its CU takes 0.6 us a k tile where its
+// MFMAs take 0.35.
 #include "group_f32.h"
 
 namespace {

@@ -19,7 +19,8 @@
 // Bound: reading the logits.  4,096 rows of 131,072 classes, bf16, top 8: 203 to
 // 208 us (5.2 TB/s; reads alone reach 6.2).  One row of as many, top 20: 6 + 4.4
 // us in two kernels, launches and latency.  The gradient reads and writes once:
-// 4,096 x 50,021, fp32, 298 us (5.5 TB/s).
+// 4,096 x 50,021, fp32, 298 us (5.5 TB/s), bf16 143 (5.7).  Its short rows are
+// bound by workgroups, one or more a row: 65,536 x 10, fp32, 49 us, bf16 43.
 #include <algorithm>
 
 #include "runtime.h"
