@@ -193,8 +193,9 @@ def fuse_replicas(theta, weights, stream=None):
 # dw, db, or new ones.  stream: a torch stream, the current one by default.
 # What is newly allocated for another stream comes from that stream's memory and
 # is marked as used on the current one too; as with any work of two streams, the
-# caller makes `stream` wait for inputs made elsewhere, and whoever reads the
-# results wait for `stream`.
+# caller makes `stream` wait for inputs made elsewhere, keeps them until it is
+# done with them (or marks them as used there: Tensor.record_stream), and makes
+# whoever reads the results wait for `stream`.
 #
 # Autograd does not see these calls: tensors that require a gradient are taken as
 # plain ones, results never require one, and what is written (out, dw, db) does
