@@ -303,7 +303,7 @@ def _own(s):
                                                w_next=s["w_next"], alpha=_ALPHA, beta=_BETA, eps=_EPS))
     if s["do"] == "norm_grad":
         return tuple(gcpsl.group_residual_norm_grad(
-            s["x"], s["offsets"], dx=s["dx"], dh=s["dh"], y=s["y"], gate=s["gate"], w_block=s["w_block"],
+            s["x"], s["offsets"], g_out=s["dx"], g_h=s["dh"], y=s["y"], gate=s["gate"], w_block=s["w_block"],
             w_next=s["w_next"], r_block=s["r_block"], r_next=s["r_next"], alpha=_ALPHA, beta=_BETA))
     if s["do"] == "distill":
         r = gcpsl.distill(s["z"], s["t_class"], s["t_value"], temperature=s["temperature"], labels=s["y"])
