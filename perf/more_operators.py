@@ -339,7 +339,7 @@ def work(case):
 # ----------------------------------------------------- 64-bit definitions
 
 def _phi(g):
-    return torch.special.ndtr(g)
+    return torch.erfc(g / -math.sqrt(2)) / 2  # (special.ndtr takes 1 + erf, which loses the lower tail)
 
 
 def _exact_act(g, name):
