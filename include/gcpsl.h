@@ -54,6 +54,11 @@ extern "C" {
 #define GCPSL_F32 0  /* fp32 activations and weights                        */
 #define GCPSL_BF16 1 /* bf16 activations and weights, fp32 master weights   */
 
+/* Activations of gated layers (gcpsl_group_gated_forward). */
+#define GCPSL_SILU 0 /* f(g) = g / (1 + e^-g)                               */
+#define GCPSL_GELU 1 /* f(g) = g Phi(g), Phi the normal distribution        */
+#define GCPSL_RELU 2 /* f(g) = max(g, 0), f' = 0 at 0                       */
+
 /* Round schedules (Sec. III-A, Sec. IV-D). */
 #define GCPSL_SCHED_LOCKSTEP 0 /* every cluster takes one local round per step  */
 #define GCPSL_SCHED_EPOCH 1    /* epoch barrier: a cluster takes floor(n_n/B)
@@ -439,7 +444,8 @@ int gcpsl_timing_read(gcpsl_ctx *ctx, gcpsl_kernel_stat *out, int32_t cap, int32
 
 /*
  * Operators on caller-owned tensors, without a context: layers over rows
- * grouped by cluster, dropout and label scores.  They serve what surrounds a
+ * grouped by cluster, residual updates with norms, dropout, label scores and
+ * distillation.  They serve what surrounds a
  * round and has no fixed batch: evaluating the fused model, or training one
  * layer per cluster, on all n_n examples of every cluster at once.
  *
@@ -506,6 +512,79 @@ int gcpsl_group_weight_grad(int32_t dtype, int32_t G, int64_t rows, int32_t n, i
                             const void *dy, int64_t lddy, const void *x, int64_t ldx, float *dw, int64_t dw_gs,
                             float *db, int64_t db_gs, void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * Gated layer over grouped rows: (g_r, u_r) = W_g x_r + b_g and y_r = f(g_r) u_r
+ * for every row r of every group g: x [rows][k], y [rows][n].  W_g is [2 n][k],
+ * the gates' n rows and then the values', at w + g w_gs; b_g is [2 n] at bias +
+ * g bias_gs (bias may be NULL).  act: GCPSL_SILU, GCPSL_GELU or GCPSL_RELU is f
+ * (a NaN passes through each).  pre [rows][2 n], if not NULL, receives the pairs
+ * (g_r | u_r), rounded; y comes from them unrounded.  1 <= n <= 2^27.
+ */
+int gcpsl_group_gated_forward(int32_t dtype, int32_t G, int64_t rows, int32_t n, int32_t k, const int32_t *offsets,
+                              const void *x, int64_t ldx, const void *w, int64_t w_gs, const float *bias,
+                              int64_t bias_gs, int32_t act, void *y, int64_t ldy, void *pre, int64_t ldpre,
+                              void *stream);
+
+/*
+ * Gradient of a gated layer's pairs through the layer z_r = V_g y_r after it: dh_r
+ * = V_g^T dz_r and dpre_r = (f'(g_r) u_r dh_r | f(g_r) dh_r): dz [rows][m], V_g
+ * [m][n] at v + g v_gs, pre and dpre [rows][2 n].  What dz is scaled by, a dropout
+ * say, is the caller's.  The gradients of the gated layer's input, weights and
+ * bias are those of a layer of 2 n outputs: gcpsl_group_input_grad and
+ * gcpsl_group_weight_grad on dpre.
+ */
+int gcpsl_group_gated_grad(int32_t dtype, int32_t G, int64_t rows, int32_t m, int32_t n, const int32_t *offsets,
+                           const void *dz, int64_t lddz, const void *v, int64_t v_gs, int32_t act, const void *pre,
+                           int64_t ldpre, void *dpre, int64_t lddpre, void *stream);
+
+/*
+ * Residual update of grouped rows by a block's output, with the norm after the
+ * block, the block's gate and the norm before the next block: for every row r of
+ * every group g, element by element,
+ *   out = alpha x + beta sigmoid(gate) t,  t = w_block_g y r_block,
+ *   h   = w_next_g out r_next,             r_v = 1 / sqrt(mean(v^2) + eps),
+ * r_block of y's row and r_next of out's before its rounding.  x, y, gate, out, h
+ * are [rows][n]; w_block and w_next [n] fp32 at + g w_block_gs and + g w_next_gs
+ * (a stride of 0 gives every group the same one); r_block and r_next [rows] fp32,
+ * either may be NULL.  gate NULL: no gate (1).  w_block NULL: no norm after the
+ * block, t = y, r_block not written.  w_next and h NULL, together: no norm before
+ * the next block, r_next not written.  y NULL: the norm alone, out = x, not
+ * written: gate, w_block and out NULL and alpha 1.  out may be x (ldo = ldx).
+ * alpha and beta are finite, 2^-100 <= eps <= 2^100; 1 <= n <= 2^28.  Squares are
+ * summed in fp32: a row with values of 2^63 or more may have r = 0.
+ */
+int gcpsl_group_residual_norm(int32_t dtype, int32_t G, int64_t rows, int32_t n, const int32_t *offsets, const void *x,
+                              int64_t ldx, const void *y, int64_t ldy, const void *gate, int64_t ldgate,
+                              const float *w_block, int64_t w_block_gs, const float *w_next, int64_t w_next_gs,
+                              double alpha, double beta, double eps, void *out, int64_t ldo, void *h, int64_t ldh,
+                              float *r_block, float *r_next, void *stream);
+
+/*
+ * Its gradients: with g_out and g_h [rows][n] the loss's gradients by out and by h
+ * (either may be NULL; g_h comes with w_next and r_next, and only then),
+ *   D  = g_out + r_next (a - o mean(a o)),  a = w_next_g g_h, o = out r_next
+ *   dx = alpha D,  dgate = beta D t s (1 - s),  s = sigmoid(gate)
+ *   dy = r_block (c - v mean(c v)),  c = beta D s w_block_g, v = y r_block
+ * (dy = beta D s without w_block), and dw_block_g = sum beta D s v, dw_next_g =
+ * sum g_h o over the rows of group g, fp32 [n] at + g dw_block_gs and + g
+ * dw_next_gs (>= n if G > 1), zero for a group without rows.  out, y, gate and the
+ * weights as the forward call had or gave them, r_block and r_next as it gave
+ * them; out is needed with g_h only.  dx is always given, dy where y is; dgate,
+ * dw_block and dw_next may be NULL.  The summation order of the weights'
+ * gradients depends on G, rows, n and the group's count.  workspace:
+ * gcpsl_group_residual_workspace_bytes() bytes on the device, 16-byte aligned
+ * (NULL if that is 0), used until the call's work on the stream is done.
+ */
+int gcpsl_group_residual_workspace_bytes(int32_t dtype, int32_t G, int64_t rows, int32_t n, size_t *bytes);
+int gcpsl_group_residual_norm_grad(int32_t dtype, int32_t G, int64_t rows, int32_t n, const int32_t *offsets,
+                                   const void *out, int64_t ldo, const void *g_out, int64_t ldgo, const void *g_h,
+                                   int64_t ldgh, const void *y, int64_t ldy, const void *gate, int64_t ldgate,
+                                   const float *w_block, int64_t w_block_gs, const float *w_next, int64_t w_next_gs,
+                                   const float *r_block, const float *r_next, double alpha, double beta, void *dx,
+                                   int64_t lddx, void *dy, int64_t lddy, void *dgate, int64_t lddgate, float *dw_block,
+                                   int64_t dw_block_gs, float *dw_next, int64_t dw_next_gs, void *workspace,
+                                   size_t workspace_bytes, void *stream);
+
 /* y = dropout(x), both [rows][cols], cols <= 2^28; y may be x (ldy = ldx).  The gradient
  * is the same call on dy with the same seed. */
 int gcpsl_dropout(int32_t dtype, int64_t rows, int64_t cols, const void *x, int64_t ldx, double p, uint64_t seed,
@@ -547,6 +626,43 @@ int gcpsl_score(int32_t dtype, int64_t rows, int32_t L, const void *z, int64_t l
 int gcpsl_score_grad(int32_t dtype, int64_t rows, int32_t L, const void *z, int64_t ldz, const int32_t *labels,
                      const float *lse, const float *entropy, const float *g_logp, const float *g_entropy, void *dz,
                      int64_t lddz, void *stream);
+
+/*
+ * Distillation of rows of logits z [rows][L] from a teacher's `top` best classes,
+ * t_class [rows][top] and their logits or log probabilities t_value (what
+ * gcpsl_score gives as top_class and top_logp), at a temperature T: with q =
+ * softmax(t_value / T) over the row's `top` entries and p = softmax(z / T),
+ *   kl    sum_k q_k (log q_k - log p_k), p_k that of class t_class[k]
+ *   lse_t log sum_c exp(z_c / T)
+ * and, as gcpsl_score has them, logp of the row's label and lse (T = 1).  Entries
+ * of a class outside [0, L) are left out, as are those of value -inf; a row
+ * without any left has kl 0.  A class given twice counts with both entries.  A
+ * class that the row rules out (-inf) and the teacher does not makes kl +inf, a
+ * NaN or +inf among a row's logits or the entries left makes it NaN.  1 <= top
+ * <= 256, 2^-10 <= T <= 2^10, 1 <= L <= 2^28.  kl, lse_t, logp and lse may be NULL
+ * (labels too if logp is).  workspace: gcpsl_distill_workspace_bytes() bytes on
+ * the device, 16-byte aligned (NULL if that is 0), used until the call's work on
+ * the stream is done.
+ */
+int gcpsl_distill_workspace_bytes(int32_t dtype, int64_t rows, int32_t L, size_t *bytes);
+int gcpsl_distill(int32_t dtype, int64_t rows, int32_t L, const void *z, int64_t ldz, int32_t top,
+                  const int32_t *t_class, const float *t_value, double temperature, const int32_t *labels, float *kl,
+                  float *lse_t, float *logp, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Gradient of both by the logits: with g_kl and g_logp [rows] the loss's gradients
+ * by kl and logp (either may be NULL),
+ *   dz_c = g_kl (p_c - q_c) / T + g_logp (1[c = y] - e^(z_c - lse)),
+ * p_c = exp(z_c / T - lse_t), q_c the sum of q over the entries of class c; lse_t
+ * (with g_kl) and lse (with g_logp) as gcpsl_distill gave them, off by roundings
+ * as in gcpsl_score_grad.  g_kl adds nothing to a row without entries, g_logp to
+ * one without a label, and neither to a row whose lse_t (lse) is -2^23 or less:
+ * all its classes are ruled out.  dz may be z (lddz = ldz).
+ */
+int gcpsl_distill_grad(int32_t dtype, int64_t rows, int32_t L, const void *z, int64_t ldz, int32_t top,
+                       const int32_t *t_class, const float *t_value, double temperature, const int32_t *labels,
+                       const float *lse_t, const float *lse, const float *g_kl, const float *g_logp, void *dz,
+                       int64_t lddz, void *stream);
 
 /* Release the context (host metadata only; device memory is the caller's;
  * a context of gcpsl_create_static releases its device's static workspace). */

@@ -19,7 +19,7 @@ BIND = os.path.join(HERE, "_ops.so")
 SOURCES = ["api.cpp", "assign.cpp", "k_conv.hip", "k_conv_f32.hip", "k_misc.hip", "k_wgrad_lds.hip", "k_conv_lds.hip", "k_conv_img.hip", "k_norm.hip", "k_block.hip",
            "ops.cpp", "k_group.hip", "k_group_tile.hip", "k_group_f32.hip", "k_group_f32_deep.hip",
            "k_group_mid.hip",
-           "k_group_few.hip", "k_score.hip", "k_drop.hip"]
+           "k_group_few.hip", "k_score.hip", "k_drop.hip", "k_residual.hip", "k_distill.hip"]
 ARCH = "gfx950"
 FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wshadow", "-Wno-unused-function",

@@ -31,9 +31,18 @@ struct {
   decltype(&gcpsl_score_workspace_bytes) score_workspace_bytes;
   decltype(&gcpsl_score) score;
   decltype(&gcpsl_score_grad) score_grad;
+  decltype(&gcpsl_group_gated_forward) gated_forward;
+  decltype(&gcpsl_group_gated_grad) gated_grad;
+  decltype(&gcpsl_group_residual_norm) residual_norm;
+  decltype(&gcpsl_group_residual_workspace_bytes) residual_workspace_bytes;
+  decltype(&gcpsl_group_residual_norm_grad) residual_norm_grad;
+  decltype(&gcpsl_distill_workspace_bytes) distill_workspace_bytes;
+  decltype(&gcpsl_distill) distill;
+  decltype(&gcpsl_distill_grad) distill_grad;
 } entry;
 PyObject *get_device, *get_stream;  // torch's own: the current device, a device's current stream as a number
-PyTypeObject *scores_type;          // gcpsl.Scores
+// gcpsl.Scores, Gated, Residual, ResidualGrads and Distilled
+PyTypeObject *scores_type, *gated_type, *residual_type, *residual_grads_type, *distilled_type;
 
 struct Irregular {};  // thrown: gcpsl.py takes the call
 
@@ -333,14 +342,178 @@ PyObject *score_grad(PyObject *, PyObject *const *a, Py_ssize_t na) {
   });
 }
 
-// init(entries' addresses in the order of `entry`, get_device, get_stream, Scores)
+// group_gated_forward(x, offsets, w, bias, act, keep, out, pre)
+PyObject *group_gated_forward(PyObject *, PyObject *const *a, Py_ssize_t na) {
+  return guarded(na, 8, [&] {
+    const Tensor &xt = tensor(a[0]), &wt = tensor(a[2]);
+    const Call c(xt);
+    const Rows x(c, xt);
+    const Groups g(c, tensor(a[1]));
+    if (wt.dim() != 3 || x.cols < 1 || wt.size(1) % 2) throw Irregular();
+    const int64_t n2 = wt.size(1), n = n2 / 2;
+    const Weights w(c, &wt, c.type, g.n, n2, x.cols), b(c, optional(a[3]), at::kFloat, g.n, n2, 0);
+    const int32_t act = int32(integer(a[4]));
+    const int keep = PyObject_IsTrue(a[5]);
+    if (keep < 0) throw python_error();
+    const bool kept = keep || a[7] != Py_None;
+    Rows y, pre;
+    const Tensor out = result(c, a[6], x.rows, n, y), pairs = kept ? result(c, a[7], x.rows, n2, pre) : Tensor();
+    call(entry.gated_forward, c.code, g.n, x.rows, int32(n), int32(x.cols), g.offsets, x.p, x.ld, w.p, w.stride,
+         (const float *)b.p, b.stride, act, y.p, y.ld, pre.p, pre.ld, c.stream);
+    return tuple({&out, kept ? &pairs : nullptr}, gated_type);
+  });
+}
+
+// group_gated_grad(dz, offsets, w, pre, act, out)
+PyObject *group_gated_grad(PyObject *, PyObject *const *a, Py_ssize_t na) {
+  return guarded(na, 6, [&] {
+    const Tensor &dt = tensor(a[0]), &wt = tensor(a[2]);
+    const Call c(dt);
+    const Rows dz(c, dt);
+    const Groups g(c, tensor(a[1]));
+    if (wt.dim() != 3 || wt.size(2) < 1) throw Irregular();
+    const int64_t n = wt.size(2);
+    const Weights w(c, &wt, c.type, g.n, dz.cols, n);
+    const Rows pre(c, tensor(a[3]), dz.rows, 2 * n);
+    Rows d;
+    const Tensor out = result(c, a[5], dz.rows, 2 * n, d);
+    call(entry.gated_grad, c.code, g.n, dz.rows, int32(dz.cols), int32(n), g.offsets, dz.p, dz.ld, w.p, w.stride,
+         int32(integer(a[4])), pre.p, pre.ld, d.p, d.ld, c.stream);
+    return THPVariable_Wrap(out);
+  });
+}
+
+// group_residual_norm(x, offsets, y, gate, w_block, w_next, alpha, beta, eps, out, h)
+PyObject *group_residual_norm(PyObject *, PyObject *const *a, Py_ssize_t na) {
+  return guarded(na, 11, [&] {
+    const Tensor &xt = tensor(a[0]);
+    const Call c(xt);
+    const Rows x(c, xt);
+    const Groups g(c, tensor(a[1]));
+    const int64_t rows = x.rows, n = x.cols;
+    if (n < 1) throw Irregular();
+    const auto given = [&](PyObject *o) { return o == Py_None ? Rows() : Rows(c, tensor(o), rows, n); };
+    const Rows y = given(a[2]), gate = given(a[3]);
+    const Weights w1(c, optional(a[4]), at::kFloat, g.n, n, 0), w2(c, optional(a[5]), at::kFloat, g.n, n, 0);
+    const bool block = a[2] != Py_None, first = a[4] != Py_None, next = a[5] != Py_None;
+    const double alpha = number(a[6]), beta = number(a[7]), eps = number(a[8]);
+    if ((!block && a[9] != Py_None) || (!next && a[10] != Py_None)) throw Irregular();
+    Rows o, hr;
+    const Tensor out = block ? result(c, a[9], rows, n, o) : xt, h = next ? result(c, a[10], rows, n, hr) : Tensor(),
+                 r1 = first ? c.empty({rows}, at::kFloat) : Tensor(), r2 = next ? c.empty({rows}, at::kFloat) : Tensor();
+    call(entry.residual_norm, c.code, g.n, rows, int32(n), g.offsets, x.p, x.ld, y.p, y.ld, gate.p, gate.ld,
+         (const float *)w1.p, w1.stride, (const float *)w2.p, w2.stride, alpha, beta, eps, o.p, o.ld, hr.p, hr.ld,
+         first ? (float *)r1.data_ptr() : nullptr, next ? (float *)r2.data_ptr() : nullptr, c.stream);
+    return tuple({&out, next ? &h : nullptr, first ? &r1 : nullptr, next ? &r2 : nullptr}, residual_type);
+  });
+}
+
+// group_residual_norm_grad(out, offsets, g_out, g_h, y, gate, w_block, w_next, r_block, r_next, alpha, beta)
+PyObject *group_residual_norm_grad(PyObject *, PyObject *const *a, Py_ssize_t na) {
+  return guarded(na, 12, [&] {
+    const Tensor &xt = tensor(a[0]);
+    const Call c(xt);
+    const Rows x(c, xt);
+    const Groups g(c, tensor(a[1]));
+    const int64_t rows = x.rows, n = x.cols;
+    if (n < 1) throw Irregular();
+    const auto given = [&](PyObject *o) { return o == Py_None ? Rows() : Rows(c, tensor(o), rows, n); };
+    const Rows go = given(a[2]), gh = given(a[3]), y = given(a[4]), gate = given(a[5]);
+    const Weights w1(c, optional(a[6]), at::kFloat, g.n, n, 0), w2(c, optional(a[7]), at::kFloat, g.n, n, 0);
+    const float *r1 = vector<float>(c, optional(a[8]), at::kFloat, rows), *r2 = vector<float>(c, optional(a[9]), at::kFloat, rows);
+    const double alpha = number(a[10]), beta = number(a[11]);
+    const bool block = a[4] != Py_None, gated = a[5] != Py_None, first = a[6] != Py_None, next = a[7] != Py_None;
+    size_t need = 0;
+    if (first || next) call(entry.residual_workspace_bytes, c.code, g.n, rows, int32(n), &need);
+    const auto made = [&](bool is) { return is ? c.empty({rows, n}, c.type) : Tensor(); };
+    const auto summed = [&](bool is) { return is ? c.empty({g.n, n}, at::kFloat) : Tensor(); };
+    const Tensor dx = made(true), dy = made(block), dgate = made(gated), dw1 = summed(first), dw2 = summed(next),
+                 work = need ? c.empty({(int64_t)need}, at::kByte) : Tensor();
+    const auto at = [](const Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
+    call(entry.residual_norm_grad, c.code, g.n, rows, int32(n), g.offsets, x.p, x.ld, go.p, go.ld, gh.p, gh.ld, y.p, y.ld,
+         gate.p, gate.ld, (const float *)w1.p, w1.stride, (const float *)w2.p, w2.stride, r1, r2, alpha, beta, at(dx), n,
+         at(dy), n, at(dgate), n, (float *)at(dw1), n, (float *)at(dw2), n, at(work), need, c.stream);
+    return tuple({&dx, block ? &dy : nullptr, gated ? &dgate : nullptr, first ? &dw1 : nullptr, next ? &dw2 : nullptr},
+                 residual_grads_type);
+  });
+}
+
+// A teacher's classes and values, [rows][top].
+struct Teacher {
+  const int32_t *cls;
+  const float *value;
+  int32_t top;
+  Teacher(const Call &c, const Tensor &k, const Tensor &v, int64_t rows) {
+    for (const Tensor *t : {&k, &v})
+      if (t->dim() != 2 || t->size(0) != rows || t->size(1) != k.size(1) || t->device() != c.device || !t->is_contiguous())
+        throw Irregular();
+    if (k.scalar_type() != at::kInt || v.scalar_type() != at::kFloat) throw Irregular();
+    cls = (const int32_t *)k.data_ptr();
+    value = (const float *)v.data_ptr();
+    top = int32(k.size(1));
+  }
+};
+
+// distill(logits, t_class, t_value, temperature, labels)
+PyObject *distill(PyObject *, PyObject *const *a, Py_ssize_t na) {
+  return guarded(na, 5, [&] {
+    const Tensor &zt = tensor(a[0]);
+    const Call c(zt);
+    const Rows z(c, zt);
+    const Teacher teacher(c, tensor(a[1]), tensor(a[2]), z.rows);
+    const double temperature = number(a[3]);
+    const int32_t *labels = vector<int32_t>(c, optional(a[4]), at::kInt, z.rows);
+    const bool given = a[4] != Py_None;
+    const int32_t L = int32(z.cols);
+    size_t need = 0;
+    call(entry.distill_workspace_bytes, c.code, z.rows, L, &need);
+    const Tensor work = need ? c.empty({(int64_t)need}, at::kByte) : Tensor();
+    const int64_t n = z.rows;
+    const Tensor held = c.empty({n * (given ? 4 : 2)}, at::kFloat);
+    const Tensor kl = part(held, 0, {n}, at::kFloat), lse_t = part(held, n, {n}, at::kFloat),
+                 logp = given ? part(held, 2 * n, {n}, at::kFloat) : Tensor(),
+                 lse = given ? part(held, 3 * n, {n}, at::kFloat) : Tensor();
+    call(entry.distill, c.code, n, L, z.p, z.ld, teacher.top, teacher.cls, teacher.value, temperature, labels,
+         (float *)kl.data_ptr(), (float *)lse_t.data_ptr(), given ? (float *)logp.data_ptr() : nullptr,
+         given ? (float *)lse.data_ptr() : nullptr, need ? work.data_ptr() : nullptr, need, c.stream);
+    return tuple({&kl, given ? &logp : nullptr, &lse_t, given ? &lse : nullptr}, distilled_type);
+  });
+}
+
+// distill_grad(logits, t_class, t_value, lse_t, temperature, labels, lse, g_kl, g_logp, out)
+PyObject *distill_grad(PyObject *, PyObject *const *a, Py_ssize_t na) {
+  return guarded(na, 10, [&] {
+    const Tensor &zt = tensor(a[0]);
+    const Call c(zt);
+    const Rows z(c, zt);
+    const Teacher teacher(c, tensor(a[1]), tensor(a[2]), z.rows);
+    const auto row = [&](PyObject *o) { return (const float *)vector<float>(c, optional(o), at::kFloat, z.rows); };
+    const float *lse_t = row(a[3]), *lse = row(a[6]), *g_kl = row(a[7]), *g_logp = row(a[8]);
+    const double temperature = number(a[4]);
+    const int32_t *labels = vector<int32_t>(c, optional(a[5]), at::kInt, z.rows);
+    Rows dz;
+    const Tensor out = result(c, a[9], z.rows, z.cols, dz);
+    call(entry.distill_grad, c.code, z.rows, int32(z.cols), z.p, z.ld, teacher.top, teacher.cls, teacher.value, temperature,
+         labels, lse_t, lse, g_kl, g_logp, dz.p, dz.ld, c.stream);
+    return THPVariable_Wrap(out);
+  });
+}
+
+// init(entries' addresses in the order of `entry`, get_device, get_stream, the results' types)
 PyObject *init(PyObject *, PyObject *args) {
-  PyObject *addresses, *device, *stream, *scores;
-  if (!PyArg_ParseTuple(args, "O!OOO!", &PyTuple_Type, &addresses, &device, &stream, &PyType_Type, &scores)) return nullptr;
+  PyObject *addresses, *device, *stream, *types;
+  if (!PyArg_ParseTuple(args, "O!OOO!", &PyTuple_Type, &addresses, &device, &stream, &PyTuple_Type, &types)) return nullptr;
   void *p[sizeof(entry) / sizeof(void *)];
   constexpr Py_ssize_t n = sizeof(p) / sizeof(p[0]);
-  if (PyTuple_GET_SIZE(addresses) != n || !PyType_IsSubtype((PyTypeObject *)scores, &PyTuple_Type)) {
-    PyErr_SetString(PyExc_ValueError, "addresses of the entries and a tuple type expected");
+  PyTypeObject **const to[] = {&scores_type, &gated_type, &residual_type, &residual_grads_type, &distilled_type};
+  constexpr Py_ssize_t nt = sizeof(to) / sizeof(to[0]);
+  bool ok = PyTuple_GET_SIZE(addresses) == n && PyTuple_GET_SIZE(types) == nt;
+  for (Py_ssize_t i = 0; ok && i < nt; ++i) {
+    PyObject *t = PyTuple_GET_ITEM(types, i);
+    ok = PyType_Check(t) && PyType_IsSubtype((PyTypeObject *)t, &PyTuple_Type);
+  }
+  if (!ok) {
+    PyErr_SetString(PyExc_ValueError, "addresses of the entries and tuple types expected");
     return nullptr;
   }
   for (Py_ssize_t i = 0; i < n; ++i) {
@@ -350,7 +523,7 @@ PyObject *init(PyObject *, PyObject *args) {
   memcpy(&entry, p, sizeof(entry));
   get_device = Py_NewRef(device);  // kept for the process's life
   get_stream = Py_NewRef(stream);
-  scores_type = (PyTypeObject *)Py_NewRef(scores);
+  for (Py_ssize_t i = 0; i < nt; ++i) *to[i] = (PyTypeObject *)Py_NewRef(PyTuple_GET_ITEM(types, i));
   Py_RETURN_NONE;
 }
 
@@ -361,6 +534,12 @@ PyMethodDef methods[] = {
     {"group_weight_grad", (PyCFunction)(void (*)(void))group_weight_grad, METH_FASTCALL, nullptr},
     {"dropout", (PyCFunction)(void (*)(void))dropout, METH_FASTCALL, nullptr},
     {"score", (PyCFunction)(void (*)(void))score, METH_FASTCALL, nullptr},
+    {"group_gated_forward", (PyCFunction)(void (*)(void))group_gated_forward, METH_FASTCALL, nullptr},
+    {"group_gated_grad", (PyCFunction)(void (*)(void))group_gated_grad, METH_FASTCALL, nullptr},
+    {"group_residual_norm", (PyCFunction)(void (*)(void))group_residual_norm, METH_FASTCALL, nullptr},
+    {"group_residual_norm_grad", (PyCFunction)(void (*)(void))group_residual_norm_grad, METH_FASTCALL, nullptr},
+    {"distill", (PyCFunction)(void (*)(void))distill, METH_FASTCALL, nullptr},
+    {"distill_grad", (PyCFunction)(void (*)(void))distill_grad, METH_FASTCALL, nullptr},
     {"score_grad", (PyCFunction)(void (*)(void))score_grad, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -117,6 +117,7 @@ GROUP_DEVICE int lane_of(const LaneTiles &l, uint32_t t) {
 // operands read from memory: 716 against 640 us for 16 groups of 1,024 rows.)
 // (Offsets that decrease can make more partials than there is room for: those
 // are left out.)
+template <int GRAIN = 64>  // rows that pieces are multiples of
 GROUP_DEVICE bool piece_of(const GroupArgs &a, uint32_t tiles, uint32_t b, int &g, int &q0, int &q1, int &slot,
                            uint32_t &tile) {
   LaneTiles l;
@@ -143,7 +144,7 @@ GROUP_DEVICE bool piece_of(const GroupArgs &a, uint32_t tiles, uint32_t b, int &
   }
   const int begin = of_lane(l.begin, i), end = of_lane(l.end, i);
   const int n = of_lane((int)l.tiles, i), k = (int)(t - (uint32_t)of_lane((int)l.first, i));
-  const int part = ((end - begin + n - 1) / n + 63) / 64 * 64;
+  const int part = ((end - begin + n - 1) / n + GRAIN - 1) / GRAIN * GRAIN;
   const int64_t at = begin + (int64_t)k * part;  // may pass the group's end, and 31 bits
   g = __builtin_amdgcn_readfirstlane(base + i);
   q0 = __builtin_amdgcn_readfirstlane((int)min(at, (int64_t)end));
@@ -384,6 +385,73 @@ template <typename T, int MODE, int ROWS, bool EDGES = true> struct FinishRows {
     }
   }
 };
+
+// ------------------------------------------------------------ gated layers
+// What a gated layer's columns are in the tiles of operand b: of BN columns the
+// first half are gates c0 .. and the second the values of the same outputs, N
+// rows of w further on; c0 = nt BN / 2.
+
+constexpr float kLog2E = 1.44269504088896340736f;
+// s = 1 / (1 + e^-g) and 1 - s, from e^-|g|: neither overflows nor cancels.
+GROUP_DEVICE float sigmoid_of(float g, float &rest) {
+  const float e = __builtin_amdgcn_exp2f(-kLog2E * fabsf(g)), r = __builtin_amdgcn_rcpf(1.f + e), er = e * r;
+  rest = g < 0.f ? r : er;
+  return g < 0.f ? er : r;
+}
+// f(g)
+GROUP_DEVICE float gate_of(int act, float g) {
+  float rest;
+  if (act == GCPSL_SILU) return g * sigmoid_of(g, rest);
+  if (act == GCPSL_GELU) return 0.5f * g * erfcf(-0.70710678118654752440f * g);  // (1 + erf would lose the lower tail)
+  return g <= 0.f ? 0.f : g;
+}
+// f(g) and f'(g)
+GROUP_DEVICE void gate_grad_of(int act, float g, float &f, float &d) {
+  if (act == GCPSL_SILU) {
+    float rest;
+    const float s = sigmoid_of(g, rest);
+    f = g * s;
+    d = fmaf(f, rest, s);
+  } else if (act == GCPSL_GELU) {
+    const float phi = 0.5f * erfcf(-0.70710678118654752440f * g);
+    f = g * phi;
+    d = fmaf(g * 0.39894228040143267794f, __builtin_amdgcn_exp2f(-0.5f * kLog2E * g * g), phi);
+  } else {
+    f = g <= 0.f ? 0.f : g;
+    d = g <= 0.f ? 0.f : g > 0.f ? 1.f : g;  // (a NaN stays one)
+  }
+}
+
+// Up to four columns c .. c + 3 of row m of a gated layer's result.  MODE
+// GROUP_GATED: from the sums of gates and values; GROUP_GATED_GRAD: from those
+// of the gradient (gates unused).
+template <typename T, int MODE, typename V>
+GROUP_DEVICE void finish_pair(const GroupArgs &a, int g, int m, int c, const V &gates, const V &values) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    if (c + r >= a.N) break;
+    if constexpr (MODE == GROUP_GATED) {
+      float p = gates[r], u = values[r];
+      if (a.bias) {
+        p += a.bias[g * a.bias_gs + c + r];
+        u += a.bias[g * a.bias_gs + a.N + c + r];
+      }
+      ((T *)a.out)[(int64_t)m * a.ldo + c + r] = ElemT<T>::from_f(gate_of(a.act, p) * u);
+      if (a.pre) {
+        T *pre = (T *)a.pre + (int64_t)m * a.ldp + c + r;
+        pre[0] = ElemT<T>::from_f(p);
+        pre[a.N] = ElemT<T>::from_f(u);
+      }
+    } else {
+      const T *pre = (const T *)a.pre + (int64_t)m * a.ldp + c + r;
+      float f, d;
+      gate_grad_of(a.act, ElemT<T>::to_f(pre[0]), f, d);
+      T *out = (T *)a.out + (int64_t)m * a.ldo + c + r;
+      out[0] = ElemT<T>::from_f(d * ElemT<T>::to_f(pre[a.N]) * values[r]);
+      out[a.N] = ElemT<T>::from_f(f * values[r]);
+    }
+  }
+}
 
 // Four columns of a weight gradient, to its place or (slot >= 0) to a partial.
 template <typename V> GROUP_DEVICE void store_grad(const GroupArgs &a, int g, int slot, int m, int c, const V &acc) {

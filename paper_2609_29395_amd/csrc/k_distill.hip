@@ -1,0 +1,534 @@
+// Distillation of rows of logits from a teacher's best classes (gfx950): the
+// divergence beside the label's log probability, and the logits' gradient.
+//
+//   kl = sum_k q_k (log q_k - log p_k),  q = softmax(v / T),  p = softmax(z / T)
+//   dz = g_kl (p - q) / T + g_logp (1[c = y] - softmax(z))
+//
+// Forward, one pass over the logits: every thread keeps a running maximum m of its
+// own and the sums of e^((z - m) / T) and, where both are asked for, e^(z - m), and
+// brings them to a larger maximum once for a batch of 16-byte vectors.  A row is a
+// workgroup's, or a wave's where it is short; where the rows are fewer than the
+// chip holds workgroups, each is cut into parts that a second kernel joins.  With
+// w_k = e^((v_k - max v) / T) and W their sum, kl = sum_k w_k (log w_k - log p_k) / W
+// - log W, from `top` logits of the row.
+//
+// Gradient: the dense terms go over the row; then, behind a barrier, the
+// teacher's classes of the part are written again with their q_k, which all
+// entries of a class sum in the same order (no atomics: the same bits always).
+//
+// Bound: memory.
+#include <algorithm>
+
+#include "ops.h"
+#include "runtime.h"
+
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));  // global memory takes 16-byte accesses at any alignment
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
+__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
+__device__ __forceinline__ float log_of(float s) { return __builtin_amdgcn_logf(s) * kLn2; }
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
+
+// An lse from which on a row's classes count as ruled out, as for the score gradient.
+constexpr float kRuledOut = -8388608.f;
+
+template <typename T> struct Bits;  // the elements of a 16-byte vector
+template <> struct Bits<float> {
+  static constexpr int VEC = 4;
+  static __device__ __forceinline__ float at(const u32x4 &w, int j) { return __uint_as_float(w[j]); }
+  static __device__ __forceinline__ void drop_first(u32x4 &w, int n) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < n) w[j] = 0xff800000u;  // -inf
+  }
+};
+template <> struct Bits<bf16_t> {
+  static constexpr int VEC = 8;
+  static __device__ __forceinline__ float at(const u32x4 &w, int j) {
+    return __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
+  }
+  static __device__ __forceinline__ void drop_first(u32x4 &w, int n) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < n) w[j >> 1] = j & 1 ? (w[j >> 1] & 0xffffu) | 0xff800000u : (w[j >> 1] & 0xffff0000u) | 0xff80u;
+  }
+};
+
+// Over groups of W lanes (16 or 64).
+template <int W> __device__ __forceinline__ float lanes_max(float v) {
+#pragma unroll
+  for (int d = W / 2; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, W));
+  return v;
+}
+template <int W> __device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+  for (int d = W / 2; d; d >>= 1) v += __shfl_xor(v, d, W);
+  return v;
+}
+// Over a row's TPR threads; buf [4].
+template <int TPR> __device__ __forceinline__ float row_max(float v, float *buf) {
+  v = lanes_max<TPR == 256 ? 64 : TPR>(v);
+  if constexpr (TPR == 256) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = fmaxf(fmaxf(buf[0], buf[1]), fmaxf(buf[2], buf[3]));
+  }
+  return v;
+}
+template <int TPR> __device__ __forceinline__ float row_sum(float v, float *buf) {
+  v = lanes_sum<TPR == 256 ? 64 : TPR>(v);
+  if constexpr (TPR == 256) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = (buf[0] + buf[1]) + (buf[2] + buf[3]);
+  }
+  return v;
+}
+template <int TPR> __device__ __forceinline__ void row_sync() {
+  if constexpr (TPR == 256) __syncthreads();
+  else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+// Sums of a set of logits below its maximum m: of e^((z - m) / T), of e^(z - m).
+struct Sums {
+  float m, t, s;
+};
+__device__ __forceinline__ void rebase(Sums &p, float m, float inv_t) {
+  const float d = p.m - base_of(m);  // (-inf or less where nothing was summed: t = s = 0)
+  p.t *= exp_of(d * inv_t);
+  p.s *= exp_of(d);
+  p.m = m;
+}
+__device__ __forceinline__ void join(Sums &p, Sums q, float inv_t) {
+  const float m = fmaxf(p.m, q.m);
+  rebase(p, m, inv_t);
+  rebase(q, m, inv_t);
+  p.t += q.t;
+  p.s += q.s;
+}
+template <int W> __device__ __forceinline__ void lanes_join(Sums &p, float inv_t) {
+  rebase(p, lanes_max<W>(p.m), inv_t);
+  p.t = lanes_sum<W>(p.t);
+  p.s = lanes_sum<W>(p.s);
+}
+
+// Logarithms of a row's probabilities at one temperature; rows without a class
+// left have -inf throughout, those with a NaN or +inf NaN.
+struct RowLog {
+  float base, ls, lse, inv;
+  bool empty;
+  __device__ __forceinline__ RowLog(float m, float s, float inv_) : inv(inv_) {
+    empty = s == 0.f;
+    base = base_of(m);
+    ls = s < INFINITY ? log_of(s) : NAN;
+    lse = empty ? -INFINITY : fmaf(base, inv, ls);
+  }
+  __device__ __forceinline__ float logp(float x) const { return empty ? -INFINITY : fmaf(x - base, inv, -ls); }
+};
+
+// Results of a row from its sums, by W lanes (this one is lane t).  a.temperature 1: the two sums are one.
+template <typename T, int W> __device__ __forceinline__ void write_row(const DistillArgs &a, int64_t row, const Sums &p, int t) {
+  const float inv_t = 1.f / a.temperature;
+  const RowLog soft(p.m, p.t, inv_t);
+  const T *z = (const T *)a.z + row * a.ldz;
+  if (t == 0) {
+    const RowLog plain(p.m, a.temperature == 1.f ? p.t : p.s, 1.f);
+    if (a.lse_t) a.lse_t[row] = soft.lse;
+    if (a.lse) a.lse[row] = plain.lse;
+    if (a.logp) {
+      const int y = a.labels[row];
+      a.logp[row] = (unsigned)y < (unsigned)a.L ? plain.logp(ElemT<T>::to_f(z[y])) : 0.f;
+    }
+  }
+  if (!a.kl) return;
+  const int32_t *tc = a.t_class + row * a.top;
+  const float *tv = a.t_value + row * a.top;
+  float best = -INFINITY;
+  for (int k = t; k < a.top; k += W)
+    if ((unsigned)tc[k] < (unsigned)a.L) best = fmaxf(best, tv[k]);
+  best = base_of(lanes_max<W>(best));
+  float sum = 0.f, part = 0.f;
+  for (int k = t; k < a.top; k += W) {
+    const int c = tc[k];
+    if ((unsigned)c >= (unsigned)a.L) continue;
+    const float d = (tv[k] - best) * inv_t, w = exp_of(d);
+    if (w == 0.f) continue;  // (-inf, or so far below that its term is 0)
+    sum += w;
+    part = fmaf(w, d - soft.logp(ElemT<T>::to_f(z[c])), part);
+  }
+  sum = lanes_sum<W>(sum);
+  part = lanes_sum<W>(part);
+  if (t == 0) a.kl[row] = sum == 0.f ? 0.f : part / sum - log_of(sum);
+}
+
+constexpr int kAhead = 4;  // vectors of a thread in flight
+
+// Part `job` % parts of row `job` / parts by TPR threads; a part is `per` vectors.  TWO: both sums.
+template <typename T, int TPR, bool TWO>
+__global__ void __launch_bounds__(256) distill_kernel(DistillArgs a, uint32_t jobs, FastDiv fd_parts, uint32_t per) {
+  using B = Bits<T>;
+  constexpr int VEC = B::VEC, GROUPS = 256 / TPR;
+  __shared__ float4 wsum[4];
+  const int t = threadIdx.x % TPR, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t job = blockIdx.x * GROUPS + (TPR == 256 ? 0 : wave);
+  if (job >= jobs) return;  // (a wave's own row where it shares the workgroup)
+  const int64_t row = fdiv(job, fd_parts);
+  const uint32_t part = job - (uint32_t)row * fd_parts.d;
+  const T *z = (const T *)a.z + row * a.ldz;
+  const int L = a.L;
+  const uint32_t vectors = ((uint32_t)L + VEC - 1) / VEC, v0 = part * per, v1 = min(vectors, v0 + per);
+  const float inv_t = 1.f / a.temperature, ct = kLog2e * inv_t;
+  Sums p{-INFINITY, 0.f, 0.f};
+  for (uint32_t v = v0; v < v1; v += kAhead * TPR) {
+    u32x4 w[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const uint32_t i = (v + u * TPR + t) * VEC;
+      w[u] = *(const u32x4_any *)(z + min(i, (uint32_t)(L - VEC)));
+    }
+    if (v + kAhead * TPR >= v1) {  // the part's last vectors: without what is the next part's or counted before
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const uint32_t at = v + u * TPR + t;
+        B::drop_first(w[u], at >= v1 ? VEC : max((int)(at * VEC + VEC) - L, 0));
+      }
+    }
+    float m = p.m;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) m = fmaxf(m, B::at(w[u], j));
+    rebase(p, m, inv_t);
+    const float base = base_of(m);
+    float t2[2] = {0.f, 0.f}, s2[2] = {0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const float d = B::at(w[u], j) - base;
+        t2[j & 1] += __builtin_amdgcn_exp2f(d * ct);
+        if (TWO) s2[j & 1] += __builtin_amdgcn_exp2f(d * kLog2e);
+      }
+    p.t += t2[0] + t2[1];
+    p.s += s2[0] + s2[1];
+  }
+  lanes_join<64>(p, inv_t);
+  if constexpr (TPR == 256) {
+    if ((threadIdx.x & 63) == 0) wsum[wave] = make_float4(p.m, p.t, p.s, 0.f);
+    __syncthreads();
+    if (wave) return;
+    p = Sums{wsum[0].x, wsum[0].y, wsum[0].z};
+#pragma unroll
+    for (int i = 1; i < 4; ++i) join(p, Sums{wsum[i].x, wsum[i].y, wsum[i].z}, inv_t);
+  }
+  if (fd_parts.d > 1) {
+    if (t == 0) ((float4 *)a.work)[job] = make_float4(p.m, p.t, p.s, 0.f);
+  } else {
+    write_row<T, 64>(a, row, p, t);
+  }
+}
+
+// Rows of several parts, a wave each.
+template <typename T> __global__ void __launch_bounds__(256) distill_join_kernel(DistillArgs a, uint32_t parts) {
+  const int lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (row >= a.rows) return;
+  const float inv_t = 1.f / a.temperature;
+  const float4 *work = (const float4 *)a.work + row * parts;
+  Sums p{-INFINITY, 0.f, 0.f};
+  for (uint32_t i = lane; i < parts; i += 64) join(p, Sums{work[i].x, work[i].y, work[i].z}, inv_t);
+  lanes_join<64>(p, inv_t);
+  write_row<T, 64>(a, row, p, lane);
+}
+
+// Rows of at most 64 classes: 16 lanes a row.
+template <typename T> __global__ void __launch_bounds__(256) distill_small_kernel(DistillArgs a) {
+  const int lane = threadIdx.x & 15;
+  const int64_t job = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  if (job >= a.rows) return;  // (shuffles stay within the 16 lanes)
+  const T *z = (const T *)a.z + job * a.ldz;
+  const float inv_t = 1.f / a.temperature;
+  float x[4], m = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[i] = i * 16 + lane < a.L ? ElemT<T>::to_f(z[i * 16 + lane]) : -INFINITY;
+    m = fmaxf(m, x[i]);
+  }
+  Sums p{lanes_max<16>(m), 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float d = x[i] - base_of(p.m);
+    p.t += exp_of(d * inv_t);
+    p.s += exp_of(d);
+  }
+  p.t = lanes_sum<16>(p.t);
+  p.s = lanes_sum<16>(p.s);
+  write_row<T, 16>(a, job, p, lane);
+}
+
+// --------------------------------------------------------------- gradient
+// What an element's gradient takes of its row; ruled-out rows and those without label or teacher have weights 0.
+struct GradRow {
+  float gk, lse_t, gl, lse, inv_t;
+  int y;
+  __device__ __forceinline__ GradRow(const DistillGradArgs &a, int64_t row, bool teacher) : lse_t(0.f), lse(0.f), y(-1) {
+    inv_t = 1.f / a.temperature;
+    gk = gl = 0.f;
+    if (a.g_kl && teacher) {
+      lse_t = a.lse_t[row];
+      if (!(lse_t <= kRuledOut)) gk = a.g_kl[row] * inv_t;
+      else lse_t = 0.f;
+    }
+    if (a.g_logp) {
+      const int label = a.labels[row];
+      lse = a.lse[row];
+      if ((unsigned)label < (unsigned)a.L && !(lse <= kRuledOut)) {
+        gl = a.g_logp[row];
+        y = label;
+      } else {
+        lse = 0.f;
+      }
+    }
+  }
+  // of the dense terms and the label
+  __device__ __forceinline__ float operator()(float x, int i) const {
+    float d = 0.f;
+    if (gk != 0.f) d = gk * exp_of(fmaf(x, inv_t, -lse_t));
+    if (gl != 0.f) d = fmaf(-gl, exp_of(x - lse), d);
+    return i == y ? d + gl : d;
+  }
+};
+
+// Part of a row by TPR threads, as in the forward pass.
+template <typename T, int TPR>
+__global__ void __launch_bounds__(256) distill_grad_kernel(DistillGradArgs a, uint32_t jobs, FastDiv fd_parts, uint32_t per) {
+  using B = Bits<T>;
+  constexpr int VEC = B::VEC, GROUPS = 256 / TPR;
+  __shared__ float buf[4], weight_[GROUPS][kMaxTeacher], logit_[GROUPS][kMaxTeacher];
+  __shared__ int class_[GROUPS][kMaxTeacher];
+  const int t = threadIdx.x % TPR, grp = TPR == 256 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  float *weight = weight_[grp], *logit = logit_[grp];
+  int *cls = class_[grp];
+  const uint32_t job = blockIdx.x * GROUPS + grp;
+  if (job >= jobs) return;
+  const int64_t row = fdiv(job, fd_parts);
+  const uint32_t part = job - (uint32_t)row * fd_parts.d;
+  const T *z = (const T *)a.z + row * a.ldz;
+  T *dz = (T *)a.dz + row * a.lddz;
+  const int L = a.L, top = a.g_kl ? a.top : 0;
+  const uint32_t vectors = ((uint32_t)L + VEC - 1) / VEC, v0 = part * per, v1 = min(vectors, v0 + per);
+  const uint32_t c0 = v0 * VEC, c1 = min((uint32_t)L, v1 * VEC);  // the part's classes
+  const float inv_t = 1.f / a.temperature;
+
+  // the teacher's classes: weights, and the logits of those in this part (read before anything of it is written)
+  float best = -INFINITY, sum = 0.f;
+  bool any = false;
+  for (int k = t; k < top; k += TPR) {
+    int c = a.t_class[row * a.top + k];
+    const float v = a.t_value[row * a.top + k];
+    if ((unsigned)c >= (unsigned)L || v == -INFINITY) c = -1;
+    cls[k] = c;
+    weight[k] = v;
+    if (c >= 0) {
+      best = fmaxf(best, v);
+      any = true;
+    }
+    logit[k] = (uint32_t)c - c0 < c1 - c0 ? ElemT<T>::to_f(z[c]) : 0.f;
+  }
+  if (top) {
+    best = base_of(row_max<TPR>(best, buf));
+    for (int k = t; k < top; k += TPR) {
+      const float w = cls[k] >= 0 ? exp_of((weight[k] - best) * inv_t) : 0.f;
+      weight[k] = w;
+      sum += w;
+    }
+    sum = row_sum<TPR>(sum, buf);
+    any = row_max<TPR>(any ? 1.f : 0.f, buf) > 0.f;
+  }
+  const GradRow grad(a, row, any);
+  row_sync<TPR>();
+
+  for (uint32_t v = v0; v < v1; v += kAhead * TPR) {
+    u32x4 w[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const uint32_t at = v + u * TPR + t;
+      w[u] = u32x4{0, 0, 0, 0};
+      if (at < v1 && at * VEC + VEC <= (uint32_t)L) w[u] = *(const u32x4_any *)(z + at * VEC);
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const uint32_t at = v + u * TPR + t;
+      if (at >= v1) break;
+      const int i = (int)(at * VEC);
+      if (i + VEC <= L) {
+        u32x4 o;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if constexpr (VEC == 4) o[j] = __float_as_uint(grad(B::at(w[u], j), i + j));
+          else o[j] = pack2_bf16(grad(B::at(w[u], 2 * j), i + 2 * j), grad(B::at(w[u], 2 * j + 1), i + 2 * j + 1));
+        }
+        *(u32x4_any *)(dz + i) = o;
+      } else {
+        for (int k = i; k < L; ++k) dz[k] = ElemT<T>::from_f(grad(ElemT<T>::to_f(z[k]), k));
+      }
+    }
+  }
+  if (!any || grad.gk == 0.f) return;
+  row_sync<TPR>();
+  for (int k = t; k < top; k += TPR) {
+    const int c = cls[k];
+    if ((uint32_t)c - c0 >= c1 - c0) continue;
+    float q = 0.f;
+    for (int j = 0; j < top; ++j)
+      if (cls[j] == c) q += weight[j];
+    dz[c] = ElemT<T>::from_f(fmaf(-grad.gk, q / sum, grad(logit[k], c)));
+  }
+}
+
+// Rows of at most 64 classes: 16 lanes a row.
+template <typename T> __global__ void __launch_bounds__(256) distill_grad_small_kernel(DistillGradArgs a) {
+  const int lane = threadIdx.x & 15;
+  const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  if (row >= a.rows) return;  // (shuffles stay within the 16 lanes)
+  const T *z = (const T *)a.z + row * a.ldz;
+  T *dz = (T *)a.dz + row * a.lddz;
+  const int top = a.g_kl ? a.top : 0;
+  const int32_t *tc = a.t_class + row * a.top;
+  const float *tv = a.t_value + row * a.top;
+  const float inv_t = 1.f / a.temperature;
+  float x[4], q[4] = {0.f, 0.f, 0.f, 0.f}, best = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = i * 16 + lane < a.L ? ElemT<T>::to_f(z[i * 16 + lane]) : 0.f;
+  bool any = false;
+  for (int k = lane; k < top; k += 16)
+    if ((unsigned)tc[k] < (unsigned)a.L && tv[k] != -INFINITY) {
+      best = fmaxf(best, tv[k]);
+      any = true;
+    }
+  best = base_of(lanes_max<16>(best));
+  any = lanes_max<16>(any ? 1.f : 0.f) > 0.f;
+  for (int k = 0; k < top; ++k) {  // every lane all entries, in the same order
+    const int c = tc[k];
+    if ((unsigned)c >= (unsigned)a.L || tv[k] == -INFINITY) continue;
+    const float w = exp_of((tv[k] - best) * inv_t);
+    sum += w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] += c == i * 16 + lane ? w : 0.f;
+  }
+  const GradRow grad(a, row, any);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int c = i * 16 + lane;
+    if (c >= a.L) continue;
+    float d = grad(x[i], c);
+    if (grad.gk != 0.f) d = fmaf(-grad.gk, q[i] / sum, d);
+    dz[c] = ElemT<T>::from_f(d);
+  }
+}
+
+// Vectors of a part, and parts of a row: whole rows where they are enough for
+// every CU to have four workgroups, else parts of 2,048 vectors at least.
+struct Parts {
+  bool wave;  // a wave a row
+  uint32_t n, per;
+};
+template <typename T> Parts parts_of_row(int64_t rows, int L) {
+  const uint32_t vectors = ((uint32_t)L + Bits<T>::VEC - 1) / Bits<T>::VEC;
+  if (vectors <= 64 * kAhead) return {true, 1, vectors};
+  const uint32_t step = 256 * kAhead;
+  const int64_t most = (vectors + step - 1) / step, want = (1024 + rows - 1) / std::max<int64_t>(rows, 1);
+  const uint32_t n = (uint32_t)std::max<int64_t>(1, std::min(most, want));
+  const uint32_t per = ((vectors + n - 1) / n + step - 1) / step * step;
+  return {false, (vectors + per - 1) / per, per};
+}
+
+template <typename P> P *entry_at(P *p, int64_t r) { return p ? p + r : nullptr; }
+
+template <typename T> hipError_t run(const DistillArgs &all, hipStream_t s) {
+  const Parts parts = parts_of_row<T>(all.rows, all.L);
+  const bool two = all.temperature != 1.f && (all.lse || all.logp);
+  const int64_t slab = kMaxBlocks / parts.n;
+  for (int64_t r = 0; r < all.rows; r += slab) {
+    DistillArgs a = all;
+    a.z = (const T *)all.z + r * all.ldz;
+    a.rows = std::min(slab, all.rows - r);
+    a.t_class = all.t_class + r * all.top;
+    a.t_value = all.t_value + r * all.top;
+    a.labels = entry_at(all.labels, r);
+    a.kl = entry_at(all.kl, r);
+    a.lse_t = entry_at(all.lse_t, r);
+    a.logp = entry_at(all.logp, r);
+    a.lse = entry_at(all.lse, r);
+    if (a.L <= 64) {
+      hipLaunchKernelGGL(distill_small_kernel<T>, dim3((uint32_t)((a.rows + 15) / 16)), dim3(256), 0, s, a);
+    } else {
+      const uint32_t jobs = (uint32_t)(a.rows * parts.n);
+      const auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3(parts.wave ? (jobs + 3) / 4 : jobs), dim3(256), 0, s, a, jobs,
+                           make_fastdiv(parts.n), parts.per);
+      };
+      if (parts.wave) two ? launch(distill_kernel<T, 64, true>) : launch(distill_kernel<T, 64, false>);
+      else two ? launch(distill_kernel<T, 256, true>) : launch(distill_kernel<T, 256, false>);
+      if (parts.n > 1)
+        hipLaunchKernelGGL(distill_join_kernel<T>, dim3((uint32_t)((a.rows + 3) / 4)), dim3(256), 0, s, a, parts.n);
+    }
+    const hipError_t e = hipGetLastError();  // (one after another on the stream: the workspace serves each)
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <typename T> hipError_t run_grad(const DistillGradArgs &all, hipStream_t s) {
+  const Parts parts = parts_of_row<T>(all.rows, all.L);
+  const int64_t slab = kMaxBlocks / parts.n;
+  for (int64_t r = 0; r < all.rows; r += slab) {
+    DistillGradArgs a = all;
+    a.z = (const T *)all.z + r * all.ldz;
+    a.dz = (T *)all.dz + r * all.lddz;
+    a.rows = std::min(slab, all.rows - r);
+    a.t_class = entry_at(all.t_class, r * all.top);
+    a.t_value = entry_at(all.t_value, r * all.top);
+    a.labels = entry_at(all.labels, r);
+    a.lse_t = entry_at(all.lse_t, r);
+    a.lse = entry_at(all.lse, r);
+    a.g_kl = entry_at(all.g_kl, r);
+    a.g_logp = entry_at(all.g_logp, r);
+    if (a.L <= 64) {
+      hipLaunchKernelGGL(distill_grad_small_kernel<T>, dim3((uint32_t)((a.rows + 15) / 16)), dim3(256), 0, s, a);
+    } else {
+      const uint32_t jobs = (uint32_t)(a.rows * parts.n);
+      const auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3(parts.wave ? (jobs + 3) / 4 : jobs), dim3(256), 0, s, a, jobs,
+                           make_fastdiv(parts.n), parts.per);
+      };
+      if (parts.wave) launch(distill_grad_kernel<T, 64>);
+      else launch(distill_grad_kernel<T, 256>);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <typename T> size_t work_of(int64_t rows, int L) {
+  const Parts parts = parts_of_row<T>(rows, L);
+  return L > 64 && parts.n > 1 ? sizeof(float4) * (size_t)rows * parts.n : 0;
+}
+
+}  // namespace
+
+size_t distill_work_bytes(int dtype, int64_t rows, int L) {
+  return dtype == GCPSL_BF16 ? work_of<bf16_t>(rows, L) : work_of<float>(rows, L);
+}
+hipError_t launch_distill(int dtype, const DistillArgs &a, hipStream_t s) {
+  return dtype == GCPSL_BF16 ? run<bf16_t>(a, s) : run<float>(a, s);
+}
+hipError_t launch_distill_grad(int dtype, const DistillGradArgs &a, hipStream_t s) {
+  return dtype == GCPSL_BF16 ? run_grad<bf16_t>(a, s) : run_grad<float>(a, s);
+}

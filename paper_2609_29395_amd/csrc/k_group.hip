@@ -50,7 +50,9 @@ template <typename T, int MODE>
 __global__ void __launch_bounds__(256) group_any_kernel(GroupArgs a, int NT) {
   using K = Any<T>;
   constexpr int BQ = K::BQ, LD = K::LD, BM = 64, BN = 64;
-  constexpr bool AT = MODE == GROUP_DW, BT = MODE != GROUP_FWD;  // q runs over the operand's rows
+  constexpr bool AT = MODE == GROUP_DW, BT = group_across(MODE);  // q runs over the operand's rows
+  constexpr bool PAIR = MODE == GROUP_GATED;
+  constexpr int COLS = PAIR ? BN / 2 : BN;                       // outputs of a tile
   constexpr int PT = BM * BQ / 256;                              // elements per thread and operand
   __shared__ __attribute__((aligned(16))) T la[BM * LD], lb[BN * LD];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -67,8 +69,10 @@ __global__ void __launch_bounds__(256) group_any_kernel(GroupArgs a, int NT) {
   } else {
     if (!tile_of(a.off, a.G, a.M, BM, NT, blockIdx.x, g, row0, row1, nt)) return;
   }
-  const int c0 = nt * BN;
+  const int c0 = nt * COLS;
   const T *A = (const T *)a.a, *B = (const T *)a.b + g * a.b_gs;
+  // b's row (BT: column) at column j of the tile
+  const auto col = [&](int j) { return PAIR ? min(c0 + j % COLS, a.N - 1) + (j < COLS ? 0 : a.N) : min(c0 + j, a.N - 1); };
 
   f32x4_t acc[2][2];  // [column fragment][row fragment]
 #pragma unroll
@@ -87,7 +91,7 @@ __global__ void __launch_bounds__(256) group_any_kernel(GroupArgs a, int NT) {
     for (int i = 0; i < PT; ++i) {
       const int e = i * 256 + tid;
       const int ra = min(row0 + (AT ? e % BM : e / BQ), row1 - 1), qa = min(q + (AT ? e / BM : e % BQ), q1 - 1);
-      const int rb = min(c0 + (BT ? e % BN : e / BQ), a.N - 1), qb = min(q + (BT ? e / BN : e % BQ), q1 - 1);
+      const int rb = col(BT ? e % BN : e / BQ), qb = min(q + (BT ? e / BN : e % BQ), q1 - 1);
       va[i] = AT ? A[(int64_t)qa * a.lda + ra] : A[(int64_t)ra * a.lda + qa];
       vb[i] = BT ? B[(int64_t)qb * a.ldb + rb] : B[(int64_t)rb * a.ldb + qb];
     }
@@ -118,6 +122,25 @@ __global__ void __launch_bounds__(256) group_any_kernel(GroupArgs a, int NT) {
   }
 
   // lane (li, lg) holds columns 4 lg .. 4 lg + 3 of row li of each fragment
+  if constexpr (PAIR) {  // the values' waves hand their sums over
+    __shared__ f32x4_t values[2][2][2][64];  // [wm][column fragment][row fragment]
+    if (wn == 1) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) values[wm][i][j][lane] = acc[i][j];
+    }
+    __syncthreads();
+    if (wn == 1) return;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int m = row0 + wm * 32 + j * 16 + li, c = c0 + i * 16 + 4 * lg;
+        if (m < row1) finish_pair<T, MODE>(a, g, m, c, acc[i][j], values[wm][i][j][lane]);
+      }
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -126,6 +149,8 @@ __global__ void __launch_bounds__(256) group_any_kernel(GroupArgs a, int NT) {
       if (m >= row1) continue;
       if constexpr (MODE == GROUP_DW) {
         if (c < a.N) store_grad(a, g, slot, m, c, acc[i][j]);
+      } else if constexpr (MODE == GROUP_GATED_GRAD) {
+        finish_pair<T, MODE>(a, g, m, c, acc[i][j], acc[i][j]);
       } else {
         if (c < a.N) finish<T, MODE>(a, g, m, c, acc[i][j]);
       }
@@ -214,7 +239,7 @@ __global__ void __launch_bounds__(256) group_join_kernel(GroupArgs a, uint32_t b
 
 template <typename T>
 hipError_t launch_any(int mode, const GroupArgs &a, hipStream_t s) {
-  const int NT = (a.N + 63) / 64;
+  const int NT = mode == GROUP_GATED ? (a.N + 31) / 32 : (a.N + 63) / 64;
   if (mode == GROUP_DW) {
     const int64_t blocks = piece_blocks(a, (int64_t)((a.M + 63) / 64) * NT);
     if (blocks > kMaxBlocks) return hipErrorInvalidConfiguration;
@@ -223,10 +248,11 @@ hipError_t launch_any(int mode, const GroupArgs &a, hipStream_t s) {
   }
   const int64_t blocks = tile_blocks(a.M, a.G, 64, NT);
   if (blocks > kMaxBlocks) return hipErrorInvalidConfiguration;
-  if (mode == GROUP_FWD)
-    hipLaunchKernelGGL((group_any_kernel<T, GROUP_FWD>), dim3((uint32_t)blocks), dim3(256), 0, s, a, NT);
-  else
-    hipLaunchKernelGGL((group_any_kernel<T, GROUP_DX>), dim3((uint32_t)blocks), dim3(256), 0, s, a, NT);
+  const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(256), 0, s, a, NT); };
+  if (mode == GROUP_FWD) launch(group_any_kernel<T, GROUP_FWD>);
+  else if (mode == GROUP_DX) launch(group_any_kernel<T, GROUP_DX>);
+  else if (mode == GROUP_GATED) launch(group_any_kernel<T, GROUP_GATED>);
+  else launch(group_any_kernel<T, GROUP_GATED_GRAD>);
   return hipGetLastError();
 }
 
@@ -283,6 +309,8 @@ GroupPieces group_pieces(int dtype, int G, int64_t rows, int n, int k) {
 
 hipError_t launch_group(int dtype, int mode, const GroupArgs &a, hipStream_t s) {
   hipError_t e;
+  if (mode == GROUP_GATED || mode == GROUP_GATED_GRAD)
+    return dtype == GCPSL_BF16 ? launch_any<bf16_t>(mode, a, s) : launch_any<float>(mode, a, s);
   if (group_few_ok(dtype, a, mode)) e = launch_group_few(dtype, mode, a, s);
   else if (group_tile_ok(dtype, a, mode) && fills_half(a, mode)) e = launch_group_tile(mode, a, s);
   else if (group_mid_ok(dtype, a, mode)) e = launch_group_mid(mode, a, s);

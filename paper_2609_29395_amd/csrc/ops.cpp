@@ -132,6 +132,67 @@ extern "C" int gcpsl_group_input_grad(int32_t dtype, int32_t G, int64_t rows, in
 }
 
 namespace {
+const char *bad_act(int act) { return act < GCPSL_SILU || act > GCPSL_RELU ? "unknown activation" : nullptr; }
+// Pairs have twice the columns.
+const char *bad_pairs(int n) { return n > kMaxCols / 2 ? "n must lie in [1, 2^27]" : nullptr; }
+}  // namespace
+
+extern "C" int gcpsl_group_gated_forward(int32_t dtype, int32_t G, int64_t rows, int32_t n, int32_t k,
+                                         const int32_t *offsets, const void *x, int64_t ldx, const void *w,
+                                         int64_t w_gs, const float *bias, int64_t bias_gs, int32_t act, void *y,
+                                         int64_t ldy, void *pre, int64_t ldpre, void *stream) {
+  gcpsl_clear_error();
+  CHECK_GROUPS(dtype, G, rows, n, k, offsets);
+  CHECK(bad_pairs(n));
+  CHECK(bad_act(act));
+  const size_t e = elem_bytes(dtype);
+  CHECK(bad_tensor(x, e, rows, k, ldx, false));
+  CHECK(bad_tensor(w, e, G, k, k, false));
+  CHECK(bad_stride(w_gs));
+  CHECK(bad_stride(bias_gs));
+  if (!aligned(bias, 4)) return fail(GCPSL_EINVAL, "tensor not aligned to its elements");
+  CHECK(bad_tensor(y, e, rows, n, ldy, true));
+  if (pre) CHECK(bad_tensor(pre, e, rows, 2 * (int64_t)n, ldpre, true));
+  if (rows == 0) return GCPSL_OK;
+  GroupArgs a{};
+  a.off = offsets;
+  a.G = G; a.M = (int)rows; a.N = n; a.Q = k;
+  a.a = x; a.lda = ldx;
+  a.b = w; a.ldb = k; a.b_gs = w_gs;
+  a.out = y; a.ldo = ldy;
+  a.bias = bias; a.bias_gs = bias_gs;
+  a.act = act;
+  a.pre = pre; a.ldp = ldpre;
+  return launched(launch_group(dtype, GROUP_GATED, a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+extern "C" int gcpsl_group_gated_grad(int32_t dtype, int32_t G, int64_t rows, int32_t m, int32_t n,
+                                      const int32_t *offsets, const void *dz, int64_t lddz, const void *v,
+                                      int64_t v_gs, int32_t act, const void *pre, int64_t ldpre, void *dpre,
+                                      int64_t lddpre, void *stream) {
+  gcpsl_clear_error();
+  CHECK_GROUPS(dtype, G, rows, m, n, offsets);
+  CHECK(bad_pairs(n));
+  CHECK(bad_act(act));
+  const size_t e = elem_bytes(dtype);
+  CHECK(bad_tensor(dz, e, rows, m, lddz, false));
+  CHECK(bad_tensor(v, e, G, n, n, false));
+  CHECK(bad_stride(v_gs));
+  CHECK(bad_tensor(pre, e, rows, 2 * (int64_t)n, ldpre, false));
+  CHECK(bad_tensor(dpre, e, rows, 2 * (int64_t)n, lddpre, true));
+  if (rows == 0) return GCPSL_OK;
+  GroupArgs a{};
+  a.off = offsets;
+  a.G = G; a.M = (int)rows; a.N = n; a.Q = m;
+  a.a = dz; a.lda = lddz;
+  a.b = v; a.ldb = n; a.b_gs = v_gs;
+  a.out = dpre; a.ldo = lddpre;
+  a.act = act;
+  a.pre = const_cast<void *>(pre); a.ldp = ldpre;
+  return launched(launch_group(dtype, GROUP_GATED_GRAD, a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+namespace {
 // Partials of a weight gradient: the weights' and then the biases'.
 size_t partial_bytes(const GroupPieces &p, int n, int k) { return sizeof(float) * (size_t)p.slots * n * ((size_t)k + 1); }
 }  // namespace
@@ -250,4 +311,198 @@ extern "C" int gcpsl_score_grad(int32_t dtype, int64_t rows, int32_t L, const vo
   if (rows == 0) return GCPSL_OK;
   const ScoreGradArgs a{z, ldz, rows, L, labels, lse, entropy, g_logp, g_entropy, dz, lddz};
   return launched(launch_score_grad(dtype, a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+namespace {
+const char *bad_residual(int dtype, int G, int64_t rows, int n, const int32_t *offsets) {
+  return bad_groups(dtype, G, rows, n, 1, offsets);
+}
+// Vectors [n] fp32 of every group; `out` ones must not overlap.
+const char *bad_vectors(const float *p, int64_t gs, int G, int n, bool out) {
+  if (!aligned(p, 4)) return "tensor not aligned to its elements";
+  if (const char *why = bad_stride(gs)) return why;
+  return p && out && G > 1 && gs < n ? "groups of an output overlap" : nullptr;
+}
+bool finite_f32(double v) { return std::fabs(v) <= 3.0e38; }  // (false for a NaN)
+size_t residual_bytes(const GroupPieces &p, int n) { return sizeof(float) * 2 * (size_t)p.slots * (size_t)n; }
+}  // namespace
+
+extern "C" int gcpsl_group_residual_norm(int32_t dtype, int32_t G, int64_t rows, int32_t n, const int32_t *offsets,
+                                         const void *x, int64_t ldx, const void *y, int64_t ldy, const void *gate,
+                                         int64_t ldgate, const float *w_block, int64_t w_block_gs, const float *w_next,
+                                         int64_t w_next_gs, double alpha, double beta, double eps, void *out,
+                                         int64_t ldo, void *h, int64_t ldh, float *r_block, float *r_next,
+                                         void *stream) {
+  gcpsl_clear_error();
+  CHECK(bad_residual(dtype, G, rows, n, offsets));
+  const size_t e = elem_bytes(dtype);
+  CHECK(bad_tensor(x, e, rows, n, ldx, false));
+  if (rows > 0 && !y && (gate || w_block || out || alpha != 1.0))
+    return fail(GCPSL_EINVAL, "no block output: gate, w_block and out must be null and alpha 1");
+  if (y) {
+    CHECK(bad_tensor(y, e, rows, n, ldy, false));
+    CHECK(bad_tensor(out, e, rows, n, ldo, true));
+    if (out && out == x && rows > 1 && ldo != ldx) return fail(GCPSL_EINVAL, "in place needs equal row strides");
+  }
+  if (gate) CHECK(bad_tensor(gate, e, rows, n, ldgate, false));
+  CHECK(bad_vectors(w_block, w_block_gs, G, n, false));
+  CHECK(bad_vectors(w_next, w_next_gs, G, n, false));
+  if (rows > 0 && !w_next != !h) return fail(GCPSL_EINVAL, "w_next and h come together");
+  if (rows > 0 && !y && !w_next) return fail(GCPSL_EINVAL, "nothing to compute");
+  if (h) CHECK(bad_tensor(h, e, rows, n, ldh, true));
+  if (!aligned(r_block, 4) || !aligned(r_next, 4)) return fail(GCPSL_EINVAL, "tensor not aligned to its elements");
+  if (!finite_f32(alpha) || !finite_f32(beta)) return fail(GCPSL_EINVAL, "alpha and beta must be finite");
+  if (!(eps >= std::ldexp(1.0, -100) && eps <= std::ldexp(1.0, 100)))
+    return fail(GCPSL_EINVAL, "eps must lie in [2^-100, 2^100]");
+  if (rows == 0) return GCPSL_OK;
+  ResidualArgs a{};
+  a.off = offsets;
+  a.G = G; a.n = n; a.rows = rows;
+  a.x = x; a.ldx = ldx;
+  a.y = y; a.ldy = ldy;
+  a.gate = gate; a.ldg = ldgate;
+  a.w_block = w_block; a.wb_gs = w_block_gs;
+  a.w_next = w_next; a.wn_gs = w_next_gs;
+  a.alpha = (float)alpha; a.beta = (float)beta; a.eps = (float)eps;
+  a.out = out; a.ldo = ldo;
+  a.h = h; a.ldh = ldh;
+  a.r_block = w_block ? r_block : nullptr;
+  a.r_next = w_next ? r_next : nullptr;
+  return launched(launch_residual(dtype, a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+extern "C" int gcpsl_group_residual_workspace_bytes(int32_t dtype, int32_t G, int64_t rows, int32_t n, size_t *bytes) {
+  gcpsl_clear_error();
+  if (!bytes) return fail(GCPSL_EINVAL, "null output");
+  alignas(4) static const int32_t none = 0;
+  CHECK(bad_residual(dtype, G, rows, n, &none));
+  if (rows > kMaxGroupRows) return fail(GCPSL_EUNSUPPORTED, "more than 2^31 - 1024 grouped rows");
+  *bytes = residual_bytes(residual_pieces(G, rows, n), n);
+  return GCPSL_OK;
+}
+
+extern "C" int gcpsl_group_residual_norm_grad(
+    int32_t dtype, int32_t G, int64_t rows, int32_t n, const int32_t *offsets, const void *out, int64_t ldo,
+    const void *g_out, int64_t ldgo, const void *g_h, int64_t ldgh, const void *y, int64_t ldy, const void *gate,
+    int64_t ldgate, const float *w_block, int64_t w_block_gs, const float *w_next, int64_t w_next_gs,
+    const float *r_block, const float *r_next, double alpha, double beta, void *dx, int64_t lddx, void *dy,
+    int64_t lddy, void *dgate, int64_t lddgate, float *dw_block, int64_t dw_block_gs, float *dw_next,
+    int64_t dw_next_gs, void *workspace, size_t workspace_bytes, void *stream) {
+  gcpsl_clear_error();
+  CHECK(bad_residual(dtype, G, rows, n, offsets));
+  if (rows > kMaxGroupRows) return fail(GCPSL_EUNSUPPORTED, "more than 2^31 - 1024 grouped rows");
+  const size_t e = elem_bytes(dtype);
+  if (rows > 0) {
+    if (!g_out && !g_h) return fail(GCPSL_EINVAL, "no gradient given");
+    if (!g_h != !w_next || (g_h && (!r_next || !out))) return fail(GCPSL_EINVAL, "g_h, w_next, r_next and out come together");
+    if (!y && (gate || w_block || dy || alpha != 1.0))
+      return fail(GCPSL_EINVAL, "no block output: gate, w_block and dy must be null and alpha 1");
+    if (w_block && !r_block) return fail(GCPSL_EINVAL, "null r_block");
+  }
+  if ((dgate && !gate) || (dw_block && !w_block) || (dw_next && !w_next))
+    return fail(GCPSL_EINVAL, "a gradient of what is not given");
+  if (g_h) CHECK(bad_tensor(out, e, rows, n, ldo, false));
+  if (g_out) CHECK(bad_tensor(g_out, e, rows, n, ldgo, false));
+  if (g_h) CHECK(bad_tensor(g_h, e, rows, n, ldgh, false));
+  if (y) {
+    CHECK(bad_tensor(y, e, rows, n, ldy, false));
+    CHECK(bad_tensor(dy, e, rows, n, lddy, true));
+  }
+  if (gate) CHECK(bad_tensor(gate, e, rows, n, ldgate, false));
+  CHECK(bad_vectors(w_block, w_block_gs, G, n, false));
+  CHECK(bad_vectors(w_next, w_next_gs, G, n, false));
+  CHECK(bad_tensor(dx, e, rows, n, lddx, true));
+  if (dgate) CHECK(bad_tensor(dgate, e, rows, n, lddgate, true));
+  CHECK(bad_vectors(dw_block, dw_block_gs, G, n, true));
+  CHECK(bad_vectors(dw_next, dw_next_gs, G, n, true));
+  if (!aligned(r_block, 4) || !aligned(r_next, 4)) return fail(GCPSL_EINVAL, "tensor not aligned to its elements");
+  if (!finite_f32(alpha) || !finite_f32(beta)) return fail(GCPSL_EINVAL, "alpha and beta must be finite");
+  const GroupPieces pieces = residual_pieces(G, rows, n);
+  if (dw_block || dw_next) {
+    if (residual_bytes(pieces, n) > workspace_bytes) return fail(GCPSL_EINVAL, "workspace too small");
+    if (pieces.slots && (!workspace || !aligned(workspace, 16)))
+      return fail(GCPSL_EINVAL, "workspace null or not 16-byte aligned");
+  }
+  if (rows == 0 && !dw_block && !dw_next) return GCPSL_OK;
+  ResidualGradArgs a{};
+  a.off = offsets;
+  a.G = G; a.n = n; a.rows = rows;
+  a.x = out; a.ldx = ldo;
+  a.g_out = g_out; a.ldgo = ldgo;
+  a.g_h = g_h; a.ldgh = ldgh;
+  a.y = y; a.ldy = ldy;
+  a.gate = gate; a.ldg = ldgate;
+  a.w_block = w_block; a.wb_gs = w_block_gs;
+  a.w_next = w_next; a.wn_gs = w_next_gs;
+  a.r_block = r_block; a.r_next = r_next;
+  a.alpha = (float)alpha; a.beta = (float)beta;
+  a.dx = dx; a.lddx = lddx;
+  a.dy = dy; a.lddy = lddy;
+  a.dgate = dgate; a.lddg = lddgate;
+  a.dw_block = dw_block; a.dwb_gs = dw_block_gs;
+  a.dw_next = dw_next; a.dwn_gs = dw_next_gs;
+  a.piece = pieces.piece;
+  a.slots = pieces.slots;
+  a.part = (float *)workspace;
+  return launched(launch_residual_grad(dtype, a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+namespace {
+const char *bad_teacher(int64_t rows, int top, const int32_t *t_class, const float *t_value, double temperature) {
+  if (top < 1 || top > kMaxTeacher) return "top must lie in [1, 256]";
+  if (rows > 0 && (!t_class || !t_value)) return "null teacher";
+  if (!aligned(t_class, 4) || !aligned(t_value, 4)) return "tensor not aligned to its elements";
+  return !(temperature >= 1.0 / 1024 && temperature <= 1024.0) ? "temperature must lie in [2^-10, 2^10]" : nullptr;
+}
+}  // namespace
+
+extern "C" int gcpsl_distill_workspace_bytes(int32_t dtype, int64_t rows, int32_t L, size_t *bytes) {
+  gcpsl_clear_error();
+  if (!bytes) return fail(GCPSL_EINVAL, "null output");
+  CHECK(bad_rows(dtype, rows, L));
+  *bytes = distill_work_bytes(dtype, rows, L);
+  return GCPSL_OK;
+}
+
+extern "C" int gcpsl_distill(int32_t dtype, int64_t rows, int32_t L, const void *z, int64_t ldz, int32_t top,
+                             const int32_t *t_class, const float *t_value, double temperature, const int32_t *labels,
+                             float *kl, float *lse_t, float *logp, float *lse, void *workspace, size_t workspace_bytes,
+                             void *stream) {
+  gcpsl_clear_error();
+  CHECK(bad_rows(dtype, rows, L));
+  CHECK(bad_tensor(z, elem_bytes(dtype), rows, L, ldz, false));
+  CHECK(bad_teacher(rows, top, t_class, t_value, temperature));
+  if (rows > 0 && logp && !labels) return fail(GCPSL_EINVAL, "log probabilities need labels");
+  for (const void *p : {(const void *)labels, (const void *)kl, (const void *)lse_t, (const void *)logp,
+                        (const void *)lse})
+    if (!aligned(p, 4)) return fail(GCPSL_EINVAL, "tensor not aligned to its elements");
+  const size_t need = distill_work_bytes(dtype, rows, L);
+  if (workspace_bytes < need || (need && (!workspace || !aligned(workspace, 16))))
+    return fail(GCPSL_EINVAL, "workspace null, too small or not 16-byte aligned");
+  if (rows == 0) return GCPSL_OK;
+  const DistillArgs a{z,  ldz,   rows, L,   top,      t_class, t_value, (float)temperature,
+                      labels, kl, lse_t, logp, lse, workspace};
+  return launched(launch_distill(dtype, a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+extern "C" int gcpsl_distill_grad(int32_t dtype, int64_t rows, int32_t L, const void *z, int64_t ldz, int32_t top,
+                                  const int32_t *t_class, const float *t_value, double temperature,
+                                  const int32_t *labels, const float *lse_t, const float *lse, const float *g_kl,
+                                  const float *g_logp, void *dz, int64_t lddz, void *stream) {
+  gcpsl_clear_error();
+  CHECK(bad_rows(dtype, rows, L));
+  CHECK(bad_tensor(z, elem_bytes(dtype), rows, L, ldz, false));
+  CHECK(bad_tensor(dz, elem_bytes(dtype), rows, L, lddz, true));
+  if (z && z == dz && rows > 1 && ldz != lddz) return fail(GCPSL_EINVAL, "in place needs equal row strides");
+  if (rows > 0 && !g_kl && !g_logp) return fail(GCPSL_EINVAL, "no gradient given");
+  CHECK(bad_teacher(g_kl ? rows : 0, top, t_class, t_value, temperature));
+  if (rows > 0 && g_kl && !lse_t) return fail(GCPSL_EINVAL, "null lse_t");
+  if (rows > 0 && g_logp && (!labels || !lse)) return fail(GCPSL_EINVAL, "log probabilities need labels and lse");
+  for (const void *p : {(const void *)labels, (const void *)lse_t, (const void *)lse, (const void *)g_kl,
+                        (const void *)g_logp})
+    if (!aligned(p, 4)) return fail(GCPSL_EINVAL, "tensor not aligned to its elements");
+  if (rows == 0) return GCPSL_OK;
+  const DistillGradArgs a{z,      ldz,   rows, L,    top,    t_class, t_value, (float)temperature,
+                          labels, lse_t, lse,  g_kl, g_logp, dz,      lddz};
+  return launched(launch_distill_grad(dtype, a, reinterpret_cast<hipStream_t>(stream)));
 }

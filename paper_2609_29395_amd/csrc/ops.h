@@ -40,7 +40,11 @@ hipError_t launch_dropout(int dtype, int64_t rows, int64_t cols, const void *x, 
 //   forward      A = x rows,  q = input feature,  B(c, q) = w_g[c][q]
 //   input grad   A = dy rows, q = output feature, B(c, q) = w_g[q][c]
 //   weight grad  A(m, q) = dy[q][m], B(c, q) = x[q][c], q = row of the group
-enum GroupMode { GROUP_FWD = 0, GROUP_DX = 1, GROUP_DW = 2 };
+// Gated layers: forward with two sums a column, those of w_g's rows c (the gate)
+// and N + c (the value); gradient: an input gradient by the pair of sums.
+enum GroupMode { GROUP_FWD = 0, GROUP_DX = 1, GROUP_DW = 2, GROUP_GATED = 3, GROUP_GATED_GRAD = 4 };
+// Whether the rows of operand b run across the sum, columns [c][q] of it lying q apart from row to row.
+constexpr bool group_across(int mode) { return mode != GROUP_FWD && mode != GROUP_GATED; }
 struct GroupArgs {
   const int32_t *off;  // device [G + 1]
   int G, M, N, Q;      // M: rows of the tensors (weight grad: output features), N columns of out; Q: length of
@@ -61,6 +65,10 @@ struct GroupArgs {
   // go to partials, [slots][M][N] and [slots][M]
   int piece, slots;
   float *part, *part_db;
+  // gated layers
+  int act;       // GCPSL_SILU, ..
+  void *pre;     // [rows][2 N], pairs of sums: forward writes them (or null), the gradient reads them
+  int64_t ldp;
 };
 // Rows of a piece of a weight gradient's sums and the partials that this can make (host).
 struct GroupPieces {
@@ -68,6 +76,72 @@ struct GroupPieces {
 };
 GroupPieces group_pieces(int dtype, int G, int64_t rows, int n, int k);
 hipError_t launch_group(int dtype, int mode, const GroupArgs &a, hipStream_t s);
+
+// ------------------------------------------- residual updates and row norms
+// out = alpha x + beta sigmoid(gate) t, t = w_block y r_block (or y); h = w_next out r_next.
+struct ResidualArgs {
+  const int32_t *off;  // device [G + 1]
+  int G, n;
+  int64_t rows;
+  const void *x, *y, *gate;  // y, gate: or null
+  int64_t ldx, ldy, ldg;
+  const float *w_block, *w_next;  // [G] rows of n, or null
+  int64_t wb_gs, wn_gs;
+  float alpha, beta, eps;
+  void *out, *h;  // or null
+  int64_t ldo, ldh;
+  float *r_block, *r_next;  // or null
+};
+hipError_t launch_residual(int dtype, const ResidualArgs &a, hipStream_t s);
+struct ResidualGradArgs {
+  const int32_t *off;
+  int G, n;
+  int64_t rows;
+  const void *x, *g_out, *g_h, *y, *gate;  // x: the forward pass's out; all or null
+  int64_t ldx, ldgo, ldgh, ldy, ldg;
+  const float *w_block, *w_next, *r_block, *r_next;
+  int64_t wb_gs, wn_gs;
+  float alpha, beta;
+  void *dx, *dy, *dgate;  // dy, dgate: or null
+  int64_t lddx, lddy, lddg;
+  float *dw_block, *dw_next;  // or null
+  int64_t dwb_gs, dwn_gs;
+  // a group of c rows is taken in max(1, round(c / piece)) pieces; the weight gradients of those of more than one go
+  // to partials [slots][2][n]
+  int piece, slots;
+  float *part;
+};
+GroupPieces residual_pieces(int G, int64_t rows, int n);
+hipError_t launch_residual_grad(int dtype, const ResidualGradArgs &a, hipStream_t s);
+
+// ------------------------------------------------------------ distillation
+constexpr int kMaxTeacher = 256;
+struct DistillArgs {
+  const void *z;
+  int64_t ldz, rows;
+  int L, top;
+  const int32_t *t_class;
+  const float *t_value;
+  float temperature;
+  const int32_t *labels;  // or null
+  float *kl, *lse_t, *logp, *lse;  // or null
+  void *work;
+};
+size_t distill_work_bytes(int dtype, int64_t rows, int L);
+hipError_t launch_distill(int dtype, const DistillArgs &a, hipStream_t s);
+struct DistillGradArgs {
+  const void *z;
+  int64_t ldz, rows;
+  int L, top;
+  const int32_t *t_class;
+  const float *t_value;
+  float temperature;
+  const int32_t *labels;  // or null
+  const float *lse_t, *lse, *g_kl, *g_logp;
+  void *dz;
+  int64_t lddz;
+};
+hipError_t launch_distill_grad(int dtype, const DistillGradArgs &a, hipStream_t s);
 
 // ------------------------------------------------------------ label scores
 constexpr int kMaxTop = 32;

@@ -23,6 +23,7 @@ RULES = {"random": 0, "size": 1, "label_l1": 2, "label_jsd": 3}
 DTYPES = {"f32": 0, "bf16": 1}
 CONV3X3, MAXPOOL2, AVGPOOL, LINEAR, BATCHNORM, GROUPNORM, BLOCK = 1, 2, 3, 4, 5, 6, 7
 RESIDUAL, STRIDE2 = 1, 2
+ACTS = {"silu": 0, "gelu": 1, "relu": 2}
 SCHEDULES = {"lockstep": 0, "epoch": 1}
 PAYLOAD = ("activations", "cut_grads", "client_grads", "client_model", "fusion")  # GCPSL_PAYLOAD_* order
 
@@ -33,7 +34,10 @@ EXPORTS = ["gcpsl_param_count", "gcpsl_state_count", "gcpsl_workspace_bytes", "g
            "gcpsl_participation", "gcpsl_batch_deviation", "gcpsl_payload",
            "gcpsl_cluster_sizes", "gcpsl_tensor", "gcpsl_timing", "gcpsl_timing_read",
            "gcpsl_group_forward", "gcpsl_group_input_grad", "gcpsl_group_workspace_bytes", "gcpsl_group_weight_grad",
+           "gcpsl_group_gated_forward", "gcpsl_group_gated_grad", "gcpsl_group_residual_norm",
+           "gcpsl_group_residual_workspace_bytes", "gcpsl_group_residual_norm_grad",
            "gcpsl_dropout", "gcpsl_score_workspace_bytes", "gcpsl_score", "gcpsl_score_grad",
+           "gcpsl_distill_workspace_bytes", "gcpsl_distill", "gcpsl_distill_grad",
            "gcpsl_destroy", "gcpsl_last_error"]
 
 
@@ -112,6 +116,17 @@ def lib():
     L.gcpsl_score_workspace_bytes.argtypes = [i32, i64, i32, i32, P(size)]
     L.gcpsl_score.argtypes = [i32, i64, i32, vp, i64, vp, i32, vp, vp, vp, vp, vp, vp, size, vp]
     L.gcpsl_score_grad.argtypes = [i32, i64, i32, vp, i64, vp, vp, vp, vp, vp, vp, i64, vp]
+    L.gcpsl_group_gated_forward.argtypes = group + [vp, i64, vp, i64, vp, i64, i32, vp, i64, vp, i64, vp]
+    L.gcpsl_group_gated_grad.argtypes = group + [vp, i64, vp, i64, i32, vp, i64, vp, i64, vp]
+    norm = [i32, i32, i64, i32, vp]  # dtype, G, rows, n, offsets
+    tensor = [vp, i64]
+    L.gcpsl_group_residual_norm.argtypes = norm + 5 * tensor + [f64, f64, f64] + 2 * tensor + [vp, vp, vp]
+    L.gcpsl_group_residual_workspace_bytes.argtypes = norm[:4] + [P(size)]
+    L.gcpsl_group_residual_norm_grad.argtypes = norm + 7 * tensor + [vp, vp, f64, f64] + 5 * tensor + [vp, size, vp]
+    teacher = [i32, vp, vp, f64]  # top, classes, values, temperature
+    L.gcpsl_distill_workspace_bytes.argtypes = [i32, i64, i32, P(size)]
+    L.gcpsl_distill.argtypes = [i32, i64, i32, vp, i64] + teacher + [vp, vp, vp, vp, vp, vp, size, vp]
+    L.gcpsl_distill_grad.argtypes = [i32, i64, i32, vp, i64] + teacher + [vp, vp, vp, vp, vp, vp, i64, vp]
     L.gcpsl_destroy.argtypes = [vp]
     L.gcpsl_destroy.restype = None
     L.gcpsl_last_error.restype = C.c_char_p
@@ -210,7 +225,10 @@ _torch = None
 _types = {}
 _ops = None
 _ENTRIES = ["gcpsl_group_forward", "gcpsl_group_input_grad", "gcpsl_group_workspace_bytes", "gcpsl_group_weight_grad",
-            "gcpsl_dropout", "gcpsl_score_workspace_bytes", "gcpsl_score", "gcpsl_score_grad"]
+            "gcpsl_dropout", "gcpsl_score_workspace_bytes", "gcpsl_score", "gcpsl_score_grad",
+            "gcpsl_group_gated_forward", "gcpsl_group_gated_grad", "gcpsl_group_residual_norm",
+            "gcpsl_group_residual_workspace_bytes", "gcpsl_group_residual_norm_grad",
+            "gcpsl_distill_workspace_bytes", "gcpsl_distill", "gcpsl_distill_grad"]
 
 
 def _load_torch():
@@ -229,7 +247,7 @@ def _native():
         from . import _ops as module
         L = lib()
         module.init(tuple(C.cast(getattr(L, name), C.c_void_p).value for name in _ENTRIES), torch._C._cuda_getDevice,
-                    torch._C._cuda_getCurrentRawStream, Scores)
+                    torch._C._cuda_getCurrentRawStream, (Scores, Gated, Residual, ResidualGrads, Distilled))
         _ops = module
     return _ops
 
@@ -487,6 +505,245 @@ def score_grad(logits, labels, lse, entropy=None, g_logp=None, g_entropy=None, o
                                   _vector(entropy, "entropy", f32, rows, device),
                                   _vector(g_logp, "g_logp", f32, rows, device),
                                   _vector(g_entropy, "g_entropy", f32, rows, device), dp, lddz, handle))
+    return dz
+
+
+class Gated(NamedTuple):
+    y: object    # [rows][n]
+    pre: object  # [rows][2 n] the gates' and the values' sums (None if not kept)
+
+
+def _act(act):
+    code = ACTS.get(act) if isinstance(act, str) else None
+    if code is None:
+        raise ValueError(f"act must be one of {', '.join(ACTS)}, is {act!r}")
+    return code
+
+
+def group_gated_forward(x, offsets, w, bias=None, act="silu", keep=False, out=None, pre=None, stream=None):
+    """gcpsl_group_gated_forward: y [rows][n] = f(g) u of x [rows][k], (g, u)
+    = W_g x_r + b_g with w [G][2 n][k], the gates' rows and then the values',
+    and bias [G][2 n] (fp32); act is f: "silu", "gelu" or "relu".  With keep
+    (or a tensor for it) the pairs come too, for group_gated_grad."""
+    code_act = _act(act)
+    if stream is None:
+        r = (_ops or _native()).group_gated_forward(x, offsets, w, bias, code_act, keep, out, pre)
+        if _done(r):
+            return r
+    torch, code, handle, device = _begin(x, stream)
+    dtype = x.dtype
+    xp, ldx = _rows(x, "x", dtype, device)
+    off, G = _offsets(offsets, torch, device)
+    rows, k = x.shape
+    n2 = w.shape[1] if w.dim() == 3 else -1
+    wp, w_gs = _weights(w, "w", dtype, device, (G, n2, k))
+    if n2 % 2:
+        raise ValueError("w must have a row for every gate and value: an even number")
+    n = n2 // 2
+    bp, b_gs = (None, 0) if bias is None else _weights(bias, "bias", torch.float32, device, (G, n2))
+    y, yp, ldy = _out(x, out, rows, n, dtype, device, stream)
+    pp, ldp = None, 0
+    if keep or pre is not None:
+        pre, pp, ldp = _out(x, pre, rows, n2, dtype, device, stream)
+    _check(lib().gcpsl_group_gated_forward(code, G, rows, n, k, off, xp, ldx, wp, w_gs, bp, b_gs, code_act, yp, ldy, pp,
+                                           ldp, handle))
+    return Gated(y, pre)
+
+
+def group_gated_grad(dz, offsets, w, pre, act="silu", out=None, stream=None):
+    """gcpsl_group_gated_grad: the gradient [rows][2 n] by a gated layer's
+    pairs `pre`, given that of the layer after it, dz [rows][m], and its
+    weights w [G][m][n].  group_input_grad and group_weight_grad of the result
+    with the gated layer's own weights and input are the rest of its backward
+    pass."""
+    code_act = _act(act)
+    if stream is None:
+        r = (_ops or _native()).group_gated_grad(dz, offsets, w, pre, code_act, out)
+        if _done(r):
+            return r
+    torch, code, handle, device = _begin(dz, stream)
+    dtype = dz.dtype
+    dp, lddz = _rows(dz, "dz", dtype, device)
+    off, G = _offsets(offsets, torch, device)
+    rows, m = dz.shape
+    n = w.shape[2] if w.dim() == 3 else -1
+    wp, w_gs = _weights(w, "w", dtype, device, (G, m, n))
+    pp, ldp = _rows(pre, "pre", dtype, device, rows, 2 * n)
+    d, op, ldo = _out(dz, out, rows, 2 * n, dtype, device, stream)
+    _check(lib().gcpsl_group_gated_grad(code, G, rows, m, n, off, dp, lddz, wp, w_gs, code_act, pp, ldp, op, ldo, handle))
+    return d
+
+
+class Residual(NamedTuple):
+    out: object      # [rows][n] the updated rows (x itself without a block's output)
+    h: object        # [rows][n] the next block's input (None without w_next)
+    r_block: object  # [rows] reciprocal rms of the block's output (None without w_block)
+    r_next: object   # [rows] of the updated rows (None without w_next)
+
+
+class ResidualGrads(NamedTuple):
+    dx: object        # [rows][n]
+    dy: object        # (each None without what it is the gradient of)
+    dgate: object
+    dw_block: object  # [G][n] fp32
+    dw_next: object
+
+
+def group_residual_norm(x, offsets, y=None, gate=None, w_block=None, w_next=None, alpha=1.0, beta=1.0, eps=1e-6,
+                        out=None, h=None, stream=None):
+    """gcpsl_group_residual_norm: out = alpha x + beta sigmoid(gate) (w_block y
+    / rms(y)) and h = w_next out / rms(out) of [rows][n] tensors and [G][n]
+    fp32 weights; without w_block the block's output y as it is, without gate
+    1, without w_next no h, without y the norm of x alone.  out may be x."""
+    if stream is None:
+        r = (_ops or _native()).group_residual_norm(x, offsets, y, gate, w_block, w_next, alpha, beta, eps, out, h)
+        if _done(r):
+            return r
+    torch, code, handle, device = _begin(x, stream)
+    dtype, f32 = x.dtype, torch.float32
+    xp, ldx = _rows(x, "x", dtype, device)
+    off, G = _offsets(offsets, torch, device)
+    rows, n = x.shape
+    yp, ldy = (None, 0) if y is None else _rows(y, "y", dtype, device, rows, n)
+    gp, ldg = (None, 0) if gate is None else _rows(gate, "gate", dtype, device, rows, n)
+    b1, s1 = (None, 0) if w_block is None else _weights(w_block, "w_block", f32, device, (G, n))
+    b2, s2 = (None, 0) if w_next is None else _weights(w_next, "w_next", f32, device, (G, n))
+    if (y is None and out is not None) or (w_next is None and h is not None):
+        raise ValueError("a tensor for a result that the call does not have")
+    new, op, ldo = (x, None, 0) if y is None else _out(x, out, rows, n, dtype, device, stream)
+    hp, ldh = None, 0
+    if w_next is not None:
+        h, hp, ldh = _out(x, h, rows, n, dtype, device, stream)
+    r1 = None if w_block is None else _empty(x, (rows,), f32, stream)
+    r2 = None if w_next is None else _empty(x, (rows,), f32, stream)
+    _check(lib().gcpsl_group_residual_norm(code, G, rows, n, off, xp, ldx, yp, ldy, gp, ldg, b1, s1, b2, s2, alpha, beta,
+                                           eps, op, ldo, hp, ldh, None if r1 is None else r1.data_ptr(),
+                                           None if r2 is None else r2.data_ptr(), handle))
+    return Residual(new, h, r1, r2)
+
+
+@functools.lru_cache(maxsize=1024)
+def _residual_workspace_bytes(code, G, rows, n):
+    b = C.c_size_t()
+    _check(lib().gcpsl_group_residual_workspace_bytes(code, G, rows, n, C.byref(b)))
+    return b.value
+
+
+def group_residual_workspace_bytes(dtype, G, rows, n):
+    """gcpsl_group_residual_workspace_bytes for "f32" or "bf16" tensors."""
+    return _residual_workspace_bytes(DTYPES[dtype], G, rows, n)
+
+
+def group_residual_norm_grad(out, offsets, g_out=None, g_h=None, y=None, gate=None, w_block=None, w_next=None,
+                             r_block=None, r_next=None, alpha=1.0, beta=1.0, workspace=None, stream=None):
+    """gcpsl_group_residual_norm_grad: the gradients by x, y, gate, w_block and
+    w_next, given those by out (g_out) and by h (g_h), of which one may be
+    None; the other tensors are the forward call's, r_block and r_next its
+    results."""
+    if stream is None and workspace is None:
+        r = (_ops or _native()).group_residual_norm_grad(out, offsets, g_out, g_h, y, gate, w_block, w_next, r_block,
+                                                         r_next, alpha, beta)
+        if _done(r):
+            return r
+    torch, code, handle, device = _begin(out, stream)
+    dtype, f32 = out.dtype, torch.float32
+    xp, ldx = _rows(out, "out", dtype, device)
+    off, G = _offsets(offsets, torch, device)
+    rows, n = out.shape
+    given = []
+    for t, what in ((g_out, "g_out"), (g_h, "g_h"), (y, "y"), (gate, "gate")):
+        given += (None, 0) if t is None else _rows(t, what, dtype, device, rows, n)
+    for t, what in ((w_block, "w_block"), (w_next, "w_next")):
+        given += (None, 0) if t is None else _weights(t, what, f32, device, (G, n))
+    dx = _empty(out, (rows, n), dtype, stream)
+    dy = None if y is None else _empty(out, (rows, n), dtype, stream)
+    dgate = None if gate is None else _empty(out, (rows, n), dtype, stream)
+    dw1 = None if w_block is None else _empty(out, (G, n), f32, stream)
+    dw2 = None if w_next is None else _empty(out, (G, n), f32, stream)
+    made = []
+    for t in (dx, dy, dgate, dw1, dw2):
+        made += (None, 0) if t is None else (t.data_ptr(), n)
+    need = _residual_workspace_bytes(code, G, rows, n) if dw1 is not None or dw2 is not None else 0
+    ptr, size, keep = _workspace(out, workspace, need, device, stream)
+    _check(lib().gcpsl_group_residual_norm_grad(code, G, rows, n, off, xp, ldx, *given,
+                                                _vector(r_block, "r_block", f32, rows, device),
+                                                _vector(r_next, "r_next", f32, rows, device), alpha, beta, *made, ptr,
+                                                size, handle))
+    return ResidualGrads(dx, dy, dgate, dw1, dw2)
+
+
+class Distilled(NamedTuple):
+    kl: object     # [rows] divergence from the teacher
+    logp: object   # [rows] log probability of each row's label (None without labels)
+    lse_t: object  # [rows] log sum of exponentials at the temperature
+    lse: object    # [rows] at 1 (None without labels)
+
+
+@functools.lru_cache(maxsize=1024)
+def _distill_workspace_bytes(code, rows, L):
+    b = C.c_size_t()
+    _check(lib().gcpsl_distill_workspace_bytes(code, rows, L, C.byref(b)))
+    return b.value
+
+
+def distill_workspace_bytes(dtype, rows, L):
+    """gcpsl_distill_workspace_bytes for "f32" or "bf16" logits."""
+    return _distill_workspace_bytes(DTYPES[dtype], rows, L)
+
+
+def _teacher(t_class, t_value, rows, torch, device):
+    """(top, addresses) of a teacher's classes and values, [rows][top] each."""
+    for t, what, dtype in ((t_class, "t_class", torch.int32), (t_value, "t_value", torch.float32)):
+        if t.dim() != 2 or t.shape != (rows, t_class.shape[1]) or t.dtype != dtype or t.get_device() != device \
+                or not t.is_contiguous():
+            raise ValueError(f"{what} must be a contiguous [rows][top] {dtype} tensor on the same GPU")
+    return t_class.shape[1], t_class.data_ptr(), t_value.data_ptr()
+
+
+def distill(logits, t_class, t_value, temperature=1.0, labels=None, workspace=None, stream=None):
+    """gcpsl_distill of logits [rows][L] and a teacher's best classes t_class
+    [rows][top] (int32) and their logits or log probabilities t_value (fp32),
+    what score's top_class and top_logp hold; with int32 labels [rows] their
+    log probabilities too."""
+    if stream is None and workspace is None:
+        r = (_ops or _native()).distill(logits, t_class, t_value, temperature, labels)
+        if _done(r):
+            return r
+    torch, code, handle, device = _begin(logits, stream)
+    zp, ldz = _rows(logits, "logits", logits.dtype, device)
+    rows, L = logits.shape
+    top, cp, vp = _teacher(t_class, t_value, rows, torch, device)
+    yp = _vector(labels, "labels", torch.int32, rows, device)
+    ptr, size, keep = _workspace(logits, workspace, _distill_workspace_bytes(code, rows, L), device, stream)
+    held = _empty(logits, (rows * (2 if labels is None else 4),), torch.float32, stream)
+    part = held.split(rows) if rows else (held,) * 4
+    kl, lse_t, logp, lse = (*part, None, None) if labels is None and rows else part
+    hp = held.data_ptr()
+    _check(lib().gcpsl_distill(code, rows, L, zp, ldz, top, cp, vp, temperature, yp, hp, hp + 4 * rows,
+                               *((None, None) if labels is None else (hp + 8 * rows, hp + 12 * rows)), ptr, size, handle))
+    return Distilled(kl, None, lse_t, None) if labels is None else Distilled(kl, logp, lse_t, lse)
+
+
+def distill_grad(logits, t_class, t_value, lse_t=None, temperature=1.0, labels=None, lse=None, g_kl=None, g_logp=None,
+                 out=None, stream=None):
+    """gcpsl_distill_grad: the loss's gradient by the logits [rows][L], given
+    those by kl (g_kl [rows]) and by logp (g_logp [rows]), of which one may be
+    None; out may be the logits."""
+    if stream is None:
+        r = (_ops or _native()).distill_grad(logits, t_class, t_value, lse_t, temperature, labels, lse, g_kl, g_logp, out)
+        if _done(r):
+            return r
+    torch, code, handle, device = _begin(logits, stream)
+    zp, ldz = _rows(logits, "logits", logits.dtype, device)
+    rows, L = logits.shape
+    top, cp, vp = _teacher(t_class, t_value, rows, torch, device)
+    yp = _vector(labels, "labels", torch.int32, rows, device)
+    f32 = torch.float32
+    dz, dp, lddz = _out(logits, out, rows, L, logits.dtype, device, stream)
+    _check(lib().gcpsl_distill_grad(code, rows, L, zp, ldz, top, cp, vp, temperature, yp,
+                                    _vector(lse_t, "lse_t", f32, rows, device), _vector(lse, "lse", f32, rows, device),
+                                    _vector(g_kl, "g_kl", f32, rows, device),
+                                    _vector(g_logp, "g_logp", f32, rows, device), dp, lddz, handle))
     return dz
 
 

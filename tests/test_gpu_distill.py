@@ -1,0 +1,204 @@
+"""Distillation from a teacher's best classes, and its gradient, on the GPU, against their 64-bit definition
+(tests/blocks_plain.py)."""
+import math
+
+import pytest
+import torch
+
+import blocks_plain as blocks
+from test_gpu_group import TYPES, gpu, make
+
+pytestmark = pytest.mark.gpu
+
+from paper_2609_29395_amd import gcpsl  # noqa: E402
+
+
+def check(got, want, bound, what=""):
+    """Within the bound; NaN and infinities where the definition has them."""
+    got = got.cpu().double()
+    far = ~torch.isfinite(want)
+    assert torch.equal(torch.isnan(got), torch.isnan(want)), what
+    same = far & ~torch.isnan(want)
+    assert torch.equal(got[same], want[same]), what
+    bad = ~far & ~((got - want).abs() <= bound)
+    assert not bad.any(), (what, int(bad.sum()), got[bad][:4], want[bad][:4], bound[bad][:4])
+
+
+def inputs(seed, rows, L, top, T, masked=False):
+    z = make(seed, rows, L, scale=3.0)
+    best = (z + make(seed + 1, rows, L, scale=2.0)).topk(min(top, L), 1)
+    gen = torch.Generator().manual_seed(seed + 2)
+    labels = torch.randint(-1, L, (rows,), generator=gen).int()
+    if masked:
+        out = torch.rand(rows, L, generator=gen) < 0.3
+        out.scatter_(1, best.indices, False)
+        z = z.masked_fill(out, -math.inf)
+    return z.to(T), best.indices.int().contiguous(), best.values.contiguous(), labels
+
+
+def run_both(z, cls, val, temperature, labels, what=""):
+    """Forward and gradient with the forward pass's own results, both checked."""
+    rows = z.shape[0]
+    got = gcpsl.distill(gpu(z), gpu(cls), gpu(val), temperature=temperature, labels=gpu(labels))
+    want = blocks.distill(z, cls, val, temperature, labels)
+    for k, v in got._asdict().items():
+        if k in want:
+            check(v, *want[k], (what, k))
+        else:
+            assert v is None
+    g_kl = make(9, rows) + 0.5
+    g_logp = None if labels is None else make(10, rows)
+    dz = gcpsl.distill_grad(gpu(z), gpu(cls), gpu(val), got.lse_t, temperature=temperature, labels=gpu(labels), lse=got.lse,
+                            g_kl=gpu(g_kl), g_logp=gpu(g_logp))
+    lse = None if got.lse is None else got.lse.cpu()
+    check(dz, *blocks.distill_grad(z, cls, val, got.lse_t.cpu(), temperature, labels, lse, g_kl, g_logp), (what, "dz"))
+    return got, dz
+
+
+# one class, fewer than a vector, 16 lanes' rows, a wave's, a workgroup's, several parts; odd numbers throughout
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,L,top", [(1, 1, 1), (3, 2, 2), (40, 10, 5), (17, 64, 64), (5, 65, 3), (9, 100, 100),
+                                        (33, 777, 20), (6, 1024, 32), (4, 1025, 256), (7, 2049, 8), (3, 5003, 17),
+                                        (1, 50021, 20), (2, 131072, 64), (1100, 300, 4), (600, 2100, 5)])
+def test_sizes(rows, L, top, dtype):
+    for i, (temperature, labelled) in enumerate([(1.0, True), (2.0, True), (0.5, False), (1.0, False)]):
+        if rows * L > 100000 and i > 1:
+            continue
+        z, cls, val, labels = inputs(100 + i, rows, L, top, TYPES[dtype], masked=i % 2 == 1)
+        run_both(z, cls, val, temperature, labels if labelled else None, (temperature, labelled))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("L", [10, 300, 5000])
+def test_teachers_of_every_kind(L, dtype):
+    """Entries left out, twice the same class, one class only, far apart values, the label among them."""
+    z, cls, val, labels = inputs(200, 12, L, 6, TYPES[dtype])
+    cls[0, :] = -1                      # no teacher
+    val[1, :] = -math.inf               # no teacher either
+    cls[2, 1:], cls[3, 2], cls[4, 0] = -1, L, 2 ** 31 - 1
+    cls[5, 1:4] = cls[5, 0]             # one class four times
+    cls[6, :] = cls[6, 0]               # one class throughout
+    val[7, 0], val[8, 1:] = 80.0, -3e38  # as good as one class
+    val[9, 2:] = -math.inf
+    labels[10] = cls[10, 0]
+    val[11] += 1e4                      # a shift changes nothing but the roundings
+    for temperature in (1.0, 3.0):
+        got, dz = run_both(z, cls, val, temperature, labels)
+        assert (got.kl[:2] == 0).all()
+        only = gcpsl.distill_grad(gpu(z), gpu(cls), gpu(val), got.lse_t, temperature=temperature,
+                                  g_kl=torch.ones(12, device="cuda"))
+        assert (only[:2] == 0).all() and (only[2:].abs().sum(1) > 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("L", [9, 90, 3000])
+def test_masks_infinities_and_nans(L, dtype):
+    T = TYPES[dtype]
+    z, cls, val, labels = inputs(300, 9, L, 4, T)
+    z[0] = -math.inf                        # nothing left
+    z[1] = torch.finfo(T).min               # nothing left, by a finite fill
+    z[2, cls[2, 1].long()] = -math.inf      # the teacher's class ruled out: kl infinite
+    z[3, 1] = math.nan
+    z[4, 2] = math.inf
+    z[5] = -1e30
+    z[5, cls[5].long()] = 1.0               # all but the teacher's classes ruled out by a finite fill
+    z[6] += 1000.0
+    val[7, 2] = math.nan
+    val[8, 0] = math.inf
+    labels[:] = 0
+    got = gcpsl.distill(gpu(z), gpu(cls), gpu(val), temperature=2.0, labels=gpu(labels))
+    kl = got.kl.cpu()
+    assert kl[0] == math.inf and kl[2] == math.inf and torch.isnan(kl[[3, 4, 7, 8]]).all()
+    assert got.lse_t[0] == -math.inf and got.logp[0] == -math.inf
+    one = torch.ones(9, device="cuda")
+    dz = gcpsl.distill_grad(gpu(z), gpu(cls), gpu(val), got.lse_t, temperature=2.0, labels=gpu(labels), lse=got.lse, g_kl=one,
+                            g_logp=one).cpu()
+    assert (dz[:2] == 0).all()
+    assert torch.isfinite(dz[[2, 5, 6]]).all() and torch.isnan(dz[[3, 4]]).any(1).all()
+    fine = [5, 6]
+    run_both(z[fine], cls[fine].contiguous(), val[fine].contiguous(), 2.0, labels[fine])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("L", [13, 203, 4099])
+def test_strides_in_place_and_what_lies_beside(L, dtype):
+    T = TYPES[dtype]
+    z, cls, val, labels = inputs(400, 7, L, 5, T)
+    wide = torch.full((8, L + 3), math.nan, dtype=T, device="cuda")
+    v = wide[:7, 1:L + 1]
+    v.copy_(z)
+    want, dz = run_both(z, cls, val, 2.0, labels)
+    got = gcpsl.distill(v, gpu(cls), gpu(val), temperature=2.0, labels=gpu(labels))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    g = {"g_kl": gpu(make(9, 7) + 0.5), "g_logp": gpu(make(10, 7))}
+    out = gcpsl.distill_grad(v, gpu(cls), gpu(val), got.lse_t, temperature=2.0, labels=gpu(labels), lse=got.lse, **g, out=v)
+    assert out is v and torch.equal(v, dz)
+    assert torch.isnan(wide[7]).all() and torch.isnan(wide[:, 0]).all() and torch.isnan(wide[:, L + 1:]).all()
+
+
+def test_workspaces_and_one_gradient_alone():
+    z, cls, val, labels = inputs(500, 3, 70000, 9, torch.bfloat16)
+    need = gcpsl.distill_workspace_bytes("bf16", 3, 70000)
+    assert need > 0 and gcpsl.distill_workspace_bytes("bf16", 3, 64) == 0
+    a = [gpu(t) for t in (z, cls, val)]
+    want = gcpsl.distill(*a, labels=gpu(labels))
+    got = gcpsl.distill(*a, labels=gpu(labels), workspace=torch.full((need,), 255, dtype=torch.uint8, device="cuda"))
+    assert all(torch.equal(u, v) for u, v in zip(got, want))
+    assert torch.equal(want.lse, want.lse_t)  # at temperature 1
+    g = make(1, 3)
+    dz = gcpsl.distill_grad(*a, labels=gpu(labels), lse=want.lse, g_logp=gpu(g))
+    check(dz, *blocks.distill_grad(z, cls, val, None, 1.0, labels, want.lse.cpu(), None, g))
+    with pytest.raises(gcpsl.GCPSLError):
+        gcpsl.distill(*a, workspace=torch.empty(need - 16, dtype=torch.uint8, device="cuda"))
+
+
+def test_teacher_from_scores():
+    """score's results are a teacher: a student that is its own teacher over all classes has divergence 0."""
+    z = gpu(make(600, 50, 20, scale=2.0))
+    s = gcpsl.score(z, top=20)
+    got = gcpsl.distill(z, s.top_class, s.top_logp)
+    assert got.kl.abs().max() <= 40 * 2.0 ** -24 * 16
+    dz = gcpsl.distill_grad(z, s.top_class, s.top_logp, got.lse_t, g_kl=torch.ones(50, device="cuda"))
+    assert dz.abs().max() <= 64 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("L", [11, 130, 2500])
+def test_gradients_against_differences(L):
+    z, cls, val, labels = inputs(700, 5, L, 6, torch.float32)
+    labels = labels.clamp(min=0)
+    a, b = make(1, 5).double(), make(2, 5).double()
+
+    def loss(z):
+        got = blocks.distill(z, cls, val, 2.0, labels)
+        return float((got["kl"][0] * a + got["logp"][0] * b).sum())
+
+    got = gcpsl.distill(gpu(z), gpu(cls), gpu(val), temperature=2.0, labels=gpu(labels))
+    dz = gcpsl.distill_grad(gpu(z), gpu(cls), gpu(val), got.lse_t, temperature=2.0, labels=gpu(labels), lse=got.lse,
+                            g_kl=gpu(a.float()), g_logp=gpu(b.float())).cpu().double()
+    for i in range(3):
+        u = torch.randn(z.shape, generator=torch.Generator().manual_seed(i), dtype=torch.float64)
+        h = 1e-5
+        want = (loss(z.double() + h * u) - loss(z.double() - h * u)) / (2 * h)
+        # lse is off by about L / 64 + 32 roundings, an element by twice that and a few more
+        assert abs(float((dz * u).sum()) - want) <= (L / 64 + 64) * 2.0 ** -22 * float((dz * u).abs().sum()) + 1e-7
+
+
+def test_refusals():
+    z, cls, val, labels = (gpu(t) for t in inputs(800, 6, 40, 4, torch.float32))
+    lse = torch.zeros(6, device="cuda")
+    for a in ({}, {"stream": torch.cuda.current_stream()}):
+        for bad in (lambda: gcpsl.distill(z, cls.long(), val, **a), lambda: gcpsl.distill(z, cls, val.double(), **a),
+                    lambda: gcpsl.distill(z, cls[:5], val[:5], **a), lambda: gcpsl.distill(z, cls, val[:, :3], **a),
+                    lambda: gcpsl.distill(z, cls[:, ::2], val[:, ::2], **a),
+                    lambda: gcpsl.distill(z, cls, val, labels=labels[:3], **a),
+                    lambda: gcpsl.distill_grad(z, cls, val, lse[:3], g_kl=lse, **a)):
+            with pytest.raises(ValueError):
+                bad()
+        for bad in (lambda: gcpsl.distill(z, cls, val, temperature=0.0, **a),
+                    lambda: gcpsl.distill(z, cls, val, temperature=float("nan"), **a),
+                    lambda: gcpsl.distill(z, cls[:, :0].contiguous(), val[:, :0].contiguous(), **a),
+                    lambda: gcpsl.distill_grad(z, cls, val, lse, **a),
+                    lambda: gcpsl.distill_grad(z, cls, val, g_kl=lse, **a),
+                    lambda: gcpsl.distill_grad(z, cls, val, lse, g_logp=lse, labels=labels, **a)):
+            with pytest.raises(gcpsl.GCPSLError):
+                bad()

@@ -1,0 +1,229 @@
+"""Residual updates with norms, and their gradients, on the GPU, against their 64-bit definition (tests/blocks_plain.py)."""
+import itertools
+
+import pytest
+import torch
+
+import blocks_plain as blocks
+from test_gpu_group import TYPES, check, gpu, make, offsets_of
+
+pytestmark = pytest.mark.gpu
+
+from paper_2609_29395_amd import gcpsl  # noqa: E402
+
+
+def inputs(seed, counts, n, T, extra=0):
+    """Tensors of the call; `extra` rows behind the last group."""
+    off, G = offsets_of(counts), len(counts)
+    rows = off[-1] + extra
+    t = {"x": make(seed, rows, n, dtype=T, scale=2.0), "y": make(seed + 1, rows, n, dtype=T, scale=3.0),
+         "gate": make(seed + 2, rows, n, dtype=T, scale=2.0), "w_block": 1 + make(seed + 3, G, n, scale=0.3),
+         "w_next": 1 + make(seed + 4, G, n, scale=0.3), "g_out": make(seed + 5, rows, n, dtype=T),
+         "g_h": make(seed + 6, rows, n, dtype=T)}
+    return off, torch.tensor(off, dtype=torch.int32).cuda(), t
+
+
+def run_both(off, o, t, block, gate, first, nxt, g_out, g_h, alpha=0.75, beta=-1.25, eps=1e-5):
+    """Forward, then the gradient with the forward pass's own results, both checked."""
+    rows = t["x"].shape[0]
+    names = [k for k, on in (("y", block), ("gate", gate), ("w_block", first), ("w_next", nxt)) if on]
+    alpha = alpha if block else 1.0
+    given = {k: t[k] for k in names}
+    got = gcpsl.group_residual_norm(gpu(t["x"]), o, **{k: gpu(v) for k, v in given.items()}, alpha=alpha, beta=beta, eps=eps)
+    want, written = blocks.residual(t["x"], off, **given, alpha=alpha, beta=beta, eps=eps)
+    keep = written.nonzero()[:, 0]
+    for k, v in got._asdict().items():
+        if k == "out" and not block:
+            assert torch.equal(v.cpu(), t["x"])
+        elif k in want:
+            check(v.cpu()[keep], want[k][0][keep], want[k][1][keep], k)
+        else:
+            assert v is None, k
+    grads = {k: t[k] for k, on in (("g_out", g_out), ("g_h", g_h)) if on}
+    given = {k: v for k, v in given.items() if k != "w_next" or g_h}
+    r = {"r_block": got.r_block if first else None, "r_next": got.r_next if g_h else None}
+    res = gcpsl.group_residual_norm_grad(got.out, o, **{k: gpu(v) for k, v in {**grads, **given}.items()}, **r, alpha=alpha,
+                                         beta=beta)
+    want, _ = blocks.residual_grad(got.out.cpu(), off, **grads, **given,
+                                   **{k: None if v is None else v.cpu() for k, v in r.items()}, alpha=alpha, beta=beta)
+    for k, v in res._asdict().items():
+        if k not in want:
+            assert v is None, k
+        elif k.startswith("dw"):
+            check(v, *want[k], k)
+        else:
+            check(v.cpu()[keep], want[k][0][keep], want[k][1][keep], k)
+    assert rows == t["x"].shape[0]
+    return got, res
+
+
+# widths: one, below a vector, not multiples of one, held by a wave, by a workgroup, by neither
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("counts,n", [([1], 1), ([5, 0, 2], 3), ([1, 1], 7), ([9], 8), ([3, 0, 30], 65), ([40, 1], 250),
+                                      ([17, 16], 512), ([12], 513), ([30, 0, 11], 1001), ([7, 20], 1024), ([9], 1030),
+                                      ([8, 5], 2047), ([13], 2056), ([6, 0, 9], 4096), ([5], 4099), ([4, 3], 8192),
+                                      ([3], 8200), ([2, 2], 16390)])
+def test_widths(counts, n, dtype):
+    run_both(*inputs(100, counts, n, TYPES[dtype]), True, True, True, True, True, True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [72, 1300, 9001])
+def test_every_part_left_out(n, dtype):
+    """All calls that the checks let through: with and without block output, gate, either norm, either gradient."""
+    off, o, t = inputs(200, [5, 0, 9], n, TYPES[dtype])
+    seen = 0
+    for block, gate, first, nxt, g_out, g_h in itertools.product([True, False], repeat=6):
+        if (not block and (gate or first or not nxt)) or not (g_out or g_h) or (g_h and not nxt):
+            continue
+        run_both(off, o, t, block, gate, first, nxt, g_out, g_h)
+        seen += 1
+    assert seen == 19
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("counts,n", [([700, 0, 1, 1300], 40), ([3000], 200), ([10] * 100, 136), ([1500, 2, 900], 1000),
+                                      ([600], 9000)])
+def test_gradients_in_pieces(counts, n, dtype):
+    """Rows enough that a group's weights' gradients are summed in pieces; any workspace, the same bits."""
+    off, o, t = inputs(300, counts, n, TYPES[dtype])
+    _, res = run_both(off, o, t, True, True, True, True, True, True)
+    need = gcpsl.group_residual_workspace_bytes(dtype, len(counts), off[-1], n)
+    assert need > 0
+    f = gcpsl.group_residual_norm(gpu(t["x"]), o, **{k: gpu(t[k]) for k in ("y", "gate", "w_block", "w_next")}, alpha=0.75,
+                                  beta=-1.25, eps=1e-5)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")  # NaN throughout
+    again = gcpsl.group_residual_norm_grad(f.out, o, **{k: gpu(t[k]) for k in ("g_out", "g_h", "y", "gate", "w_block",
+                                                                             "w_next")}, r_block=f.r_block,
+                                           r_next=f.r_next, alpha=0.75, beta=-1.25, workspace=ws)
+    assert all(torch.equal(a, b) for a, b in zip(again, res))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [33, 264, 2100, 9003])
+def test_strides_and_what_lies_beside(n, dtype):
+    """Rows of any stride and alignment; nothing beside the tensors or outside the groups is read as theirs or written."""
+    T = TYPES[dtype]
+    off, o, t = inputs(400, [4, 0, 6], n, T, extra=3)
+    off, rows = [2 + v for v in off], 13
+    o = o + 2
+
+    def wide(v=None):
+        w = torch.full((rows + 1, n + 3), float("nan"), dtype=T, device="cuda")
+        if v is not None:
+            w[:rows, 1:n + 1].copy_(v)
+        return w, w[:rows, 1:n + 1]
+
+    (_, x), (_, y), (_, gate) = (wide(t[k]) for k in ("x", "y", "gate"))
+    (bo, out), (bh, h) = wide(), wide()
+    got = gcpsl.group_residual_norm(x, o, y=y, gate=gate, w_block=gpu(t["w_block"]), w_next=gpu(t["w_next"]), out=out, h=h)
+    assert got.out is out and got.h is h
+    want, written = blocks.residual(t["x"], off, *(t[k] for k in ("y", "gate", "w_block", "w_next")))
+    keep = written.nonzero()[:, 0]
+    for k in ("out", "h"):
+        check(getattr(got, k).cpu()[keep], want[k][0][keep], want[k][1][keep], k)
+    for b in (bo, bh):
+        assert torch.isnan(b[:, 0]).all() and torch.isnan(b[:, n + 1:]).all() and torch.isnan(b[rows]).all()
+        assert torch.isnan(b[:2]).all() and torch.isnan(b[12:]).all()
+    alone = gcpsl.group_residual_norm(x, o, y=y, gate=gate, w_block=gpu(t["w_block"]), w_next=gpu(t["w_next"]), out=x)
+    assert alone.out is x and torch.equal(x[2:12], out[2:12]) and torch.equal(alone.h[2:12], h[2:12])
+    assert torch.equal(x[:2].cpu(), t["x"][:2])  # in place, the other rows as they were
+    (_, go), (_, gh) = wide(t["g_out"]), wide(t["g_h"])
+    res = gcpsl.group_residual_norm_grad(out, o, g_out=go, g_h=gh, y=y, gate=gate, w_block=gpu(t["w_block"]),
+                                         w_next=gpu(t["w_next"]), r_block=got.r_block, r_next=got.r_next)
+    want, _ = blocks.residual_grad(out.cpu(), off, t["g_out"], t["g_h"], t["y"], t["gate"], t["w_block"], t["w_next"],
+                                   got.r_block.cpu(), got.r_next.cpu())
+    for k in ("dx", "dy", "dgate"):
+        check(getattr(res, k).cpu()[keep], want[k][0][keep], want[k][1][keep], k)
+    # (the sums' 64-bit form would take the rows outside, which hold NaN: of the groups' rows alone)
+    for k in ("dw_block", "dw_next"):
+        check(getattr(res, k), *want[k], k)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_shared_weights(dtype):
+    off, o, t = inputs(500, [20, 0, 31], 96, TYPES[dtype])
+    for k in ("w_block", "w_next"):
+        t[k] = t[k][:1].repeat(3, 1)
+    one = {k: gpu(t[k][:1]).expand(3, -1) for k in ("w_block", "w_next")}
+    assert one["w_block"].stride(0) == 0
+    got, _ = run_both(off, o, t, True, True, True, True, True, True)
+    again = gcpsl.group_residual_norm(gpu(t["x"]), o, y=gpu(t["y"]), gate=gpu(t["gate"]), **one, alpha=0.75, beta=-1.25,
+                                      eps=1e-5)
+    assert all(torch.equal(a, b) for a, b in zip(again, got))
+
+
+def test_rows_of_zeros_nans_and_far_values():
+    """A row of zeros has r = eps^-1/2; a NaN stays in its row and its group's sums; far gates are 0 or 1."""
+    off, o, t = inputs(600, [3, 4], 300, torch.float32)
+    t["x"][0] = t["y"][0] = 0
+    t["gate"][1, :100], t["gate"][1, 100:200] = -3e4, 3e4
+    run_both(off, o, t, True, True, True, True, True, True)
+    t["y"][5, 17] = float("nan")
+    g = {k: gpu(v) for k, v in t.items() if k not in ("g_out", "g_h", "x")}
+    got = gcpsl.group_residual_norm(gpu(t["x"]), o, **g)
+    assert torch.isnan(got.out[5]).all() and torch.isnan(got.h[5]).all()
+    others = [0, 1, 2, 3, 4, 6]
+    assert torch.isfinite(got.out[others]).all() and torch.isfinite(got.h[others]).all()
+    res = gcpsl.group_residual_norm_grad(got.out, o, g_out=gpu(t["g_out"]), g_h=gpu(t["g_h"]), **g, r_block=got.r_block,
+                                         r_next=got.r_next)
+    assert torch.isfinite(res.dx[others]).all() and torch.isfinite(res.dw_block[0]).all()
+    assert torch.isnan(res.dw_next[1]).all()
+
+
+def test_no_rows():
+    x, o = torch.zeros(0, 40, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    w = torch.ones(3, 40, device="cuda")
+    got = gcpsl.group_residual_norm(x, o, y=x, w_block=w, w_next=w)
+    assert got.h.shape == (0, 40)
+    res = gcpsl.group_residual_norm_grad(got.out, o, g_h=x, y=x, w_block=w, w_next=w, r_block=got.r_block, r_next=got.r_next)
+    assert (res.dw_block == 0).all() and (res.dw_next == 0).all()
+
+
+@pytest.mark.parametrize("n", [40, 1200, 8800])
+def test_gradients_against_differences(n):
+    """All five gradients of sum(out g_out + h g_h) against central differences of the 64-bit forward pass."""
+    off, o, t = inputs(700, [6, 0, 9], n, torch.float32)
+    names = ["x", "y", "gate", "w_block", "w_next"]
+    at = {k: t[k].double() for k in names}
+
+    def loss(v):
+        got, _ = blocks.residual(v["x"], off, v["y"], v["gate"], v["w_block"], v["w_next"], 0.5, 2.0, 1e-3)
+        return float((got["out"][0] * t["g_out"].double() + got["h"][0] * t["g_h"].double()).sum())
+
+    got = gcpsl.group_residual_norm(gpu(t["x"]), o, **{k: gpu(t[k]) for k in names[1:]}, alpha=0.5, beta=2.0, eps=1e-3)
+    res = gcpsl.group_residual_norm_grad(got.out, o, g_out=gpu(t["g_out"]), g_h=gpu(t["g_h"]),
+                                         **{k: gpu(t[k]) for k in names[1:]}, r_block=got.r_block, r_next=got.r_next,
+                                         alpha=0.5, beta=2.0)
+    for name, grad in zip(names, res):
+        u = torch.randn(at[name].shape, generator=torch.Generator().manual_seed(len(name)), dtype=torch.float64)
+        h = 1e-5
+        ends = [loss({**at, name: at[name] + s * h * u}) for s in (1, -1)]
+        want = (ends[0] - ends[1]) / (2 * h)
+        got_d = grad.cpu().double() * u
+        # a row's sums are off by n / 64 + 40 roundings, its elements by a few more
+        assert abs(float(got_d.sum()) - want) <= (n / 64 + 64) * 2.0 ** -22 * float(got_d.abs().sum()) + 1e-6, name
+
+
+def test_refusals():
+    x, o = gpu(make(1, 8, 16)), torch.tensor([0, 8], dtype=torch.int32).cuda()
+    w, r = torch.ones(1, 16, device="cuda"), torch.ones(8, device="cuda")
+    for a in ({}, {"stream": torch.cuda.current_stream()}):
+        for bad in (lambda: gcpsl.group_residual_norm(x, o, y=x[:4], **a),
+                    lambda: gcpsl.group_residual_norm(x, o, y=x.bfloat16(), **a),
+                    lambda: gcpsl.group_residual_norm(x, o, w_next=w, out=torch.empty_like(x), **a),
+                    lambda: gcpsl.group_residual_norm(x, o, y=x, h=torch.empty_like(x), **a),
+                    lambda: gcpsl.group_residual_norm(x, o, w_next=w[:, :8], **a),
+                    lambda: gcpsl.group_residual_norm_grad(x, o, g_h=x, w_next=w, r_next=r[:4], **a)):
+            with pytest.raises(ValueError):
+                bad()
+        for bad in (lambda: gcpsl.group_residual_norm(x, o, **a),
+                    lambda: gcpsl.group_residual_norm(x, o, gate=x, w_next=w, **a),
+                    lambda: gcpsl.group_residual_norm(x, o, w_next=w, alpha=2.0, **a),
+                    lambda: gcpsl.group_residual_norm(x, o, w_next=w, eps=0.0, **a),
+                    lambda: gcpsl.group_residual_norm(x, o, y=x, alpha=float("inf"), **a),
+                    lambda: gcpsl.group_residual_norm_grad(x, o, w_next=w, r_next=r, **a),
+                    lambda: gcpsl.group_residual_norm_grad(x, o, g_h=x, w_next=w, **a),
+                    lambda: gcpsl.group_residual_norm_grad(x, o, g_out=x, w_block=w, r_block=r, **a)):
+            with pytest.raises(gcpsl.GCPSLError):
+                bad()
