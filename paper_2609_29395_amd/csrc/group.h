@@ -387,9 +387,12 @@ template <typename T, int MODE, int ROWS, bool EDGES = true> struct FinishRows {
 };
 
 // ------------------------------------------------------------ gated layers
-// What a gated layer's columns are in the tiles of operand b: of BN columns the
-// first half are gates c0 .. and the second the values of the same outputs, N
-// rows of w further on; c0 = nt BN / 2.
+// A tile of BN of operand b's rows gives BN / 2 of a gated layer's outputs, c0 =
+// nt BN / 2 on: the first half of its columns are their gates, the second their
+// values, N rows of b further on.
+inline int64_t group_cols(const GroupArgs &a, int mode) { return mode == GROUP_GATED ? 2 * (int64_t)a.N : a.N; }
+constexpr int group_outputs(int mode, int bn) { return mode == GROUP_GATED ? bn / 2 : bn; }
+constexpr bool group_is_pair(int mode) { return mode == GROUP_GATED || mode == GROUP_GATED_GRAD; }
 
 constexpr float kLog2E = 1.44269504088896340736f;
 // s = 1 / (1 + e^-g) and 1 - s, from e^-|g|: neither overflows nor cancels.
@@ -422,36 +425,202 @@ GROUP_DEVICE void gate_grad_of(int act, float g, float &f, float &d) {
   }
 }
 
+// VEC values of either type (whole vectors at any alignment) <-> fp32.
+template <typename T, int VEC> GROUP_DEVICE void load_values(const T *p, float (&v)[VEC]) {
+#pragma unroll
+  for (int j = 0; j < VEC; j += 4) {
+    if constexpr (sizeof(T) == 2) {
+      const u32x2_any b = *(const u32x2_any *)(p + j);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[j + r] = __uint_as_float(r & 1 ? b[r >> 1] & 0xffff0000u : b[r >> 1] << 16);
+    } else {
+      const f32x4_any b = *(const f32x4_any *)(p + j);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[j + r] = b[r];
+    }
+  }
+}
+template <typename T, int VEC> GROUP_DEVICE void store_values(T *p, const float (&v)[VEC]) {
+  if constexpr (sizeof(T) == 4) {
+    static_assert(VEC == 4, "");
+    *(f32x4_any *)p = f32x4_any{v[0], v[1], v[2], v[3]};
+  } else if constexpr (VEC == 8) {
+    *(u32x4_any *)p = u32x4_any{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])};
+  } else {
+    *(u32x2_any *)p = u32x2_any{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])};
+  }
+}
+
 // Up to four columns c .. c + 3 of row m of a gated layer's result.  MODE
 // GROUP_GATED: from the sums of gates and values; GROUP_GATED_GRAD: from those
 // of the gradient (gates unused).
 template <typename T, int MODE, typename V>
 GROUP_DEVICE void finish_pair(const GroupArgs &a, int g, int m, int c, const V &gates, const V &values) {
+  T *out = (T *)a.out + (int64_t)m * a.ldo + c, *pre = (T *)a.pre + (int64_t)m * a.ldp + c;
+  const bool whole = c + 4 <= a.N;
+  float p[4], u[4], x[4], y[4];
+  if constexpr (MODE == GROUP_GATED) {
+    const float *bias = a.bias ? a.bias + g * a.bias_gs + c : nullptr;
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    if (c + r >= a.N) break;
-    if constexpr (MODE == GROUP_GATED) {
-      float p = gates[r], u = values[r];
-      if (a.bias) {
-        p += a.bias[g * a.bias_gs + c + r];
-        u += a.bias[g * a.bias_gs + a.N + c + r];
+    for (int r = 0; r < 4; ++r) {
+      p[r] = gates[r];
+      u[r] = values[r];
+      if (bias && c + r < a.N) {
+        p[r] += bias[r];
+        u[r] += bias[a.N + r];
       }
-      ((T *)a.out)[(int64_t)m * a.ldo + c + r] = ElemT<T>::from_f(gate_of(a.act, p) * u);
+      x[r] = gate_of(a.act, p[r]) * u[r];
+    }
+    if (whole) {
+      store_values<T, 4>(out, x);
       if (a.pre) {
-        T *pre = (T *)a.pre + (int64_t)m * a.ldp + c + r;
-        pre[0] = ElemT<T>::from_f(p);
-        pre[a.N] = ElemT<T>::from_f(u);
+        store_values<T, 4>(pre, p);
+        store_values<T, 4>(pre + a.N, u);
       }
     } else {
-      const T *pre = (const T *)a.pre + (int64_t)m * a.ldp + c + r;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (c + r < a.N) {
+          out[r] = ElemT<T>::from_f(x[r]);
+          if (a.pre) {
+            pre[r] = ElemT<T>::from_f(p[r]);
+            pre[a.N + r] = ElemT<T>::from_f(u[r]);
+          }
+        }
+    }
+  } else {
+    if (whole) {
+      load_values<T, 4>(pre, p);
+      load_values<T, 4>(pre + a.N, u);
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        p[r] = c + r < a.N ? ElemT<T>::to_f(pre[r]) : 0.f;
+        u[r] = c + r < a.N ? ElemT<T>::to_f(pre[a.N + r]) : 0.f;
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
       float f, d;
-      gate_grad_of(a.act, ElemT<T>::to_f(pre[0]), f, d);
-      T *out = (T *)a.out + (int64_t)m * a.ldo + c + r;
-      out[0] = ElemT<T>::from_f(d * ElemT<T>::to_f(pre[a.N]) * values[r]);
-      out[a.N] = ElemT<T>::from_f(f * values[r]);
+      gate_grad_of(a.act, p[r], f, d);
+      x[r] = d * u[r] * values[r];
+      y[r] = f * values[r];
+    }
+    if (whole) {
+      store_values<T, 4>(out, x);
+      store_values<T, 4>(out + a.N, y);
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (c + r < a.N) {
+          out[r] = ElemT<T>::from_f(x[r]);
+          out[a.N + r] = ElemT<T>::from_f(y[r]);
+        }
     }
   }
 }
+
+// What FinishRows is to a layer's results, for a gated layer's: the sums of row i,
+// columns 4 j on, at acc(i, j, 0), GROUP_GATED those of the values at acc(i, j, 1).
+// The gradient's pairs are loaded for a batch of rows together, the first batch
+// before the sums are there and every other beside the one before it.
+template <typename T, int MODE, int ROWS> struct FinishPairs {
+  static constexpr int VEC = Vec16<T>::N, BATCH = ROWS < 4 ? ROWS : 4;
+  static constexpr bool GRAD = MODE == GROUP_GATED_GRAD;
+  static_assert(ROWS % BATCH == 0, "");
+  struct Pairs {
+    u32x4_any v[GRAD ? BATCH : 1][2];
+  };
+  int m0, step, m1, c, g;
+  bool whole;
+  float bias[GRAD ? 1 : 2][VEC];
+  Pairs first;
+  GROUP_DEVICE FinishPairs(const GroupArgs &a, int g_, int m0_, int step_, int m1_, int c_)
+      : m0(m0_), step(step_), m1(m1_), c(c_), g(g_) {
+    whole = c + VEC <= a.N;
+    if (!whole) return;
+    if constexpr (GRAD) {
+      load(a, 0, first);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) bias[h][j] = a.bias ? a.bias[g * a.bias_gs + h * a.N + c + j] : 0.f;
+    }
+  }
+  GROUP_DEVICE void load(const GroupArgs &a, int i0, Pairs &p) const {
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {  // (rows outside: the last one)
+      const T *q = (const T *)a.pre + (int64_t)min(m0 + (i0 + i) * step, m1 - 1) * a.ldp + c;
+      p.v[i][0] = *(const u32x4_any *)q;
+      p.v[i][1] = *(const u32x4_any *)(q + a.N);
+    }
+  }
+  template <typename F> GROUP_DEVICE void store_row(const GroupArgs &a, int i, const u32x4_any (&p)[2], const F &acc) const {
+    const int m = m0 + i * step;
+    if (m >= m1) return;
+    T *out = (T *)a.out + (int64_t)m * a.ldo + c;
+    float x[VEC], y[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC / 4; ++j) {
+      const f32x4_any v = acc(i, j, 0);
+      if constexpr (GRAD) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float f, d;
+          gate_grad_of(a.act, Vec16<T>::at(p[0], 4 * j + r), f, d);
+          x[4 * j + r] = d * Vec16<T>::at(p[1], 4 * j + r) * v[r];
+          y[4 * j + r] = f * v[r];
+        }
+      } else {
+        const f32x4_any u = acc(i, j, 1);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          x[4 * j + r] = v[r] + bias[0][4 * j + r];
+          y[4 * j + r] = u[r] + bias[1][4 * j + r];
+        }
+      }
+    }
+    if constexpr (GRAD) {
+      store_values<T, VEC>(out, x);
+      store_values<T, VEC>(out + a.N, y);
+    } else {
+      if (a.pre) {
+        T *q = (T *)a.pre + (int64_t)m * a.ldp + c;
+        store_values<T, VEC>(q, x);
+        store_values<T, VEC>(q + a.N, y);
+      }
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) x[j] = gate_of(a.act, x[j]) * y[j];
+      store_values<T, VEC>(out, x);
+    }
+  }
+  template <typename F> GROUP_DEVICE void store(const GroupArgs &a, const F &acc) const {
+    if (c >= a.N) return;
+    if (!whole) {
+#pragma unroll 1
+      for (int i = 0; i < ROWS; ++i)
+#pragma unroll 1
+        for (int j = 0; j < VEC / 4; ++j)
+          if (m0 + i * step < m1 && c + 4 * j < a.N)
+            finish_pair<T, MODE>(a, g, m0 + i * step, c + 4 * j, acc(i, j, 0), acc(i, j, GRAD ? 0 : 1));
+      return;
+    }
+    if constexpr (GRAD) {
+      Pairs next = first;
+#pragma unroll 1
+      for (int i0 = 0; i0 < ROWS; i0 += BATCH) {
+        const Pairs now = next;
+        if (i0 + BATCH < ROWS) load(a, i0 + BATCH, next);
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) store_row(a, i0 + i, now.v[i], acc);
+      }
+    } else {  // (copies of the activations' code for every row cost more in fetching it)
+#pragma unroll 1
+      for (int i = 0; i < ROWS; ++i) store_row(a, i, first.v[0], acc);
+    }
+  }
+};
 
 // Four columns of a weight gradient, to its place or (slot >= 0) to a partial.
 template <typename V> GROUP_DEVICE void store_grad(const GroupArgs &a, int g, int slot, int m, int c, const V &acc) {

@@ -267,7 +267,8 @@ namespace {
 // 1,024, 1024 -> 1024, 32 against 27.
 bool tiles_fill_half(int64_t row_tiles, int64_t cols) { return row_tiles * ((cols + 255) / 256) >= kCUs / 2; }
 bool fills_half(const GroupArgs &a, int mode) {
-  return tiles_fill_half(mode == GROUP_DW ? (int64_t)((a.M + 255) / 256) * a.G : ((int64_t)a.M + 128 * a.G) / 256, a.N);
+  return tiles_fill_half(mode == GROUP_DW ? (int64_t)((a.M + 255) / 256) * a.G : ((int64_t)a.M + 128 * a.G) / 256,
+                         group_cols(a, mode));
 }
 
 }  // namespace
@@ -309,13 +310,11 @@ GroupPieces group_pieces(int dtype, int G, int64_t rows, int n, int k) {
 
 hipError_t launch_group(int dtype, int mode, const GroupArgs &a, hipStream_t s) {
   hipError_t e;
-  if (mode == GROUP_GATED || mode == GROUP_GATED_GRAD)
-    return dtype == GCPSL_BF16 ? launch_any<bf16_t>(mode, a, s) : launch_any<float>(mode, a, s);
   if (group_few_ok(dtype, a, mode)) e = launch_group_few(dtype, mode, a, s);
   else if (group_tile_ok(dtype, a, mode) && fills_half(a, mode)) e = launch_group_tile(mode, a, s);
   else if (group_mid_ok(dtype, a, mode)) e = launch_group_mid(mode, a, s);
   else if (dtype == GCPSL_F32 && group_f32_deep_ok(a, mode)) e = launch_group_f32_deep(mode, a, s);
-  else if (dtype == GCPSL_F32 && a.N >= 64 && group_f32_ok(a, mode)) e = launch_group_f32(mode, a, s);
+  else if (dtype == GCPSL_F32 && group_cols(a, mode) >= 64 && group_f32_ok(a, mode)) e = launch_group_f32(mode, a, s);
   else e = dtype == GCPSL_BF16 ? launch_any<bf16_t>(mode, a, s) : launch_any<float>(mode, a, s);
   if (e == hipSuccess && mode == GROUP_DW && a.slots > 0) {
     // about eight workgroups a CU in all, of 256 entries or more

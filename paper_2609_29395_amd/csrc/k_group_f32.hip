@@ -44,7 +44,8 @@ template <bool T, int ROWS = 2> struct Stage {
   uint32_t off[T ? 1 : 2], ld;   // byte offsets of the thread's loads, bytes of a row
   float v[J][8];                 // [row or column][k]
 
-  __device__ __forceinline__ void init(const float *p, int64_t ld_, int n, int t) {
+  // pair: rows from the gates' to the values' of a gated layer, the second of a thread's rows (0: none)
+  __device__ __forceinline__ void init(const float *p, int64_t ld_, int n, int t, int pair = 0) {
     base = (const char *)p;
     ld = (uint32_t)ld_ * 4u;
     step = T ? ld_ * (4 * BK) : 4 * BK;
@@ -57,7 +58,8 @@ template <bool T, int ROWS = 2> struct Stage {
       chunk = t & 1;
       row = t >> 1;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) off[j] = (uint32_t)min(row + j * 64, n - 1) * ld + (uint32_t)chunk * 32u;
+      for (int j = 0; j < 2; ++j)
+        off[j] = (uint32_t)(pair ? min(row, n - 1) + j * pair : min(row + j * 64, n - 1)) * ld + (uint32_t)chunk * 32u;
     }
   }
   // the next tile, all of it inside
@@ -131,7 +133,7 @@ struct Tile {
 // The tile's sums and results; waves of 32 FJ x 64 outputs.
 template <int MODE, int FJ>
 __device__ __forceinline__ void group_f32_tile(const GroupArgs &a, const Tile &t, char *lds) {
-  constexpr bool AT = MODE == GROUP_DW, BT = MODE != GROUP_FWD;
+  constexpr bool AT = MODE == GROUP_DW, BT = group_across(MODE), PAIR = MODE == GROUP_GATED;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1, li = lane & 31, lg = lane >> 5;
   const float *const A = t.A, *const B = t.B;
@@ -205,7 +207,7 @@ __device__ __forceinline__ void group_f32_tile(const GroupArgs &a, const Tile &t
   if constexpr (AT == BT) {
     Stage<AT> stage;
     if (wave < 2) stage.init(A, a.lda, rows, tid);
-    else stage.init(B, a.ldb, cols, tid - 128);
+    else stage.init(B, a.ldb, cols, tid - 128, PAIR ? a.N : 0);
     run(stage, wave < 2);
   } else if (wave < 2) {
     Stage<AT, FJ> stage;
@@ -230,9 +232,9 @@ __device__ __forceinline__ void group_f32_tile(const GroupArgs &a, const Tile &t
       float x[FJ], w[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const int r = wm * 32 * FJ + j * 32 + li, c = wn * 64 + j * 32 + li;
+        const int r = wm * 32 * FJ + j * 32 + li, c = (PAIR ? 0 : wn * 64) + j * 32 + li;
         if (j < FJ) x[j] = r < rows && k < Q ? (AT ? A[(int64_t)k * a.lda + r] : A[(int64_t)r * a.lda + k]) : 0.f;
-        w[j] = c < cols && k < Q ? (BT ? B[(int64_t)k * a.ldb + c] : B[(int64_t)c * a.ldb + k]) : 0.f;
+        w[j] = c < cols && k < Q ? (BT ? B[(int64_t)k * a.ldb + c] : B[((int64_t)c + (PAIR ? wn * a.N : 0)) * a.ldb + k]) : 0.f;
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i)
@@ -246,9 +248,12 @@ __device__ __forceinline__ void group_f32_tile(const GroupArgs &a, const Tile &t
   const auto place = [&](int r, int c) { return lds + r * 512 + ((c >> 2) ^ ((r & 15) << 1)) * 16; };
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const int m0 = h * 32 * FJ, r0 = tid >> 5, c4 = (tid & 31) * 4;
+    constexpr int LANES = group_outputs(MODE, BN) / 4, STEP = 256 / LANES, ROWS = 32 * FJ / STEP;
+    const int m0 = h * 32 * FJ, r0 = tid / LANES, c4 = tid % LANES * 4;
     if (m0 >= rows) break;
-    const FinishRows<float, MODE == GROUP_DW ? GROUP_FWD : MODE, 4 * FJ> out(a, g, row0 + m0 + r0, 8, row0 + rows, c0 + c4);
+    using Finish = std::conditional_t<group_is_pair(MODE), FinishPairs<float, MODE, ROWS>,
+                                      FinishRows<float, MODE == GROUP_DX ? GROUP_DX : GROUP_FWD, ROWS>>;
+    const Finish out(a, g, row0 + m0 + r0, STEP, min(row0 + rows, row0 + m0 + 32 * FJ), c0 + c4);
     __syncthreads();
     if (wm == h)
 #pragma unroll
@@ -268,6 +273,8 @@ __device__ __forceinline__ void group_f32_tile(const GroupArgs &a, const Tile &t
       if (c0 + c4 < a.N)
         for (int i = 0; i < 4 * FJ && m0 + r0 + 8 * i < rows; ++i)
           store_grad(a, g, slot, row0 + m0 + r0 + 8 * i, c0 + c4, sum(i, 0));
+    } else if constexpr (group_is_pair(MODE)) {
+      out.store(a, [&](int i, int, int half) { return *(const f32x4_t *)place(r0 + STEP * i, half * (BN / 2) + c4); });
     } else {
       out.store(a, sum);
     }
@@ -287,7 +294,8 @@ __device__ __forceinline__ void group_f32_tile(const GroupArgs &a, const Tile &t
 
 template <int MODE>
 __global__ void __launch_bounds__(256, 2) group_f32_kernel(GroupArgs a, int NT) {
-  constexpr bool BT = MODE != GROUP_FWD;
+  constexpr bool BT = group_across(MODE);
+  constexpr int COLS = group_outputs(MODE, BN);
   __shared__ __attribute__((aligned(16))) char lds[2 * BUFFER];
   Tile t{(const float *)a.a, (const float *)a.b, 0, 0, 0, 0, 0, a.Q, -1, false};
   int nt;
@@ -307,18 +315,19 @@ __global__ void __launch_bounds__(256, 2) group_f32_kernel(GroupArgs a, int NT) 
     int row1;
     if (!tile_of(a.off, a.G, a.M, BM, NT, blockIdx.x, t.g, t.row0, row1, nt)) return;
     t.rows = row1 - t.row0;
-    t.c0 = nt * BN;
+    t.c0 = nt * COLS;
     t.A += (int64_t)t.row0 * a.lda;
     t.B += t.g * a.b_gs + (BT ? (int64_t)t.c0 : (int64_t)t.c0 * a.ldb);
   }
-  t.cols = min(BN, a.N - t.c0);
+  t.cols = min(COLS, a.N - t.c0);
   t.sums = MODE == GROUP_DW && a.db != nullptr && nt == 0;
   if (MODE != GROUP_DW && t.rows <= BM / 2) group_f32_tile<MODE, 1>(a, t, lds);
   else group_f32_tile<MODE, 2>(a, t, lds);
 }
 
 template <int MODE> hipError_t run_mode(const GroupArgs &a, hipStream_t s) {
-  const int64_t NT = (a.N + BN - 1) / BN;
+  constexpr int COLS = group_outputs(MODE, BN);
+  const int64_t NT = (a.N + COLS - 1) / COLS;
   const int64_t blocks = MODE == GROUP_DW ? piece_blocks(a, (int64_t)((a.M + BM - 1) / BM) * NT)
                                           : tile_blocks(a.M, a.G, BM, NT);
   if (blocks > kMaxBlocks) return hipErrorInvalidConfiguration;
@@ -329,12 +338,19 @@ template <int MODE> hipError_t run_mode(const GroupArgs &a, hipStream_t s) {
 }  // namespace
 
 // Two columns at least wherever the operands' rows run across the sum, and
-// row strides whose offsets within a tile fit 32 bits.
+// row strides whose offsets within a tile fit 32 bits (gated: those from a
+// gate's row to its value's, too).
 bool group_f32_ok(const GroupArgs &a, int mode) {
-  return a.lda <= kMaxTileLd && a.ldb <= kMaxTileLd && (mode == GROUP_FWD || a.N >= 2) && (mode != GROUP_DW || a.M >= 2);
+  if (mode == GROUP_GATED && ((int64_t)a.N + 128) * a.ldb >= (int64_t)1 << 30) return false;
+  return a.lda <= kMaxTileLd && a.ldb <= kMaxTileLd && (!group_across(mode) || a.N >= 2) && (mode != GROUP_DW || a.M >= 2);
 }
 
 hipError_t launch_group_f32(int mode, const GroupArgs &a, hipStream_t s) {
-  return mode == GROUP_FWD ? run_mode<GROUP_FWD>(a, s)
-                           : mode == GROUP_DX ? run_mode<GROUP_DX>(a, s) : run_mode<GROUP_DW>(a, s);
+  switch (mode) {
+    case GROUP_FWD: return run_mode<GROUP_FWD>(a, s);
+    case GROUP_DX: return run_mode<GROUP_DX>(a, s);
+    case GROUP_DW: return run_mode<GROUP_DW>(a, s);
+    case GROUP_GATED: return run_mode<GROUP_GATED>(a, s);
+    default: return run_mode<GROUP_GATED_GRAD>(a, s);
+  }
 }

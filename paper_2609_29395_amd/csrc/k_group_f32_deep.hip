@@ -46,7 +46,8 @@ template <bool T> struct Stage {
   uint32_t off, ld;  // byte offset of the thread's first load, bytes of a row
   float v[2][2][8];  // [set][T: column, else piece][k]
 
-  __device__ __forceinline__ void init(const float *p, int64_t ld_, int n, int t, int first) {
+  // pair: rows from the gates' to the values' of a gated layer, the second half of the tile's rows (0: none)
+  __device__ __forceinline__ void init(const float *p, int64_t ld_, int n, int t, int first, int pair = 0) {
     ld = (uint32_t)ld_ * 4u;
     base = (const char *)p + (T ? ld_ * first : first) * 4;
     step = (T ? ld_ : 1) * (2 * BK * 4);
@@ -58,7 +59,7 @@ template <bool T> struct Stage {
     } else {
       chunk = (t & 1) * 2;
       row = t >> 1;
-      off = (uint32_t)min(row, n - 1) * ld + (uint32_t)chunk * 32u;
+      off = (uint32_t)(pair ? min(row & 31, n - 1) + (row >> 5) * pair : min(row, n - 1)) * ld + (uint32_t)chunk * 32u;
     }
   }
   // the next tile, all of it inside
@@ -121,7 +122,8 @@ template <bool T> struct Stage {
 
 template <int MODE>
 __global__ void __launch_bounds__(512, 2) group_f32_deep_kernel(GroupArgs a, int NT) {
-  constexpr bool AT = MODE == GROUP_DW, BT = MODE != GROUP_FWD;
+  constexpr bool AT = MODE == GROUP_DW, BT = group_across(MODE), PAIR = MODE == GROUP_GATED;
+  constexpr int COLS = group_outputs(MODE, BN);
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int tid = threadIdx.x, lane = tid & 63, t = tid & 255;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -142,9 +144,9 @@ __global__ void __launch_bounds__(512, 2) group_f32_deep_kernel(GroupArgs a, int
   } else {
     if (!tile_of<false>(a.off, a.G, a.M, BM, NT, blockIdx.x, g, row0, row1, nt)) return;
     A += (int64_t)row0 * a.lda;
-    B += g * a.b_gs + (BT ? (int64_t)nt * BN : (int64_t)nt * BN * a.ldb);
+    B += g * a.b_gs + (BT ? (int64_t)nt * COLS : (int64_t)nt * COLS * a.ldb);
   }
-  const int rows = row1 - row0, c0 = nt * BN, cols = min(BN, a.N - c0);
+  const int rows = row1 - row0, c0 = nt * COLS, cols = min(COLS, a.N - c0);
   const bool sums = MODE == GROUP_DW && a.db != nullptr && nt == 0;  // of A's columns, too (the bias gradient)
   float colsum[2] = {0.f, 0.f};
 
@@ -220,7 +222,7 @@ __global__ void __launch_bounds__(512, 2) group_f32_deep_kernel(GroupArgs a, int
   if constexpr (AT == BT) {
     Stage<AT> stage;
     if (is_a) stage.init(A, a.lda, rows, t, team * BK);
-    else stage.init(B, a.ldb, cols, t - 128, team * BK);
+    else stage.init(B, a.ldb, cols, t - 128, team * BK, PAIR ? a.N : 0);
     run(stage, is_a);
   } else if (is_a) {
     Stage<false> stage;
@@ -237,11 +239,11 @@ __global__ void __launch_bounds__(512, 2) group_f32_deep_kernel(GroupArgs a, int
     // lane (li, lg) takes k = k0 + lg
 #pragma unroll
     for (int r = 0; r < 16; ++r) big[r] = small[0][r] = small[1][r] = 0.f;
-    const int m = wm * 32 + li, c = wn * 32 + li;
+    const int m = wm * 32 + li, c = (PAIR ? 0 : wn * 32) + li;
     for (int k0 = 2 * team; k0 < Q; k0 += 4) {
       const int k = k0 + lg;
       const float x = m < rows && k < Q ? (AT ? A[(int64_t)k * a.lda + m] : A[(int64_t)m * a.lda + k]) : 0.f;
-      const float w = c < cols && k < Q ? (BT ? B[(int64_t)k * a.ldb + c] : B[(int64_t)c * a.ldb + k]) : 0.f;
+      const float w = c < cols && k < Q ? (BT ? B[(int64_t)k * a.ldb + c] : B[((int64_t)c + (PAIR ? wn * a.N : 0)) * a.ldb + k]) : 0.f;
       big = __builtin_amdgcn_mfma_f32_32x32x2f32(w, x, big, 0, 0, 0);
     }
   }
@@ -249,8 +251,11 @@ __global__ void __launch_bounds__(512, 2) group_f32_deep_kernel(GroupArgs a, int
   // The teams' sums, and whole rows of the tile written at once.  A lane holds,
   // in four groups of four, columns 8 q + 4 lg .. + 3 of row li.
   const auto place = [&](int which, int r, int c) { return lds + which * SUMS + r * 256 + ((c >> 2) ^ (r & 15)) * 16; };
-  const int r0 = tid >> 4, c4 = (tid & 15) * 4;
-  const FinishRows<float, MODE == GROUP_DW ? GROUP_FWD : MODE, 2> out(a, g, row0 + r0, 32, row1, c0 + c4);
+  constexpr int LANES = COLS / 4, STEP = 512 / LANES, ROWS = BM / STEP;
+  const int r0 = tid / LANES, c4 = tid % LANES * 4;
+  using Finish = std::conditional_t<group_is_pair(MODE), FinishPairs<float, MODE, ROWS>,
+                                    FinishRows<float, MODE == GROUP_DX ? GROUP_DX : GROUP_FWD, ROWS>>;
+  const Finish out(a, g, row0 + r0, STEP, row1, c0 + c4);
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     f32x4_t v;
@@ -277,6 +282,11 @@ __global__ void __launch_bounds__(512, 2) group_f32_deep_kernel(GroupArgs a, int
       for (int i = 0; i < 8; ++i) v += shares[i * 64 + tid];
       store_bias_grad(a, g, slot, row0 + tid, v);
     }
+  } else if constexpr (group_is_pair(MODE)) {
+    out.store(a, [&](int i, int, int half) {
+      const int r = r0 + STEP * i, c = half * (BN / 2) + c4;
+      return *(const f32x4_t *)place(0, r, c) + *(const f32x4_t *)place(1, r, c);
+    });
   } else {
     out.store(a, sum);
   }
@@ -290,7 +300,8 @@ template <int MODE> hipError_t run_mode(const GroupArgs &a, hipStream_t s) {
     if (e != hipSuccess) return e;
     once.mark();
   }
-  const int64_t NT = (a.N + BN - 1) / BN;
+  constexpr int COLS = group_outputs(MODE, BN);
+  const int64_t NT = (a.N + COLS - 1) / COLS;
   const int64_t blocks = MODE == GROUP_DW ? piece_blocks(a, (int64_t)((a.M + BM - 1) / BM) * NT)
                                           : tile_blocks(a.M, a.G, BM, NT);
   if (blocks > kMaxBlocks / 2) return hipErrorInvalidConfiguration;  // (of 512 threads)
@@ -306,12 +317,17 @@ template <int MODE> hipError_t run_mode(const GroupArgs &a, hipStream_t s) {
 // (200), 13 and 23; input gradient, 4 of 500, 1024 <- 4096 (144), 57 and 106;
 // with more, 16 of 3,000 rows, 600 -> 600 (540), 45 and 37.
 bool group_f32_deep_ok(const GroupArgs &a, int mode) {
-  if (a.N < 32 || !group_f32_ok(a, mode)) return false;
+  if (group_cols(a, mode) < 32 || !group_f32_ok(a, mode)) return false;
   if (mode == GROUP_DW) return group_f32_deep_grad(a.G, a.Q, a.M, a.N);
-  return ((int64_t)a.M + 32 * a.G) / 64 * ((a.N + BN - 1) / BN) <= kCUs;
+  return ((int64_t)a.M + 32 * a.G) / 64 * ((group_cols(a, mode) + BN - 1) / BN) <= kCUs;
 }
 
 hipError_t launch_group_f32_deep(int mode, const GroupArgs &a, hipStream_t s) {
-  return mode == GROUP_FWD ? run_mode<GROUP_FWD>(a, s)
-                           : mode == GROUP_DX ? run_mode<GROUP_DX>(a, s) : run_mode<GROUP_DW>(a, s);
+  switch (mode) {
+    case GROUP_FWD: return run_mode<GROUP_FWD>(a, s);
+    case GROUP_DX: return run_mode<GROUP_DX>(a, s);
+    case GROUP_DW: return run_mode<GROUP_DW>(a, s);
+    case GROUP_GATED: return run_mode<GROUP_GATED>(a, s);
+    default: return run_mode<GROUP_GATED_GRAD>(a, s);
+  }
 }

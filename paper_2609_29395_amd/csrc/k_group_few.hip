@@ -65,15 +65,19 @@ template <typename T> __device__ __forceinline__ u32x4 shift_down(u32x4 v, int n
 }
 
 // One operand's vectors of a step (the sum's positions lg VEC .. + VEC - 1 for
-// this lane), whose rows run along the sum: F rows 16 apart.
+// this lane), whose rows run along the sum: F rows 16 apart (of a gated layer's
+// weights F / 2 gates' and then the values', `pair` rows on).
 template <typename T, int F> struct Along {
   using W = Few<T>;
   const T *at[F];
   u32x4 v[F];
   // rows of stride ld from p on, `n` inside: those outside are taken as the last one
-  __device__ __forceinline__ void init(const T *p, int64_t ld, int n, int li, int lg) {
+  __device__ __forceinline__ void init(const T *p, int64_t ld, int n, int li, int lg, int pair = 0) {
 #pragma unroll
-    for (int f = 0; f < F; ++f) at[f] = p + (int64_t)min(16 * f + li, n - 1) * ld + lg * W::VEC;
+    for (int f = 0; f < F; ++f) {
+      const int second = pair && f >= F / 2;
+      at[f] = p + ((int64_t)min(16 * (second ? f - F / 2 : f) + li, n - 1) + (second ? pair : 0)) * ld + lg * W::VEC;
+    }
   }
   __device__ __forceinline__ void load(int s) {
 #pragma unroll
@@ -97,7 +101,7 @@ template <typename T> struct Across {
   int64_t ld;
   u32x4 v[W::VEC];
   // columns of p, `n` of them: a vector past the end is the last whole one
-  __device__ __forceinline__ void init(const T *p, int64_t ld_, int n, int li, int lg) {
+  __device__ __forceinline__ void init(const T *p, int64_t ld_, int n, int li, int lg, int = 0) {
     ld = ld_;
     at = p + min(li * W::VEC, n - W::VEC) + lg * W::VEC * ld;
   }
@@ -129,22 +133,23 @@ template <typename T> struct Across {
 template <typename T, int MODE, int FR, int FC>
 __global__ void __launch_bounds__(64 * WAVES) group_few_kernel(GroupArgs a, int NT) {
   using F = Few<T>;
-  constexpr bool BT = MODE == GROUP_DX;
+  constexpr bool BT = group_across(MODE), PAIR = MODE == GROUP_GATED;
   constexpr int AHEAD = (BT ? 20 : 16) / (FR + FC);  // steps whose loads are in flight
   static_assert(!BT || FC == F::VEC, "");
+  static_assert(!PAIR || FC % 2 == 0, "gates' fragments, then the values'");
   __shared__ f32x4_t part[WAVES / 2][FR * FC][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int li = lane & 15, lg = lane >> 4;
   int g, row0, row1, nt;
   if (!tile_of<false>(a.off, a.G, a.M, 16 * FR, NT, blockIdx.x, g, row0, row1, nt)) return;
-  const int c0 = nt * 16 * FC, Q = a.Q;
+  const int c0 = nt * group_outputs(MODE, 16 * FC), Q = a.Q;
   const T *w = (const T *)a.b + g * a.b_gs, *x = (const T *)a.a + (int64_t)row0 * a.lda;
   Along<T, FR> ax[AHEAD];
   std::conditional_t<BT, Across<T>, Along<T, FC>> bw[AHEAD];
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i) {
     ax[i].init(x, a.lda, row1 - row0, li, lg);
-    bw[i].init(w + (BT ? c0 : (int64_t)c0 * a.ldb), a.ldb, a.N - c0, li, lg);
+    bw[i].init(w + (BT ? c0 : (int64_t)c0 * a.ldb), a.ldb, a.N - c0, li, lg, PAIR ? a.N : 0);
   }
   f32x4_t acc[FR][FC];
 #pragma unroll
@@ -200,11 +205,11 @@ __global__ void __launch_bounds__(64 * WAVES) group_few_kernel(GroupArgs a, int 
   }
   __syncthreads();
   // four columns of a row at a time: of fragment fc, or of index 4 lg + i of fragments j .. j + 3
-  constexpr int QUADS = FR * FC * 64;
+  constexpr int FO = group_outputs(MODE, FC), QUADS = FR * FO * 64;
 #pragma unroll
   for (int e = threadIdx.x; e < QUADS; e += 64 * WAVES) {
-    const int f = e / (FC * 64), fc = e / 64 % FC, m = row0 + 16 * f + li;
-    f32x4_t v = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    const int f = e / (FO * 64), fc = e / 64 % FO, m = row0 + 16 * f + li;
+    f32x4_t v = f32x4_t{0.f, 0.f, 0.f, 0.f}, u = v;
     int c;
     if constexpr (BT) {
       const int i = fc & 3, first = c0 + (4 * lg + i) * F::VEC, over = max(first + F::VEC - a.N, 0);
@@ -218,14 +223,20 @@ __global__ void __launch_bounds__(64 * WAVES) group_few_kernel(GroupArgs a, int 
     } else {
       c = c0 + 16 * fc + 4 * lg;
 #pragma unroll
-      for (int p = 0; p < WAVES / 2; ++p) v += part[p][f * FC + fc][lane];
+      for (int p = 0; p < WAVES / 2; ++p) {
+        v += part[p][f * FC + fc][lane];
+        if (PAIR) u += part[p][f * FC + FO + fc][lane];
+      }
     }
-    if (m < row1 && c < a.N) finish<T, MODE>(a, g, m, c, v);
+    if (m >= row1 || c >= a.N) continue;
+    if constexpr (group_is_pair(MODE)) finish_pair<T, MODE>(a, g, m, c, v, PAIR ? u : v);
+    else finish<T, MODE>(a, g, m, c, v);
   }
 }
 
 template <typename T, int MODE, int FR, int FC> hipError_t run(const GroupArgs &a, hipStream_t s) {
-  const int64_t NT = (a.N + 16 * FC - 1) / (16 * FC), blocks = tile_blocks(a.M, a.G, 16 * FR, NT);
+  constexpr int COLS = group_outputs(MODE, 16 * FC);
+  const int64_t NT = (a.N + COLS - 1) / COLS, blocks = tile_blocks(a.M, a.G, 16 * FR, NT);
   if (blocks > kMaxBlocks) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((group_few_kernel<T, MODE, FR, FC>), dim3((uint32_t)blocks), dim3(64 * WAVES), 0, s, a, (int)NT);
   return hipGetLastError();
@@ -234,8 +245,8 @@ template <typename T, int MODE, int FR, int FC> hipError_t run(const GroupArgs &
 // Workgroups if each has 32 rows and 32 columns (input gradient: 16 vectors'),
 // a group's last one half full on average.
 int64_t tiles32(int dtype, const GroupArgs &a, int mode) {
-  const int cols = mode == GROUP_FWD ? 32 : dtype == GCPSL_BF16 ? 128 : 64;
-  return ((int64_t)a.M + 16 * a.G) / 32 * ((a.N + cols - 1) / cols);
+  const int cols = !group_across(mode) ? 32 : dtype == GCPSL_BF16 ? 128 : 64;
+  return ((int64_t)a.M + 16 * a.G) / 32 * ((group_cols(a, mode) + cols - 1) / cols);
 }
 
 // Forward: at most four rows a group on average (or 16 in all), and few enough
@@ -251,6 +262,10 @@ bool few_rows(const GroupArgs &a) { return a.M <= std::max(16, std::min(4 * a.G,
 // 8 groups, 1,024 rows, 1024 -> 1024 (256), 11.1 and 9.9.
 template <typename T> hipError_t run(int dtype, int mode, const GroupArgs &a, hipStream_t s) {
   const int64_t tiles = tiles32(dtype, a, mode);
+  if (mode == GROUP_GATED)
+    return tiles <= 128 || few_rows(a) ? run<T, GROUP_GATED, 1, 2>(a, s) : run<T, GROUP_GATED, 2, 2>(a, s);
+  if (mode == GROUP_GATED_GRAD)
+    return tiles <= 128 ? run<T, GROUP_GATED_GRAD, 1, Few<T>::VEC>(a, s) : run<T, GROUP_GATED_GRAD, 2, Few<T>::VEC>(a, s);
   if (mode == GROUP_DX)
     return tiles <= 128 ? run<T, GROUP_DX, 1, Few<T>::VEC>(a, s) : run<T, GROUP_DX, 2, Few<T>::VEC>(a, s);
   if (tiles <= 64 || few_rows(a)) return run<T, GROUP_FWD, 1, 1>(a, s);
@@ -280,7 +295,7 @@ bool group_few_ok(int dtype, const GroupArgs &a, int mode) {
   const int vec = bf16 ? 8 : 4;
   if (mode == GROUP_DW || a.Q < vec) return false;
   const int64_t tiles = tiles32(dtype, a, mode);
-  if (mode == GROUP_DX) return a.N >= vec && tiles <= (bf16 ? 320 : a.Q < 256 || !group_f32_deep_ok(a, mode) ? 512 : 256);
+  if (group_across(mode)) return a.N >= vec && tiles <= (bf16 ? 320 : a.Q < 256 || !group_f32_deep_ok(a, mode) ? 512 : 256);
   return few_rows(a) || tiles <= (!bf16 ? (a.Q < 256 ? 768 : 304) : (a.lda | a.ldb) & 1 ? 256 : 640);
 }
 

@@ -61,7 +61,8 @@ template <bool T, int PIECES, int SETS> struct Stage {
   u32x4 v[SETS][PIECES];
   static constexpr int NEXT = T ? 16 * 256 : 32 * 128;  // bytes from piece to piece in LDS
 
-  __device__ __forceinline__ void init(const void *p, int64_t ld, int n, int tid) {
+  // pair: rows from the gates' to the values' of a gated layer, the pieces of the second half of the rows (0: none)
+  __device__ __forceinline__ void init(const void *p, int64_t ld, int n, int tid, int pair = 0) {
     base = (const char *)p;
     step = T ? ld * (2 * BK) : 2 * BK;
     if constexpr (T) {
@@ -79,7 +80,8 @@ template <bool T, int PIECES, int SETS> struct Stage {
       at = row * 128 + (chunk ^ swz_row(row)) * 16;
 #pragma unroll
       for (int j = 0; j < PIECES; ++j)
-        off[j] = (uint32_t)min(row + 32 * j, n - 1) * (uint32_t)ld * 2u + (uint32_t)chunk * 16u;
+        off[j] = (uint32_t)(pair ? min(row + 32 * (j & 1), n - 1) + (j >> 1) * pair : min(row + 32 * j, n - 1)) *
+                     (uint32_t)ld * 2u + (uint32_t)chunk * 16u;
     }
   }
   __device__ __forceinline__ void load_all(int set) {
@@ -139,7 +141,7 @@ struct Tile {
 // The tile's sums and results; waves of 16 FM x 64 outputs.
 template <int MODE, int FM, int SETS>
 __device__ __forceinline__ void group_mid_tile(const GroupArgs &a, const Tile &t, char *lds) {
-  constexpr bool AT = MODE == GROUP_DW, BT = MODE != GROUP_FWD;
+  constexpr bool AT = MODE == GROUP_DW, BT = group_across(MODE), PAIR = MODE == GROUP_GATED;
   constexpr int FN = 4;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1, li = lane & 15, lg = lane >> 4;
@@ -147,7 +149,7 @@ __device__ __forceinline__ void group_mid_tile(const GroupArgs &a, const Tile &t
   Stage<AT, FM, SETS> sa;  // half a tile has half of A's rows
   Stage<BT, 4, SETS> sb;
   sa.init(t.A, a.lda, t.rows, tid);
-  sb.init(t.B, a.ldb, t.cols, tid);
+  sb.init(t.B, a.ldb, t.cols, tid, PAIR ? a.N : 0);
   f32x4_t acc[FM][FN], bacc[2];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
@@ -223,9 +225,12 @@ __device__ __forceinline__ void group_mid_tile(const GroupArgs &a, const Tile &t
   // The results go through LDS, 32 FM rows of 512 bytes, so that whole rows of
   // the tile are written at once.
   const auto place = [&](int r, int c) { return lds + r * 512 + ((c >> 2) ^ ((r & 7) << 2)) * 16; };
-  const int r0 = tid >> 4, c8 = (tid & 15) * 8;  // forward, input gradient: this thread's first row and its columns
-  const FinishRows<bf16_t, MODE == GROUP_DW ? GROUP_FWD : MODE, 2 * FM> out(a, t.g, t.row0 + r0, 16, t.row0 + t.rows,
-                                                                            t.c0 + c8);
+  // forward, input gradient: this thread's first row and its columns
+  constexpr int LANES = group_outputs(MODE, BN) / 8, STEP = 256 / LANES, ROWS = 32 * FM / STEP;
+  const int r0 = tid / LANES, c8 = tid % LANES * 8;
+  using Finish = std::conditional_t<group_is_pair(MODE), FinishPairs<bf16_t, MODE, ROWS>,
+                                    FinishRows<bf16_t, MODE == GROUP_DX ? GROUP_DX : GROUP_FWD, ROWS>>;
+  const Finish out(a, t.g, t.row0 + r0, STEP, t.row0 + t.rows, t.c0 + c8);
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -241,15 +246,20 @@ __device__ __forceinline__ void group_mid_tile(const GroupArgs &a, const Tile &t
       const int m = (wm * FM + i) * 16 + li;
       if (t.sums && lg == 0 && (i & 1) == wn && m < t.rows) store_bias_grad(a, t.g, t.slot, t.row0 + m, bacc[i >> 1][0]);
     }
+  } else if constexpr (group_is_pair(MODE)) {
+    out.store(a, [&](int i, int j, int half) {
+      return *(const f32x4_t *)place(r0 + STEP * i, half * (BN / 2) + c8 + 4 * j);
+    });
   } else {
-    out.store(a, [&](int i, int j) { return *(const f32x4_t *)place(r0 + 16 * i, c8 + 4 * j); });
+    out.store(a, [&](int i, int j) { return *(const f32x4_t *)place(r0 + STEP * i, c8 + 4 * j); });
   }
 }
 
 // BM: rows of a tile, 128 or 64.
 template <int MODE, int BM>
 __global__ void __launch_bounds__(256, 2) group_mid_kernel(GroupArgs a, int NT) {
-  constexpr bool BT = MODE != GROUP_FWD;
+  constexpr bool BT = group_across(MODE);
+  constexpr int COLS = group_outputs(MODE, BN);
   __shared__ __attribute__((aligned(1024))) char lds[2 * BUFFER];
   Tile t{(const bf16_t *)a.a, (const bf16_t *)a.b, 0, 0, 0, 0, 0, a.Q, -1, false};
   int nt;
@@ -269,11 +279,11 @@ __global__ void __launch_bounds__(256, 2) group_mid_kernel(GroupArgs a, int NT) 
     int row1;
     if (!tile_of<BM == 128>(a.off, a.G, a.M, BM, NT, blockIdx.x, t.g, t.row0, row1, nt)) return;
     t.rows = row1 - t.row0;
-    t.c0 = nt * BN;
+    t.c0 = nt * COLS;
     t.A += (int64_t)t.row0 * a.lda;
     t.B += t.g * a.b_gs + (BT ? (int64_t)t.c0 : (int64_t)t.c0 * a.ldb);
   }
-  t.cols = min(BN, a.N - t.c0);
+  t.cols = min(COLS, a.N - t.c0);
   t.sums = MODE == GROUP_DW && a.db != nullptr && nt == 0;
   if constexpr (BM == 64) group_mid_tile<MODE, 2, 2>(a, t, lds);
   else if (MODE != GROUP_DW && t.rows <= BM / 2) group_mid_tile<MODE, 2, 1>(a, t, lds);
@@ -281,7 +291,8 @@ __global__ void __launch_bounds__(256, 2) group_mid_kernel(GroupArgs a, int NT) 
 }
 
 template <int MODE, int BM> hipError_t run_tiles(const GroupArgs &a, hipStream_t s) {
-  const int64_t NT = (a.N + BN - 1) / BN;
+  constexpr int COLS = group_outputs(MODE, BN);
+  const int64_t NT = (a.N + COLS - 1) / COLS;
   const int64_t blocks = MODE == GROUP_DW ? piece_blocks(a, (int64_t)((a.M + BM - 1) / BM) * NT)
                                           : tile_blocks(a.M, a.G, BM, NT);
   if (blocks > kMaxBlocks) return hipErrorInvalidConfiguration;
@@ -297,7 +308,7 @@ template <int MODE, int BM> hipError_t run_tiles(const GroupArgs &a, hipStream_t
 template <int MODE> hipError_t run_mode(const GroupArgs &a, hipStream_t s) {
   if constexpr (MODE != GROUP_DW) {
     // a group's last tile half full on average
-    const int64_t tiles = ((int64_t)a.M + 32 * a.G) / 64 * ((a.N + BN - 1) / BN);
+    const int64_t tiles = ((int64_t)a.M + 32 * a.G) / 64 * ((group_cols(a, MODE) + BN - 1) / BN);
     if (tiles <= 2 * kCUs) return run_tiles<MODE, 64>(a, s);
   }
   return run_tiles<MODE, 128>(a, s);
@@ -306,13 +317,19 @@ template <int MODE> hipError_t run_mode(const GroupArgs &a, hipStream_t s) {
 }  // namespace
 
 // Eight elements at least in the operands' rows, and row strides whose offsets
-// within a tile fit 32 bits.
+// within a tile fit 32 bits (gated: those from a gate's row to its value's, too).
 bool group_mid_ok(int dtype, const GroupArgs &a, int mode) {
-  return dtype == GCPSL_BF16 && a.lda <= kMaxTileLd && a.ldb <= kMaxTileLd && (mode == GROUP_FWD || a.N >= 8) &&
+  if (mode == GROUP_GATED && ((int64_t)a.N + 128) * a.ldb >= (int64_t)1 << 31) return false;
+  return dtype == GCPSL_BF16 && a.lda <= kMaxTileLd && a.ldb <= kMaxTileLd && (!group_across(mode) || a.N >= 8) &&
          (mode == GROUP_DW ? a.M >= 8 : a.Q >= 8);
 }
 
 hipError_t launch_group_mid(int mode, const GroupArgs &a, hipStream_t s) {
-  return mode == GROUP_FWD ? run_mode<GROUP_FWD>(a, s)
-                           : mode == GROUP_DX ? run_mode<GROUP_DX>(a, s) : run_mode<GROUP_DW>(a, s);
+  switch (mode) {
+    case GROUP_FWD: return run_mode<GROUP_FWD>(a, s);
+    case GROUP_DX: return run_mode<GROUP_DX>(a, s);
+    case GROUP_DW: return run_mode<GROUP_DW>(a, s);
+    case GROUP_GATED: return run_mode<GROUP_GATED>(a, s);
+    default: return run_mode<GROUP_GATED_GRAD>(a, s);
+  }
 }

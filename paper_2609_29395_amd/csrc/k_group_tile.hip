@@ -60,8 +60,10 @@ __device__ __forceinline__ int swz_col(int row) { return ((row & 3) | ((row >> 1
 template <bool T> struct Copies {
   uint32_t off[2][2];
   int q[2];
-  // T: columns [0, n) of rows of stride ld; else rows [0, n)
-  __device__ __forceinline__ Copies(int wave, int lane, int64_t ld, int n) {
+  // T: columns [0, n) of rows of stride ld; else rows [0, n), or (PAIR) in either
+  // half rows [0, n) of its own
+  template <bool PAIR = false>
+  __device__ __forceinline__ Copies(int wave, int lane, int64_t ld, int n, std::bool_constant<PAIR> = {}) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int byte = j * 8192 + wave * 1024 + lane * 16;
@@ -78,7 +80,7 @@ template <bool T> struct Copies {
         q[j] = chunk * 8;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int r = h * HALF + row;
+          const int r = (PAIR ? 0 : h * HALF) + row;
           off[h][j] = r < n ? ((uint32_t)r * (uint32_t)ld + (uint32_t)(chunk * 8)) * 2u : kOob;
         }
       }
@@ -121,7 +123,7 @@ __device__ __forceinline__ u32x4 join(const u32x2 &lo, const u32x2 &hi) {
               "ds_read_b128 %4, %13\n\tds_read_b128 %5, %13 offset:2048\n\t"                    \
               "ds_read_b128 %6, %13 offset:4096\n\tds_read_b128 %7, %13 offset:6144\n\t"
 __device__ __forceinline__ void read_phase(FragA &A, FragB &B, const uint32_t (&a)[2], const uint32_t (&b)[2],
-                                           std::integral_constant<int, GROUP_FWD>) {
+                                           std::integral_constant<int, GROUP_FWD>) {  // (and GROUP_GATED)
   asm volatile(ROW_A
                "ds_read_b128 %8, %14\n\tds_read_b128 %9, %14 offset:2048\n\t"
                "ds_read_b128 %10, %15\n\tds_read_b128 %11, %15 offset:2048\n\t"
@@ -217,7 +219,8 @@ template <int N> __device__ __forceinline__ void wait_copies() {
 
 template <int MODE>
 __global__ void __launch_bounds__(512, 2) group_tile_kernel(GroupArgs a, int NT) {
-  constexpr bool AT = MODE == GROUP_DW, BT = MODE != GROUP_FWD;
+  constexpr bool AT = MODE == GROUP_DW, BT = group_across(MODE), PAIR = MODE == GROUP_GATED;
+  constexpr int COLS = group_outputs(MODE, BN);
   constexpr int NA = AT ? FM : 2;  // fragment addresses of A
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -242,19 +245,20 @@ __global__ void __launch_bounds__(512, 2) group_tile_kernel(GroupArgs a, int NT)
     int row1;
     if (!tile_of(a.off, a.G, a.M, BM, NT, blockIdx.x, g, row0, row1, nt)) return;
     rows = row1 - row0;
-    c0 = nt * BN;
+    c0 = nt * COLS;
     Q = a.Q;
     A = (const char *)a.a + (int64_t)row0 * a.lda * 2;
     B = (const char *)a.b + (g * a.b_gs + (BT ? (int64_t)c0 : (int64_t)c0 * a.ldb)) * 2;
   }
-  const int cols = min(BN, a.N - c0), nk = (Q + BK - 1) / BK;
+  const int cols = min(COLS, a.N - c0), nk = (Q + BK - 1) / BK;
   const int64_t stepA = AT ? a.lda * (BK * 2) : BK * 2, stepB = BT ? a.ldb * (BK * 2) : BK * 2;
   const Copies<AT> ca(wave, lane, a.lda, rows);
-  const Copies<BT> cb(wave, lane, a.ldb, cols);
+  const Copies<BT> cb(wave, lane, a.ldb, cols, std::bool_constant<PAIR>{});
+  const char *const B1 = PAIR ? B + (int64_t)a.N * a.ldb * 2 : B;  // of the second half's copies
   char *const dst = smem + wave * 1024;
   const auto copyA = [&](int kt, int h) { issue<AT>(ca, A, stepA, kt, Q, h, dst + (kt & 1) * STAGE + h * HALF_BYTES); };
   const auto copyB = [&](int kt, int h) {
-    issue<BT>(cb, B, stepB, kt, Q, h, dst + (kt & 1) * STAGE + (2 + h) * HALF_BYTES);
+    issue<BT>(cb, h ? B1 : B, stepB, kt, Q, h, dst + (kt & 1) * STAGE + (2 + h) * HALF_BYTES);
   };
 
   // fragment addresses in the first halves of the first stage
@@ -325,7 +329,7 @@ __global__ void __launch_bounds__(512, 2) group_tile_kernel(GroupArgs a, int NT)
     __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);
   };
-  using Mode = std::integral_constant<int, MODE>;
+  using Mode = std::integral_constant<int, AT ? GROUP_DW : BT ? GROUP_DX : GROUP_FWD>;  // as the operands lie
   // addresses d bytes on
   const auto at_a = [&](uint32_t d, uint32_t(&r)[NA]) {
 #pragma unroll
@@ -343,7 +347,7 @@ __global__ void __launch_bounds__(512, 2) group_tile_kernel(GroupArgs a, int NT)
       char *const d = dst + p * (3 * HALF_BYTES);
       issue<AT>(ca, A, stepA, kt, Q, 0, d);
       issue<BT>(cb, B, stepB, kt, Q, 0, d + HALF_BYTES);
-      issue<BT>(cb, B, stepB, kt, Q, 1, d + 2 * HALF_BYTES);
+      issue<BT>(cb, B1, stepB, kt, Q, 1, d + 2 * HALF_BYTES);
     };
     copy(0, 0);
     copy(1, 1);
@@ -416,31 +420,50 @@ __global__ void __launch_bounds__(512, 2) group_tile_kernel(GroupArgs a, int NT)
 
   // The results go through LDS, a half at a time, so that whole rows of the
   // tile are written at once.
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    if (h * HALF >= rows) break;
+  const auto half = [&](int h, const auto &sum) {
     const int high = min(HALF, rows - h * HALF), m0 = row0 + h * HALF;
-    // forward, input gradient: two rows a wave, eight columns a lane
-    const int r0 = wave * 2 + (lane >> 5), c = (lane & 31) * 8;
-    const FinishRows<bf16_t, MODE == GROUP_DW ? GROUP_FWD : MODE, HALF / 16, false> out(a, g, m0 + r0, 16, m0 + high,
-                                                                                        c0 + c);
+    // forward, input gradient: two rows a wave, eight columns a lane (gated: four rows)
+    constexpr int LANES = COLS / 8, STEP = 512 / LANES;
+    const int r0 = tid / LANES, c = (lane & (LANES - 1)) * 8;
+    using Finish = std::conditional_t<group_is_pair(MODE), FinishPairs<bf16_t, MODE, HALF / STEP>,
+                                      FinishRows<bf16_t, MODE == GROUP_DX ? GROUP_DX : GROUP_FWD, HALF / STEP, false>>;
+    const Finish out(a, g, m0 + r0, STEP, m0 + high, c0 + c);
     __syncthreads();
+    sum([&](const f32x4_t(&v)[FM][2][FN]) {
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+      for (int i = 0; i < FM; ++i)
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
-          *(f32x4_t *)(smem + ((wm * FM + i) * 16 + li) * OUT_ROW + (k * HALF + (wn * FN + j) * 16 + 4 * lg) * 4) =
-              acc[h][i][k][j];
+          for (int j = 0; j < FN; ++j)
+            *(f32x4_t *)(smem + ((wm * FM + i) * 16 + li) * OUT_ROW + (k * HALF + (wn * FN + j) * 16 + 4 * lg) * 4) = v[i][k][j];
+    });
     __syncthreads();
     if constexpr (MODE == GROUP_DW) {  // a row a wave
       const int c4 = c0 + lane * 4;
       if (c4 < a.N)
         for (int r = wave; r < high; r += 8)
           store_grad(a, g, slot, m0 + r, c4, *(const f32x4_t *)(smem + r * OUT_ROW + lane * 16));
+    } else if constexpr (group_is_pair(MODE)) {
+      out.store(a, [&](int i, int j, int k) {
+        return *(const f32x4_t *)(smem + (r0 + STEP * i) * OUT_ROW + (k * HALF + c + 4 * j) * 4);
+      });
     } else {
-      out.store(a, [&](int i, int j) { return *(const f32x4_t *)(smem + (r0 + 16 * i) * OUT_ROW + (c + 4 * j) * 4); });
+      out.store(a, [&](int i, int j) { return *(const f32x4_t *)(smem + (r0 + STEP * i) * OUT_ROW + (c + 4 * j) * 4); });
+    }
+  };
+  if constexpr (group_is_pair(MODE)) {  // one copy of the activations' code
+#pragma unroll 1
+    for (int h = 0; h * HALF < rows; ++h)
+      half(h, [&](auto put) {
+        if (h == 0) put(acc[0]);
+        else put(acc[1]);
+      });
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (h * HALF >= rows) break;
+      half(h, [&](auto put) { put(acc[h]); });
     }
   }
   if (sums && lg == 0) {
@@ -460,7 +483,8 @@ template <int MODE> hipError_t run(const GroupArgs &a, hipStream_t s) {
     if (e != hipSuccess) return e;
     once.mark();
   }
-  const int64_t NT = (a.N + BN - 1) / BN;
+  constexpr int COLS = group_outputs(MODE, BN);
+  const int64_t NT = (a.N + COLS - 1) / COLS;
   const int64_t blocks = MODE == GROUP_DW ? piece_blocks(a, (int64_t)((a.M + BM - 1) / BM) * NT)
                                           : tile_blocks(a.M, a.G, BM, NT);
   if (blocks > kMaxBlocks / 2) return hipErrorInvalidConfiguration;  // (of 512 threads)
@@ -478,5 +502,11 @@ bool group_tile_ok(int dtype, const GroupArgs &a, int mode) {
 }
 
 hipError_t launch_group_tile(int mode, const GroupArgs &a, hipStream_t s) {
-  return mode == GROUP_FWD ? run<GROUP_FWD>(a, s) : mode == GROUP_DX ? run<GROUP_DX>(a, s) : run<GROUP_DW>(a, s);
+  switch (mode) {
+    case GROUP_FWD: return run<GROUP_FWD>(a, s);
+    case GROUP_DX: return run<GROUP_DX>(a, s);
+    case GROUP_DW: return run<GROUP_DW>(a, s);
+    case GROUP_GATED: return run<GROUP_GATED>(a, s);
+    default: return run<GROUP_GATED_GRAD>(a, s);
+  }
 }
