@@ -425,7 +425,7 @@ __global__ void __launch_bounds__(512, 2) group_tile_kernel(GroupArgs a, int NT)
     // forward, input gradient: two rows a wave, eight columns a lane (gated: four rows)
     constexpr int LANES = COLS / 8, STEP = 512 / LANES;
     const int r0 = tid / LANES, c = (lane & (LANES - 1)) * 8;
-    using Finish = std::conditional_t<group_is_pair(MODE), FinishPairs<bf16_t, MODE, HALF / STEP>,
+    using Finish = std::conditional_t<group_is_pair(MODE), FinishPairs<bf16_t, MODE, HALF / STEP, false>,
                                       FinishRows<bf16_t, MODE == GROUP_DX ? GROUP_DX : GROUP_FWD, HALF / STEP, false>>;
     const Finish out(a, g, m0 + r0, STEP, m0 + high, c0 + c);
     __syncthreads();
