@@ -377,7 +377,7 @@ extern "C" int gcpsl_group_residual_workspace_bytes(int32_t dtype, int32_t G, in
   alignas(4) static const int32_t none = 0;
   CHECK(bad_residual(dtype, G, rows, n, &none));
   if (rows > kMaxGroupRows) return fail(GCPSL_EUNSUPPORTED, "more than 2^31 - 1024 grouped rows");
-  *bytes = residual_bytes(residual_pieces(G, rows, n), n);
+  *bytes = residual_bytes(residual_pieces(dtype, G, rows, n), n);
   return GCPSL_OK;
 }
 
@@ -417,7 +417,7 @@ extern "C" int gcpsl_group_residual_norm_grad(
   CHECK(bad_vectors(dw_next, dw_next_gs, G, n, true));
   if (!aligned(r_block, 4) || !aligned(r_next, 4)) return fail(GCPSL_EINVAL, "tensor not aligned to its elements");
   if (!finite_f32(alpha) || !finite_f32(beta)) return fail(GCPSL_EINVAL, "alpha and beta must be finite");
-  const GroupPieces pieces = residual_pieces(G, rows, n);
+  const GroupPieces pieces = residual_pieces(dtype, G, rows, n);
   if (dw_block || dw_next) {
     if (residual_bytes(pieces, n) > workspace_bytes) return fail(GCPSL_EINVAL, "workspace too small");
     if (pieces.slots && (!workspace || !aligned(workspace, 16)))

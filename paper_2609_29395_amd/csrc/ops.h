@@ -111,7 +111,7 @@ struct ResidualGradArgs {
   int piece, slots;
   float *part;
 };
-GroupPieces residual_pieces(int G, int64_t rows, int n);
+GroupPieces residual_pieces(int dtype, int G, int64_t rows, int n);
 hipError_t launch_residual_grad(int dtype, const ResidualGradArgs &a, hipStream_t s);
 
 // ------------------------------------------------------------ distillation
