@@ -640,7 +640,8 @@ int gcpsl_score_grad(int32_t dtype, int64_t rows, int32_t L, const void *z, int6
  * class that the row rules out (-inf) and the teacher does not makes kl +inf, a
  * NaN or +inf among a row's logits or the entries left makes it NaN.  1 <= top
  * <= 256, 2^-10 <= T <= 2^10, 1 <= L <= 2^28.  kl, lse_t, logp and lse may be NULL
- * (labels too if logp is).  workspace: gcpsl_distill_workspace_bytes() bytes on
+ * (labels too if logp is).  The summation order depends on dtype, rows, L and the
+ * row's address modulo 16.  workspace: gcpsl_distill_workspace_bytes() bytes on
  * the device, 16-byte aligned (NULL if that is 0), used until the call's work on
  * the stream is done.
  */

@@ -18,6 +18,7 @@
 //
 // Bound: memory.
 #include <algorithm>
+#include <type_traits>
 
 #include "ops.h"
 #include "runtime.h"
@@ -26,6 +27,7 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_any __attribute__((aligned(2)));  // global memory takes 16-byte accesses at any alignment
+template <int N> using Count = std::integral_constant<int, N>;
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 __device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
@@ -39,21 +41,46 @@ template <typename T> struct Bits;  // the elements of a 16-byte vector
 template <> struct Bits<float> {
   static constexpr int VEC = 4;
   static __device__ __forceinline__ float at(const u32x4 &w, int j) { return __uint_as_float(w[j]); }
-  static __device__ __forceinline__ void drop_first(u32x4 &w, int n) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (j < n) w[j] = 0xff800000u;  // -inf
-  }
+  static __device__ __forceinline__ u32x4 none() { return u32x4{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u}; }  // -inf
 };
 template <> struct Bits<bf16_t> {
   static constexpr int VEC = 8;
   static __device__ __forceinline__ float at(const u32x4 &w, int j) {
     return __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
   }
-  static __device__ __forceinline__ void drop_first(u32x4 &w, int n) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < n) w[j >> 1] = j & 1 ? (w[j >> 1] & 0xffffu) | 0xff800000u : (w[j >> 1] & 0xffff0000u) | 0xff80u;
+  static __device__ __forceinline__ u32x4 none() { return u32x4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u}; }
+};
+
+// A part of a row: vectors [v0, v1) of those that lie on 16-byte boundaries of
+// `base` and, the first part, the row's classes before and behind them, one by one.
+// (Vectors from the row's first class on, at odd addresses: 4,096 rows of 50,021
+// classes, bf16, 93 and 195 us where DISTILL_TIMES do.)
+template <typename T> struct Part {
+  static constexpr int VEC = Bits<T>::VEC;
+  int head, behind, L;  // classes before the vectors, the first behind them
+  uint32_t v0, v1;
+  bool ends;            // takes them
+  __device__ __forceinline__ Part(const T *base, int L_, uint32_t part, uint32_t per) : L(L_) {
+    const int past = (int)(reinterpret_cast<uintptr_t>(base) / sizeof(T)) & (VEC - 1);
+    head = (VEC - past) & (VEC - 1);
+    const uint32_t all = (uint32_t)(L - head) / VEC;  // (rows here have more than 64 classes)
+    behind = head + (int)(all * VEC);
+    v0 = min(part * per, all);
+    v1 = min(v0 + per, all);
+    ends = part == 0;
+  }
+  // Class of the t-th one by itself, -1 if there is none.
+  __device__ __forceinline__ int single(int t) const {
+    if (!ends) return -1;
+    if (t < head) return t;
+    const int c = behind + (t - head);
+    return c < L ? c : -1;
+  }
+  __device__ __forceinline__ bool has(int c) const {
+    if ((unsigned)c >= (unsigned)L) return false;
+    if (c < head || c >= behind) return ends;
+    const uint32_t v = (uint32_t)(c - head) / VEC;
+    return v >= v0 && v < v1;
   }
 };
 
@@ -68,11 +95,10 @@ template <int W> __device__ __forceinline__ float lanes_sum(float v) {
   for (int d = W / 2; d; d >>= 1) v += __shfl_xor(v, d, W);
   return v;
 }
-// Over a row's TPR threads; buf [4].
+// Over a row's TPR threads; buf [4], each used once.
 template <int TPR> __device__ __forceinline__ float row_max(float v, float *buf) {
   v = lanes_max<TPR == 256 ? 64 : TPR>(v);
   if constexpr (TPR == 256) {
-    __syncthreads();
     if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
     __syncthreads();
     v = fmaxf(fmaxf(buf[0], buf[1]), fmaxf(buf[2], buf[3]));
@@ -82,7 +108,6 @@ template <int TPR> __device__ __forceinline__ float row_max(float v, float *buf)
 template <int TPR> __device__ __forceinline__ float row_sum(float v, float *buf) {
   v = lanes_sum<TPR == 256 ? 64 : TPR>(v);
   if constexpr (TPR == 256) {
-    __syncthreads();
     if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
     __syncthreads();
     v = (buf[0] + buf[1]) + (buf[2] + buf[3]);
@@ -166,48 +191,66 @@ template <typename T, int W> __device__ __forceinline__ void write_row(const Dis
   if (t == 0) a.kl[row] = sum == 0.f ? 0.f : part / sum - log_of(sum);
 }
 
-constexpr int kAhead = 4;  // vectors of a thread in flight
+// f(N, whole, v) for a thread's vectors of [v0, v1): N of them from v + t on, TPR apart,
+// four while all threads have as many, then as many as any has left (whole false).
+template <int TPR, typename F> __device__ __forceinline__ void each_batch(uint32_t v0, uint32_t v1, F f) {
+  uint32_t v = v0;
+  for (; v + 4 * TPR <= v1; v += 4 * TPR) f(Count<4>{}, std::true_type{}, v);
+  const uint32_t left = v1 - v;
+  if (left > 3 * TPR) f(Count<4>{}, std::false_type{}, v);
+  else if (left > 2 * TPR) f(Count<3>{}, std::false_type{}, v);
+  else if (left > TPR) f(Count<2>{}, std::false_type{}, v);
+  else if (left > 0) f(Count<1>{}, std::false_type{}, v);
+}
+// The row of this thread among those of its workgroup, in a scalar register where a wave has one.
+template <int TPR> __device__ __forceinline__ int row_in_block() {
+  const int i = (int)threadIdx.x / TPR;
+  return TPR >= 64 ? __builtin_amdgcn_readfirstlane(i) : i;
+}
 
 // Part `job` % parts of row `job` / parts by TPR threads; a part is `per` vectors.  TWO: both sums.
 template <typename T, int TPR, bool TWO>
 __global__ void __launch_bounds__(256) distill_kernel(DistillArgs a, uint32_t jobs, FastDiv fd_parts, uint32_t per) {
   using B = Bits<T>;
-  constexpr int VEC = B::VEC, GROUPS = 256 / TPR;
+  constexpr int VEC = B::VEC, GROUPS = 256 / TPR, LANES = TPR < 64 ? TPR : 64;
   __shared__ float4 wsum[4];
   const int t = threadIdx.x % TPR, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t job = blockIdx.x * GROUPS + (TPR == 256 ? 0 : wave);
-  if (job >= jobs) return;  // (a wave's own row where it shares the workgroup)
+  const uint32_t job = blockIdx.x * GROUPS + row_in_block<TPR>();
+  if (job >= jobs) return;  // (rows that share a workgroup share no barrier, those that share a wave no shuffle)
   const int64_t row = fdiv(job, fd_parts);
-  const uint32_t part = job - (uint32_t)row * fd_parts.d;
   const T *z = (const T *)a.z + row * a.ldz;
-  const int L = a.L;
-  const uint32_t vectors = ((uint32_t)L + VEC - 1) / VEC, v0 = part * per, v1 = min(vectors, v0 + per);
+  const Part<T> part(z, a.L, job - (uint32_t)row * fd_parts.d, per);
+  const T *vectors = z + part.head;
   const float inv_t = 1.f / a.temperature, ct = kLog2e * inv_t;
   Sums p{-INFINITY, 0.f, 0.f};
-  for (uint32_t v = v0; v < v1; v += kAhead * TPR) {
-    u32x4 w[kAhead];
+  const int single = part.single(t);
+  if (single >= 0) {
+    const float x = ElemT<T>::to_f(z[single]);
+    p.m = fmaxf(p.m, x);
+    const float d = x - base_of(p.m);
+    p.t = exp_of(d * inv_t);
+    p.s = exp_of(d);
+  }
+  each_batch<TPR>(part.v0, part.v1, [&](auto count, auto whole, uint32_t v) {
+    constexpr int N = decltype(count)::value;
+    constexpr bool WHOLE = decltype(whole)::value;
+    u32x4 w[N];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const uint32_t i = (v + u * TPR + t) * VEC;
-      w[u] = *(const u32x4_any *)(z + min(i, (uint32_t)(L - VEC)));
+    for (int u = 0; u < N; ++u) {
+      const uint32_t i = v + u * TPR + t;
+      w[u] = *(const u32x4 *)(vectors + (WHOLE ? i : min(i, part.v1 - 1)) * VEC);
     }
-    if (v + kAhead * TPR >= v1) {  // the part's last vectors: without what is the next part's or counted before
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const uint32_t at = v + u * TPR + t;
-        B::drop_first(w[u], at >= v1 ? VEC : max((int)(at * VEC + VEC) - L, 0));
-      }
-    }
+    if (!WHOLE && v + (N - 1) * TPR + t >= part.v1) w[N - 1] = B::none();
     float m = p.m;
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u)
+    for (int u = 0; u < N; ++u)
 #pragma unroll
       for (int j = 0; j < VEC; ++j) m = fmaxf(m, B::at(w[u], j));
     rebase(p, m, inv_t);
     const float base = base_of(m);
     float t2[2] = {0.f, 0.f}, s2[2] = {0.f, 0.f};
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u)
+    for (int u = 0; u < N; ++u)
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         const float d = B::at(w[u], j) - base;
@@ -216,8 +259,8 @@ __global__ void __launch_bounds__(256) distill_kernel(DistillArgs a, uint32_t jo
       }
     p.t += t2[0] + t2[1];
     p.s += s2[0] + s2[1];
-  }
-  lanes_join<64>(p, inv_t);
+  });
+  lanes_join<LANES>(p, inv_t);
   if constexpr (TPR == 256) {
     if ((threadIdx.x & 63) == 0) wsum[wave] = make_float4(p.m, p.t, p.s, 0.f);
     __syncthreads();
@@ -229,7 +272,7 @@ __global__ void __launch_bounds__(256) distill_kernel(DistillArgs a, uint32_t jo
   if (fd_parts.d > 1) {
     if (t == 0) ((float4 *)a.work)[job] = make_float4(p.m, p.t, p.s, 0.f);
   } else {
-    write_row<T, 64>(a, row, p, t);
+    write_row<T, LANES>(a, row, p, t);
   }
 }
 
@@ -276,24 +319,20 @@ template <typename T> __global__ void __launch_bounds__(256) distill_small_kerne
 struct GradRow {
   float gk, lse_t, gl, lse, inv_t;
   int y;
-  __device__ __forceinline__ GradRow(const DistillGradArgs &a, int64_t row, bool teacher) : lse_t(0.f), lse(0.f), y(-1) {
+  __device__ __forceinline__ GradRow(const DistillGradArgs &a, int64_t row) {
     inv_t = 1.f / a.temperature;
-    gk = gl = 0.f;
-    if (a.g_kl && teacher) {
-      lse_t = a.lse_t[row];
-      if (!(lse_t <= kRuledOut)) gk = a.g_kl[row] * inv_t;
-      else lse_t = 0.f;
+    gk = a.g_kl ? a.g_kl[row] * inv_t : 0.f;
+    lse_t = a.g_kl ? a.lse_t[row] : 0.f;
+    gl = a.g_logp ? a.g_logp[row] : 0.f;
+    lse = a.g_logp ? a.lse[row] : 0.f;
+    y = a.g_logp ? a.labels[row] : -1;
+    if (lse <= kRuledOut || (unsigned)y >= (unsigned)a.L) {
+      gl = lse = 0.f;
+      y = -1;
     }
-    if (a.g_logp) {
-      const int label = a.labels[row];
-      lse = a.lse[row];
-      if ((unsigned)label < (unsigned)a.L && !(lse <= kRuledOut)) {
-        gl = a.g_logp[row];
-        y = label;
-      } else {
-        lse = 0.f;
-      }
-    }
+  }
+  __device__ __forceinline__ void teach(bool teacher) {
+    if (lse_t <= kRuledOut || !teacher) gk = lse_t = 0.f;
   }
   // of the dense terms and the label
   __device__ __forceinline__ float operator()(float x, int i) const {
@@ -309,81 +348,73 @@ template <typename T, int TPR>
 __global__ void __launch_bounds__(256) distill_grad_kernel(DistillGradArgs a, uint32_t jobs, FastDiv fd_parts, uint32_t per) {
   using B = Bits<T>;
   constexpr int VEC = B::VEC, GROUPS = 256 / TPR;
-  __shared__ float buf[4], weight_[GROUPS][kMaxTeacher], logit_[GROUPS][kMaxTeacher];
-  __shared__ int class_[GROUPS][kMaxTeacher];
-  const int t = threadIdx.x % TPR, grp = TPR == 256 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  float *weight = weight_[grp], *logit = logit_[grp];
-  int *cls = class_[grp];
+  __shared__ float buf[2][4];
+  extern __shared__ float teacher[];  // of every row: weights, logits and classes [top]
+  const int t = threadIdx.x % TPR, grp = row_in_block<TPR>(), top = a.g_kl ? a.top : 0;
+  float *weight = teacher + grp * 3 * top, *logit = weight + top;
+  int *cls = (int *)(logit + top);
   const uint32_t job = blockIdx.x * GROUPS + grp;
   if (job >= jobs) return;
   const int64_t row = fdiv(job, fd_parts);
-  const uint32_t part = job - (uint32_t)row * fd_parts.d;
   const T *z = (const T *)a.z + row * a.ldz;
   T *dz = (T *)a.dz + row * a.lddz;
-  const int L = a.L, top = a.g_kl ? a.top : 0;
-  const uint32_t vectors = ((uint32_t)L + VEC - 1) / VEC, v0 = part * per, v1 = min(vectors, v0 + per);
-  const uint32_t c0 = v0 * VEC, c1 = min((uint32_t)L, v1 * VEC);  // the part's classes
+  const Part<T> part(dz, a.L, job - (uint32_t)row * fd_parts.d, per);  // (z may lie otherwise: loads at any alignment)
   const float inv_t = 1.f / a.temperature;
 
   // the teacher's classes: weights, and the logits of those in this part (read before anything of it is written)
+  GradRow grad(a, row);
   float best = -INFINITY, sum = 0.f;
-  bool any = false;
   for (int k = t; k < top; k += TPR) {
     int c = a.t_class[row * a.top + k];
     const float v = a.t_value[row * a.top + k];
-    if ((unsigned)c >= (unsigned)L || v == -INFINITY) c = -1;
+    if ((unsigned)c >= (unsigned)a.L || v == -INFINITY) c = -1;
     cls[k] = c;
     weight[k] = v;
-    if (c >= 0) {
-      best = fmaxf(best, v);
-      any = true;
-    }
-    logit[k] = (uint32_t)c - c0 < c1 - c0 ? ElemT<T>::to_f(z[c]) : 0.f;
+    if (c >= 0) best = fmaxf(best, v);
+    logit[k] = part.has(c) ? ElemT<T>::to_f(z[c]) : 0.f;
   }
+  const int single = part.single(t);
+  const float single_logit = single >= 0 ? ElemT<T>::to_f(z[single]) : 0.f;
   if (top) {
-    best = base_of(row_max<TPR>(best, buf));
+    best = base_of(row_max<TPR>(best, buf[0]));
     for (int k = t; k < top; k += TPR) {
       const float w = cls[k] >= 0 ? exp_of((weight[k] - best) * inv_t) : 0.f;
       weight[k] = w;
       sum += w;
     }
-    sum = row_sum<TPR>(sum, buf);
-    any = row_max<TPR>(any ? 1.f : 0.f, buf) > 0.f;
+    sum = row_sum<TPR>(sum, buf[1]);
   }
-  const GradRow grad(a, row, any);
+  grad.teach(sum != 0.f);  // (an entry left has weight 1, or makes the sum NaN)
   row_sync<TPR>();
 
-  for (uint32_t v = v0; v < v1; v += kAhead * TPR) {
-    u32x4 w[kAhead];
+  if (single >= 0) dz[single] = ElemT<T>::from_f(grad(single_logit, single));
+  each_batch<TPR>(part.v0, part.v1, [&](auto count, auto whole, uint32_t v) {
+    constexpr int N = decltype(count)::value;
+    constexpr bool WHOLE = decltype(whole)::value;
+    u32x4 w[N];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const uint32_t at = v + u * TPR + t;
-      w[u] = u32x4{0, 0, 0, 0};
-      if (at < v1 && at * VEC + VEC <= (uint32_t)L) w[u] = *(const u32x4_any *)(z + at * VEC);
+    for (int u = 0; u < N; ++u) {
+      const uint32_t i = v + u * TPR + t;
+      w[u] = *(const u32x4_any *)(z + part.head + (WHOLE ? i : min(i, part.v1 - 1)) * VEC);
     }
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const uint32_t at = v + u * TPR + t;
-      if (at >= v1) break;
-      const int i = (int)(at * VEC);
-      if (i + VEC <= L) {
-        u32x4 o;
+    for (int u = 0; u < N; ++u) {
+      if (!WHOLE && u == N - 1 && v + u * TPR + t >= part.v1) break;
+      const int i = part.head + (int)((v + u * TPR + t) * VEC);
+      u32x4 o;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if constexpr (VEC == 4) o[j] = __float_as_uint(grad(B::at(w[u], j), i + j));
-          else o[j] = pack2_bf16(grad(B::at(w[u], 2 * j), i + 2 * j), grad(B::at(w[u], 2 * j + 1), i + 2 * j + 1));
-        }
-        *(u32x4_any *)(dz + i) = o;
-      } else {
-        for (int k = i; k < L; ++k) dz[k] = ElemT<T>::from_f(grad(ElemT<T>::to_f(z[k]), k));
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (VEC == 4) o[j] = __float_as_uint(grad(B::at(w[u], j), i + j));
+        else o[j] = pack2_bf16(grad(B::at(w[u], 2 * j), i + 2 * j), grad(B::at(w[u], 2 * j + 1), i + 2 * j + 1));
       }
+      *(u32x4 *)(dz + i) = o;
     }
-  }
-  if (!any || grad.gk == 0.f) return;
+  });
+  if (grad.gk == 0.f) return;  // (the same in all the row's threads)
   row_sync<TPR>();
   for (int k = t; k < top; k += TPR) {
     const int c = cls[k];
-    if ((uint32_t)c - c0 >= c1 - c0) continue;
+    if (!part.has(c)) continue;
     float q = 0.f;
     for (int j = 0; j < top; ++j)
       if (cls[j] == c) q += weight[j];
@@ -405,14 +436,9 @@ template <typename T> __global__ void __launch_bounds__(256) distill_grad_small_
   float x[4], q[4] = {0.f, 0.f, 0.f, 0.f}, best = -INFINITY, sum = 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) x[i] = i * 16 + lane < a.L ? ElemT<T>::to_f(z[i * 16 + lane]) : 0.f;
-  bool any = false;
   for (int k = lane; k < top; k += 16)
-    if ((unsigned)tc[k] < (unsigned)a.L && tv[k] != -INFINITY) {
-      best = fmaxf(best, tv[k]);
-      any = true;
-    }
+    if ((unsigned)tc[k] < (unsigned)a.L) best = fmaxf(best, tv[k]);
   best = base_of(lanes_max<16>(best));
-  any = lanes_max<16>(any ? 1.f : 0.f) > 0.f;
   for (int k = 0; k < top; ++k) {  // every lane all entries, in the same order
     const int c = tc[k];
     if ((unsigned)c >= (unsigned)a.L || tv[k] == -INFINITY) continue;
@@ -421,7 +447,8 @@ template <typename T> __global__ void __launch_bounds__(256) distill_grad_small_
 #pragma unroll
     for (int i = 0; i < 4; ++i) q[i] += c == i * 16 + lane ? w : 0.f;
   }
-  const GradRow grad(a, row, any);
+  GradRow grad(a, row);
+  grad.teach(sum != 0.f);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int c = i * 16 + lane;
@@ -433,19 +460,20 @@ template <typename T> __global__ void __launch_bounds__(256) distill_grad_small_
 }
 
 // Vectors of a part, and parts of a row: whole rows where they are enough for
-// every CU to have four workgroups, else parts of 2,048 vectors at least.
+// every CU to have four workgroups, else parts of 1,024 vectors at least.
 struct Parts {
-  bool wave;  // a wave a row
+  int threads;  // of a row: 16 and 64 with more of them in a workgroup
   uint32_t n, per;
 };
 template <typename T> Parts parts_of_row(int64_t rows, int L) {
   const uint32_t vectors = ((uint32_t)L + Bits<T>::VEC - 1) / Bits<T>::VEC;
-  if (vectors <= 64 * kAhead) return {true, 1, vectors};
-  const uint32_t step = 256 * kAhead;
+  if (vectors <= 32) return {16, 1, vectors};
+  if (vectors <= 256) return {64, 1, vectors};
+  const uint32_t step = 1024;
   const int64_t most = (vectors + step - 1) / step, want = (1024 + rows - 1) / std::max<int64_t>(rows, 1);
   const uint32_t n = (uint32_t)std::max<int64_t>(1, std::min(most, want));
   const uint32_t per = ((vectors + n - 1) / n + step - 1) / step * step;
-  return {false, (vectors + per - 1) / per, per};
+  return {256, (vectors + per - 1) / per, per};
 }
 
 template <typename P> P *entry_at(P *p, int64_t r) { return p ? p + r : nullptr; }
@@ -469,11 +497,13 @@ template <typename T> hipError_t run(const DistillArgs &all, hipStream_t s) {
       hipLaunchKernelGGL(distill_small_kernel<T>, dim3((uint32_t)((a.rows + 15) / 16)), dim3(256), 0, s, a);
     } else {
       const uint32_t jobs = (uint32_t)(a.rows * parts.n);
+      const uint32_t at_once = 256 / parts.threads;
       const auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(parts.wave ? (jobs + 3) / 4 : jobs), dim3(256), 0, s, a, jobs,
-                           make_fastdiv(parts.n), parts.per);
+        hipLaunchKernelGGL(kernel, dim3((jobs + at_once - 1) / at_once), dim3(256), 0, s, a, jobs, make_fastdiv(parts.n),
+                           parts.per);
       };
-      if (parts.wave) two ? launch(distill_kernel<T, 64, true>) : launch(distill_kernel<T, 64, false>);
+      if (parts.threads == 16) two ? launch(distill_kernel<T, 16, true>) : launch(distill_kernel<T, 16, false>);
+      else if (parts.threads == 64) two ? launch(distill_kernel<T, 64, true>) : launch(distill_kernel<T, 64, false>);
       else two ? launch(distill_kernel<T, 256, true>) : launch(distill_kernel<T, 256, false>);
       if (parts.n > 1)
         hipLaunchKernelGGL(distill_join_kernel<T>, dim3((uint32_t)((a.rows + 3) / 4)), dim3(256), 0, s, a, parts.n);
@@ -503,11 +533,14 @@ template <typename T> hipError_t run_grad(const DistillGradArgs &all, hipStream_
       hipLaunchKernelGGL(distill_grad_small_kernel<T>, dim3((uint32_t)((a.rows + 15) / 16)), dim3(256), 0, s, a);
     } else {
       const uint32_t jobs = (uint32_t)(a.rows * parts.n);
+      const uint32_t at_once = 256 / parts.threads;
+      const size_t lds = sizeof(float) * 3 * at_once * (a.g_kl ? a.top : 0);
       const auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(parts.wave ? (jobs + 3) / 4 : jobs), dim3(256), 0, s, a, jobs,
-                           make_fastdiv(parts.n), parts.per);
+        hipLaunchKernelGGL(kernel, dim3((jobs + at_once - 1) / at_once), dim3(256), lds, s, a, jobs, make_fastdiv(parts.n),
+                           parts.per);
       };
-      if (parts.wave) launch(distill_grad_kernel<T, 64>);
+      if (parts.threads == 16) launch(distill_grad_kernel<T, 16>);
+      else if (parts.threads == 64) launch(distill_grad_kernel<T, 64>);
       else launch(distill_grad_kernel<T, 256>);
     }
     const hipError_t e = hipGetLastError();

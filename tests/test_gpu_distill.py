@@ -127,11 +127,16 @@ def test_strides_in_place_and_what_lies_beside(L, dtype):
     wide = torch.full((8, L + 3), math.nan, dtype=T, device="cuda")
     v = wide[:7, 1:L + 1]
     v.copy_(z)
-    want, dz = run_both(z, cls, val, 2.0, labels)
+    # the sums' order goes by the rows' addresses: within the bounds, not the same bits as elsewhere
     got = gcpsl.distill(v, gpu(cls), gpu(val), temperature=2.0, labels=gpu(labels))
-    assert all(torch.equal(a, b) for a, b in zip(got, want))
-    g = {"g_kl": gpu(make(9, 7) + 0.5), "g_logp": gpu(make(10, 7))}
-    out = gcpsl.distill_grad(v, gpu(cls), gpu(val), got.lse_t, temperature=2.0, labels=gpu(labels), lse=got.lse, **g, out=v)
+    want = blocks.distill(z, cls, val, 2.0, labels)
+    for k, t in got._asdict().items():
+        check(t, *want[k], k)
+    g_kl, g_logp = make(9, 7) + 0.5, make(10, 7)
+    args = dict(temperature=2.0, labels=gpu(labels), lse=got.lse, g_kl=gpu(g_kl), g_logp=gpu(g_logp))
+    dz = gcpsl.distill_grad(v, gpu(cls), gpu(val), got.lse_t, **args)
+    check(dz, *blocks.distill_grad(z, cls, val, got.lse_t.cpu(), 2.0, labels, got.lse.cpu(), g_kl, g_logp), "dz")
+    out = gcpsl.distill_grad(v, gpu(cls), gpu(val), got.lse_t, **args, out=v)
     assert out is v and torch.equal(v, dz)
     assert torch.isnan(wide[7]).all() and torch.isnan(wide[:, 0]).all() and torch.isnan(wide[:, L + 1:]).all()
 
