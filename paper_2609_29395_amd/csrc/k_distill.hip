@@ -12,11 +12,15 @@
 // w_k = e^((v_k - max v) / T) and W their sum, kl = sum_k w_k (log w_k - log p_k) / W
 // - log W, from `top` logits of the row.
 //
-// Gradient: the dense terms go over the row; then, behind a barrier, the
-// teacher's classes of the part are written again with their q_k, which all
-// entries of a class sum in the same order (no atomics: the same bits always).
+// Gradient: the dense terms go over the part; then, behind a barrier, the
+// teacher's classes in it are written again with their q_k, which all entries of a
+// class sum in the same order (no atomics: the same bits always).
 //
-// Bound: memory.
+// Bound: memory.  bf16, 4,096 rows: 131,072 classes at T = 2 190 us forward (5.6
+// TB/s), 355 the gradient (6.0, where a copy reaches 5.0); 50,021 classes 76 and 152
+// (5.4 both).  Short rows by their latency, the teacher's entries and their logits
+// being loads after loads: 65,536 rows of 1,000 classes 43 and 68 us.  One row of
+// 131,072 classes 7 and 6 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -54,7 +58,7 @@ template <> struct Bits<bf16_t> {
 // A part of a row: vectors [v0, v1) of those that lie on 16-byte boundaries of
 // `base` and, the first part, the row's classes before and behind them, one by one.
 // (Vectors from the row's first class on, at odd addresses: 4,096 rows of 50,021
-// classes, bf16, 93 and 195 us where DISTILL_TIMES do.)
+// classes, bf16, 93 and 195 us where 78 and 180 do.)
 template <typename T> struct Part {
   static constexpr int VEC = Bits<T>::VEC;
   int head, behind, L;  // classes before the vectors, the first behind them
@@ -156,35 +160,53 @@ struct RowLog {
   __device__ __forceinline__ float logp(float x) const { return empty ? -INFINITY : fmaf(x - base, inv, -ls); }
 };
 
+// What a row's results need beside its sums: the label's logit (lane 0), the lane's
+// first entry and its class's logit, loaded before the row is read, as each takes
+// a load after another.
+template <typename T> struct RowEnds {
+  int y, c;
+  float label, v, x;
+  __device__ __forceinline__ RowEnds(const DistillArgs &a, int64_t row, int t) : y(-1), c(-1), label(0.f), v(0.f), x(0.f) {
+    const T *z = (const T *)a.z + row * a.ldz;
+    if (a.logp && t == 0) y = a.labels[row];
+    if (a.kl && t < a.top) entry(a, row, t, c, v, x);
+    if ((unsigned)y < (unsigned)a.L) label = ElemT<T>::to_f(z[y]);
+  }
+  // entry k of the row; c -1 if it is left out
+  static __device__ __forceinline__ void entry(const DistillArgs &a, int64_t row, int k, int &c, float &v, float &x) {
+    c = a.t_class[row * a.top + k];
+    v = a.t_value[row * a.top + k];
+    if ((unsigned)c < (unsigned)a.L) x = ElemT<T>::to_f(((const T *)a.z)[row * a.ldz + c]);
+    else c = -1;
+  }
+};
+
 // Results of a row from its sums, by W lanes (this one is lane t).  a.temperature 1: the two sums are one.
-template <typename T, int W> __device__ __forceinline__ void write_row(const DistillArgs &a, int64_t row, const Sums &p, int t) {
+template <typename T, int W>
+__device__ __forceinline__ void write_row(const DistillArgs &a, int64_t row, const Sums &p, int t, const RowEnds<T> &ends) {
   const float inv_t = 1.f / a.temperature;
   const RowLog soft(p.m, p.t, inv_t);
-  const T *z = (const T *)a.z + row * a.ldz;
   if (t == 0) {
     const RowLog plain(p.m, a.temperature == 1.f ? p.t : p.s, 1.f);
     if (a.lse_t) a.lse_t[row] = soft.lse;
     if (a.lse) a.lse[row] = plain.lse;
-    if (a.logp) {
-      const int y = a.labels[row];
-      a.logp[row] = (unsigned)y < (unsigned)a.L ? plain.logp(ElemT<T>::to_f(z[y])) : 0.f;
-    }
+    if (a.logp) a.logp[row] = (unsigned)ends.y < (unsigned)a.L ? plain.logp(ends.label) : 0.f;
   }
   if (!a.kl) return;
-  const int32_t *tc = a.t_class + row * a.top;
-  const float *tv = a.t_value + row * a.top;
-  float best = -INFINITY;
-  for (int k = t; k < a.top; k += W)
-    if ((unsigned)tc[k] < (unsigned)a.L) best = fmaxf(best, tv[k]);
+  float best = ends.c >= 0 ? fmaxf(-INFINITY, ends.v) : -INFINITY;
+  for (int k = t + W; k < a.top; k += W)
+    if ((unsigned)a.t_class[row * a.top + k] < (unsigned)a.L) best = fmaxf(best, a.t_value[row * a.top + k]);
   best = base_of(lanes_max<W>(best));
   float sum = 0.f, part = 0.f;
+  int c = ends.c;
+  float v = ends.v, x = ends.x;
   for (int k = t; k < a.top; k += W) {
-    const int c = tc[k];
-    if ((unsigned)c >= (unsigned)a.L) continue;
-    const float d = (tv[k] - best) * inv_t, w = exp_of(d);
+    if (k != t) RowEnds<T>::entry(a, row, k, c, v, x);
+    if (c < 0) continue;
+    const float d = (v - best) * inv_t, w = exp_of(d);
     if (w == 0.f) continue;  // (-inf, or so far below that its term is 0)
     sum += w;
-    part = fmaf(w, d - soft.logp(ElemT<T>::to_f(z[c])), part);
+    part = fmaf(w, d - soft.logp(x), part);
   }
   sum = lanes_sum<W>(sum);
   part = lanes_sum<W>(part);
@@ -223,6 +245,8 @@ __global__ void __launch_bounds__(256) distill_kernel(DistillArgs a, uint32_t jo
   const T *vectors = z + part.head;
   const float inv_t = 1.f / a.temperature, ct = kLog2e * inv_t;
   Sums p{-INFINITY, 0.f, 0.f};
+  const bool last = fd_parts.d == 1 && (TPR < 256 || wave == 0);  // writes the results
+  const RowEnds<T> ends(a, row, last ? t : INT32_MAX);
   const int single = part.single(t);
   if (single >= 0) {
     const float x = ElemT<T>::to_f(z[single]);
@@ -272,7 +296,7 @@ __global__ void __launch_bounds__(256) distill_kernel(DistillArgs a, uint32_t jo
   if (fd_parts.d > 1) {
     if (t == 0) ((float4 *)a.work)[job] = make_float4(p.m, p.t, p.s, 0.f);
   } else {
-    write_row<T, LANES>(a, row, p, t);
+    write_row<T, LANES>(a, row, p, t, ends);
   }
 }
 
@@ -283,10 +307,11 @@ template <typename T> __global__ void __launch_bounds__(256) distill_join_kernel
   if (row >= a.rows) return;
   const float inv_t = 1.f / a.temperature;
   const float4 *work = (const float4 *)a.work + row * parts;
+  const RowEnds<T> ends(a, row, lane);
   Sums p{-INFINITY, 0.f, 0.f};
   for (uint32_t i = lane; i < parts; i += 64) join(p, Sums{work[i].x, work[i].y, work[i].z}, inv_t);
   lanes_join<64>(p, inv_t);
-  write_row<T, 64>(a, row, p, lane);
+  write_row<T, 64>(a, row, p, lane, ends);
 }
 
 // Rows of at most 64 classes: 16 lanes a row.
@@ -296,6 +321,7 @@ template <typename T> __global__ void __launch_bounds__(256) distill_small_kerne
   if (job >= a.rows) return;  // (shuffles stay within the 16 lanes)
   const T *z = (const T *)a.z + job * a.ldz;
   const float inv_t = 1.f / a.temperature;
+  const RowEnds<T> ends(a, job, lane);
   float x[4], m = -INFINITY;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -311,7 +337,7 @@ template <typename T> __global__ void __launch_bounds__(256) distill_small_kerne
   }
   p.t = lanes_sum<16>(p.t);
   p.s = lanes_sum<16>(p.s);
-  write_row<T, 16>(a, job, p, lane);
+  write_row<T, 16>(a, job, p, lane, ends);
 }
 
 // --------------------------------------------------------------- gradient
@@ -361,45 +387,47 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(DistillGradArgs a, ui
   const Part<T> part(dz, a.L, job - (uint32_t)row * fd_parts.d, per);  // (z may lie otherwise: loads at any alignment)
   const float inv_t = 1.f / a.temperature;
 
-  // the teacher's classes: weights, and the logits of those in this part (read before anything of it is written)
-  GradRow grad(a, row);
-  float best = -INFINITY, sum = 0.f;
-  for (int k = t; k < top; k += TPR) {
-    int c = a.t_class[row * a.top + k];
-    const float v = a.t_value[row * a.top + k];
-    if ((unsigned)c >= (unsigned)a.L || v == -INFINITY) c = -1;
-    cls[k] = c;
-    weight[k] = v;
-    if (c >= 0) best = fmaxf(best, v);
-    logit[k] = part.has(c) ? ElemT<T>::to_f(z[c]) : 0.f;
-  }
-  const int single = part.single(t);
-  const float single_logit = single >= 0 ? ElemT<T>::to_f(z[single]) : 0.f;
-  if (top) {
-    best = base_of(row_max<TPR>(best, buf[0]));
-    for (int k = t; k < top; k += TPR) {
-      const float w = cls[k] >= 0 ? exp_of((weight[k] - best) * inv_t) : 0.f;
-      weight[k] = w;
-      sum += w;
-    }
-    sum = row_sum<TPR>(sum, buf[1]);
-  }
-  grad.teach(sum != 0.f);  // (an entry left has weight 1, or makes the sum NaN)
-  row_sync<TPR>();
-
-  if (single >= 0) dz[single] = ElemT<T>::from_f(grad(single_logit, single));
-  each_batch<TPR>(part.v0, part.v1, [&](auto count, auto whole, uint32_t v) {
-    constexpr int N = decltype(count)::value;
-    constexpr bool WHOLE = decltype(whole)::value;
-    u32x4 w[N];
+  const auto load = [&](auto count, auto whole, uint32_t v, auto &w) {
 #pragma unroll
-    for (int u = 0; u < N; ++u) {
+    for (int u = 0; u < decltype(count)::value; ++u) {
       const uint32_t i = v + u * TPR + t;
-      w[u] = *(const u32x4_any *)(z + part.head + (WHOLE ? i : min(i, part.v1 - 1)) * VEC);
+      w[u] = *(const u32x4_any *)(z + part.head + (decltype(whole)::value ? i : min(i, part.v1 - 1)) * VEC);
     }
+  };
+  GradRow grad(a, row);
+  float sum = 0.f;
+  // the teacher's classes: weights, and the logits of those in this part (read before anything of it is written)
+  const auto teach = [&] {
+    float best = -INFINITY;
+    for (int k = t; k < top; k += TPR) {
+      int c = a.t_class[row * a.top + k];
+      const float v = a.t_value[row * a.top + k];
+      if ((unsigned)c >= (unsigned)a.L || v == -INFINITY) c = -1;
+      cls[k] = c;
+      weight[k] = v;
+      if (c >= 0) best = fmaxf(best, v);
+      logit[k] = part.has(c) ? ElemT<T>::to_f(z[c]) : 0.f;
+    }
+    const int single = part.single(t);
+    const float x = single >= 0 ? ElemT<T>::to_f(z[single]) : 0.f;
+    if (top) {
+      best = base_of(row_max<TPR>(best, buf[0]));
+      for (int k = t; k < top; k += TPR) {
+        const float w = cls[k] >= 0 ? exp_of((weight[k] - best) * inv_t) : 0.f;
+        weight[k] = w;
+        sum += w;
+      }
+      sum = row_sum<TPR>(sum, buf[1]);
+    }
+    grad.teach(sum != 0.f);  // (an entry left has weight 1, or makes the sum NaN)
+    row_sync<TPR>();
+    if (single >= 0) dz[single] = ElemT<T>::from_f(grad(x, single));
+  };
+  const auto finish = [&](auto count, auto whole, uint32_t v, const auto &w) {
+    constexpr int N = decltype(count)::value;
 #pragma unroll
     for (int u = 0; u < N; ++u) {
-      if (!WHOLE && u == N - 1 && v + u * TPR + t >= part.v1) break;
+      if (!decltype(whole)::value && u == N - 1 && v + u * TPR + t >= part.v1) break;
       const int i = part.head + (int)((v + u * TPR + t) * VEC);
       u32x4 o;
 #pragma unroll
@@ -409,7 +437,22 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(DistillGradArgs a, ui
       }
       *(u32x4 *)(dz + i) = o;
     }
+  };
+  // Rows of a wave load their first vectors before the teacher's entries are taken,
+  // which is a chain of loads (65,536 rows of 1,000 classes, bf16: 73 and 68 us); a
+  // workgroup would wait for them at its barriers (4,096 rows of 6,000: 24 and 28).
+  bool taught = TPR == 256;
+  if (taught) teach();
+  each_batch<TPR>(part.v0, part.v1, [&](auto count, auto whole, uint32_t v) {
+    u32x4 w[decltype(count)::value];
+    load(count, whole, v, w);
+    if (!taught) {  // (the same in all the row's threads)
+      teach();
+      taught = true;
+    }
+    finish(count, whole, v, w);
   });
+  if (!taught) teach();
   if (grad.gk == 0.f) return;  // (the same in all the row's threads)
   row_sync<TPR>();
   for (int k = t; k < top; k += TPR) {
@@ -460,17 +503,20 @@ template <typename T> __global__ void __launch_bounds__(256) distill_grad_small_
 }
 
 // Vectors of a part, and parts of a row: whole rows where they are enough for
-// every CU to have four workgroups, else parts of 1,024 vectors at least.
+// every CU to have four workgroups, else parts of 1,024 vectors at least; the
+// gradient, which has no parts to join, in such parts always: of 4,096 rows of
+// 50,021 classes, bf16, in whole rows 180 us, in parts of 2,048 166, of 1,024 152 and
+// of 512 200.
 struct Parts {
   int threads;  // of a row: 16 and 64 with more of them in a workgroup
   uint32_t n, per;
 };
-template <typename T> Parts parts_of_row(int64_t rows, int L) {
+template <typename T> Parts parts_of_row(int64_t rows, int L, int64_t groups = 1024) {
   const uint32_t vectors = ((uint32_t)L + Bits<T>::VEC - 1) / Bits<T>::VEC;
   if (vectors <= 32) return {16, 1, vectors};
   if (vectors <= 256) return {64, 1, vectors};
   const uint32_t step = 1024;
-  const int64_t most = (vectors + step - 1) / step, want = (1024 + rows - 1) / std::max<int64_t>(rows, 1);
+  const int64_t most = (vectors + step - 1) / step, want = (groups + rows - 1) / std::max<int64_t>(rows, 1);
   const uint32_t n = (uint32_t)std::max<int64_t>(1, std::min(most, want));
   const uint32_t per = ((vectors + n - 1) / n + step - 1) / step * step;
   return {256, (vectors + per - 1) / per, per};
@@ -515,7 +561,7 @@ template <typename T> hipError_t run(const DistillArgs &all, hipStream_t s) {
 }
 
 template <typename T> hipError_t run_grad(const DistillGradArgs &all, hipStream_t s) {
-  const Parts parts = parts_of_row<T>(all.rows, all.L);
+  const Parts parts = parts_of_row<T>(all.rows, all.L, (int64_t)1 << 40);
   const int64_t slab = kMaxBlocks / parts.n;
   for (int64_t r = 0; r < all.rows; r += slab) {
     DistillGradArgs a = all;
