@@ -6,9 +6,11 @@ differ.  Here the split model is kept as it is; a layer with ReLU and dropout an
 on the pooled features of all its examples, the rows of all clusters one after another and every operator one launch
 for all of them (gcpsl.group_forward, dropout, score and their gradients).
 
-    python -m paper_2609_29395_amd.heads [--workload tiny_epoch] [--steps 60] [--dtype f32]
+    python -m paper_2609_29395_amd.heads [--workload tiny_epoch] [--steps 60] [--dtype f32] [--blocks 2]
 
-runs a workload, fuses it, and prints each cluster's loss, accuracy, top classes and entropy before and after.
+runs a workload, fuses it, and prints each cluster's loss, accuracy, top classes and entropy before and after.  With
+--blocks, deeper heads follow (residual gated blocks), which learn from the labels and from the top classes that the
+fused heads give each row: what the other clusters know reaches a cluster's own head without their examples.
 PyTorch holds memory, casts the fp32 masters for bf16 products, and adds the SGD update.
 """
 from __future__ import annotations
@@ -85,6 +87,116 @@ class ClusterHeads:
         gcpsl.fuse_replicas(self.theta, sizes)
 
 
+class BlockHeads:
+    """Heads of G clusters on k features with residual gated blocks: a layer to d features, `depth` blocks
+
+        h = norm(x);  v = W_2 (silu(g) u) + b_2, (g, u) = W_1 h + b_1;  q = W_q h + b_q
+        x <- x + beta sigmoid(q) norm(v)
+
+    each norm with weights of its own per cluster, and a classifier on the last norm.  One fp32 vector per cluster,
+    [G][P], as for ClusterHeads."""
+
+    def __init__(self, G, k, d, hidden, L, depth=2, dtype="f32", lr=0.1, momentum=0.9, beta=1.0, eps=1e-6, seed=0):
+        self.G, self.depth, self.dtype, self.lr, self.momentum = G, depth, DTYPES[dtype], lr, momentum
+        self.beta, self.eps = float(beta), eps
+        self.shapes = {"w_in": (d, k), "b_in": (d,), "norm_in": (d,)}
+        for i in range(depth):
+            self.shapes.update({f"w1_{i}": (2 * hidden, d), f"b1_{i}": (2 * hidden,), f"w2_{i}": (d, hidden),
+                                f"b2_{i}": (d,), f"wq_{i}": (d, d), f"bq_{i}": (d,), f"norm_block_{i}": (d,),
+                                f"norm_next_{i}": (d,)})
+        self.shapes.update(w_out=(L, d), b_out=(L,))
+        gen = torch.Generator().manual_seed(int(seed))
+        one = torch.cat([(torch.ones(s) if name.startswith("norm") else torch.zeros(s) if name.startswith("b") else
+                          (torch.rand(s, generator=gen) * 2 - 1) * s[1] ** -0.5).flatten()
+                         for name, s in self.shapes.items()])
+        self.theta = one.cuda().repeat(G, 1).contiguous()  # every cluster starts alike
+        self.mom = torch.zeros_like(self.theta)
+        self.grad = torch.zeros_like(self.theta)
+
+    def _views(self, flat):
+        """{name: [G][..]} inside a [G][P] tensor."""
+        out, at = {}, 0
+        for name, s in self.shapes.items():
+            n = s[0] * (s[1] if len(s) == 2 else 1)
+            out[name] = flat[:, at:at + n].view(self.G, *s)
+            at += n
+        return out
+
+    def _forward(self, x, offsets, keep):
+        """(logits, what the backward pass needs)."""
+        p = {name: v.to(self.dtype) if v.dim() == 3 else v for name, v in self._views(self.theta).items()}
+        first = gcpsl.group_residual_norm(gcpsl.group_forward(x, offsets, p["w_in"], p["b_in"]), offsets,
+                                          w_next=p["norm_in"], eps=self.eps)
+        state, blocks = first, []
+        for i in range(self.depth):
+            h = state.h
+            gated = gcpsl.group_gated_forward(h, offsets, p[f"w1_{i}"], p[f"b1_{i}"], keep=keep)
+            v = gcpsl.group_forward(gated.y, offsets, p[f"w2_{i}"], p[f"b2_{i}"])
+            q = gcpsl.group_forward(h, offsets, p[f"wq_{i}"], p[f"bq_{i}"])
+            state = gcpsl.group_residual_norm(state.out, offsets, y=v, gate=q, w_block=p[f"norm_block_{i}"],
+                                              w_next=p[f"norm_next_{i}"], beta=self.beta, eps=self.eps)
+            blocks.append((h, gated, v, q, state) if keep else None)
+        return gcpsl.group_forward(state.h, offsets, p["w_out"], p["b_out"]), (p, first, blocks, state)
+
+    def logits(self, x, offsets):
+        return self._forward(x, offsets, False)[0]
+
+    def score(self, x, offsets, labels, top=1):
+        return gcpsl.score(self.logits(x, offsets), labels, top=top)
+
+    def _layer_grads(self, g, w, b, dy, x, offsets):
+        gcpsl.group_weight_grad(dy, x, offsets, dw=g[w], db=g[b])
+
+    def gradients(self, x, offsets, labels, row_weight, teacher=None, temperature=2.0, share=0.5):
+        """Fills self.grad with the gradient of every cluster's mean loss (row_weight [rows]: 1 / n_n); returns the
+        rows' losses.  teacher: (top classes, their values) [rows][K], as score gives them; the loss is then (1 - share)
+        of the labels' and share of T^2 times the divergence from the teacher at temperature T."""
+        z, (p, first, blocks, state) = self._forward(x, offsets, True)
+        g = self._views(self.grad)
+        if teacher is None:
+            s = gcpsl.score(z, labels)
+            loss = -s.logp
+            dz = gcpsl.score_grad(z, labels, s.lse, g_logp=-row_weight, out=z)
+        else:
+            weight = share * temperature ** 2
+            s = gcpsl.distill(z, *teacher, temperature=temperature, labels=labels)
+            loss = weight * s.kl - (1 - share) * s.logp
+            dz = gcpsl.distill_grad(z, *teacher, s.lse_t, temperature=temperature, labels=labels, lse=s.lse,
+                                    g_kl=weight * row_weight, g_logp=(share - 1) * row_weight, out=z)
+        self._layer_grads(g, "w_out", "b_out", dz, state.h, offsets)
+        g_out, g_h = None, gcpsl.group_input_grad(dz, offsets, p["w_out"])
+        for i in reversed(range(self.depth)):
+            h, gated, v, q, r = blocks[i]
+            d = gcpsl.group_residual_norm_grad(r.out, offsets, g_out=g_out, g_h=g_h, y=v, gate=q,
+                                               w_block=p[f"norm_block_{i}"], w_next=p[f"norm_next_{i}"],
+                                               r_block=r.r_block, r_next=r.r_next, beta=self.beta)
+            g[f"norm_block_{i}"].copy_(d.dw_block)
+            g[f"norm_next_{i}"].copy_(d.dw_next)
+            self._layer_grads(g, f"w2_{i}", f"b2_{i}", d.dy, gated.y, offsets)
+            dpre = gcpsl.group_gated_grad(d.dy, offsets, p[f"w2_{i}"], gated.pre)
+            self._layer_grads(g, f"w1_{i}", f"b1_{i}", dpre, h, offsets)
+            self._layer_grads(g, f"wq_{i}", f"bq_{i}", d.dgate, h, offsets)
+            g_out = d.dx
+            g_h = gcpsl.group_input_grad(dpre, offsets, p[f"w1_{i}"])
+            g_h += gcpsl.group_input_grad(d.dgate, offsets, p[f"wq_{i}"])
+        d = gcpsl.group_residual_norm_grad(first.out, offsets, g_out=g_out, g_h=g_h, w_next=p["norm_in"],
+                                           r_next=first.r_next)
+        g["norm_in"].copy_(d.dw_next)
+        self._layer_grads(g, "w_in", "b_in", d.dx, x, offsets)
+        return loss
+
+    def step(self, x, offsets, labels, row_weight, **distillation):
+        """One SGD step of every cluster; returns the rows' losses before it."""
+        loss = self.gradients(x, offsets, labels, row_weight, **distillation)
+        self.mom.mul_(self.momentum).add_(self.grad)
+        self.theta.sub_(self.mom, alpha=self.lr)
+        return loss
+
+    def fuse(self, sizes):
+        """Eq. 5 over the heads, by the clusters' example counts."""
+        gcpsl.fuse_replicas(self.theta, sizes)
+
+
 def cluster_features(ctx):
     """(x [rows][channels], labels [rows], offsets [C + 1], sizes [C]) of one epoch of every cluster: the pooled features
     that the split model gives each example, rows sorted by cluster.  The context runs its rounds, so one with lr 0 is
@@ -117,6 +229,7 @@ def main(argv=None):
     ap.add_argument("--steps", type=int, default=60)
     ap.add_argument("--hidden", type=int, default=64)
     ap.add_argument("--dtype", choices=sorted(DTYPES), default="f32")
+    ap.add_argument("--blocks", type=int, default=0, help="residual gated blocks of heads taught by the fused ones")
     a = ap.parse_args(argv)
     cfg = get_config(a.workload, schedule="epoch")
     ctx, _ = driver.setup(cfg)
@@ -132,8 +245,8 @@ def main(argv=None):
     heads = ClusterHeads(cfg["C"], x.shape[1], a.hidden, cfg["L"], dtype=a.dtype, seed=cfg["seed"])
     top = min(3, cfg["L"])
 
-    def report(what):
-        s = heads.score(x, offsets, labels, top=top)
+    def report(what, of=heads):
+        s = of.score(x, offsets, labels, top=top)
         loss, entropy = by_cluster(-s.logp, sizes), by_cluster(s.entropy, sizes)
         right = s.top_class == labels[:, None]
         first, among = by_cluster(right[:, 0], sizes), by_cluster(right.any(1), sizes)
@@ -148,6 +261,13 @@ def main(argv=None):
     after = report("after")
     heads.fuse(sizes)
     report("heads fused")
+    if a.blocks:
+        best = heads.score(x, offsets, labels, top=top)
+        deep = BlockHeads(cfg["C"], x.shape[1], a.hidden, a.hidden, cfg["L"], depth=a.blocks, dtype=a.dtype,
+                          seed=cfg["seed"])
+        for _ in range(a.steps):
+            deep.step(x, offsets, labels, weight, teacher=(best.top_class, best.top_logp))
+        report("blocks taught", deep)
     return before, after
 
 
