@@ -253,6 +253,15 @@ PyObject *tuple(std::initializer_list<const Tensor *> items, PyTypeObject *type)
   return t;
 }
 
+// Entries [first, ..) of a vector of 4-byte entries as a tensor of its own (five allocations took 1.3 us longer).
+Tensor part(const Tensor &held, int64_t first, at::IntArrayRef shape, at::ScalarType type) {
+  Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(held.storage()), held.key_set(),
+                                                      c10::scalarTypeToTypeMeta(type));
+  t.unsafeGetTensorImpl()->set_storage_offset(first);
+  t.unsafeGetTensorImpl()->set_sizes_contiguous(shape);
+  return t;
+}
+
 // group_weight_grad(dy, x, offsets, dw, db, bias)
 PyObject *group_weight_grad(PyObject *, PyObject *const *a, Py_ssize_t na) {
   return guarded(na, 6, [&] {
@@ -290,15 +299,6 @@ PyObject *dropout(PyObject *, PyObject *const *a, Py_ssize_t na) {
     call(entry.dropout, c.code, x.rows, x.cols, x.p, x.ld, p, seed, y.p, y.ld, c.stream);
     return THPVariable_Wrap(out);
   });
-}
-
-// Entries [first, ..) of a vector of 4-byte entries as a tensor of its own (five allocations took 1.3 us longer).
-Tensor part(const Tensor &held, int64_t first, at::IntArrayRef shape, at::ScalarType type) {
-  Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(held.storage()), held.key_set(),
-                                                      c10::scalarTypeToTypeMeta(type));
-  t.unsafeGetTensorImpl()->set_storage_offset(first);
-  t.unsafeGetTensorImpl()->set_sizes_contiguous(shape);
-  return t;
 }
 
 // score(logits, labels, top)
@@ -399,8 +399,10 @@ PyObject *group_residual_norm(PyObject *, PyObject *const *a, Py_ssize_t na) {
     const double alpha = number(a[6]), beta = number(a[7]), eps = number(a[8]);
     if ((!block && a[9] != Py_None) || (!next && a[10] != Py_None)) throw Irregular();
     Rows o, hr;
-    const Tensor out = block ? result(c, a[9], rows, n, o) : xt, h = next ? result(c, a[10], rows, n, hr) : Tensor(),
-                 r1 = first ? c.empty({rows}, at::kFloat) : Tensor(), r2 = next ? c.empty({rows}, at::kFloat) : Tensor();
+    const Tensor out = block ? result(c, a[9], rows, n, o) : xt, h = next ? result(c, a[10], rows, n, hr) : Tensor();
+    const Tensor held = first || next ? c.empty({rows * (first + next)}, at::kFloat) : Tensor();  // both rows' vectors
+    const Tensor r1 = first ? part(held, 0, {rows}, at::kFloat) : Tensor(),
+                 r2 = next ? part(held, first ? rows : 0, {rows}, at::kFloat) : Tensor();
     call(entry.residual_norm, c.code, g.n, rows, int32(n), g.offsets, x.p, x.ld, y.p, y.ld, gate.p, gate.ld,
          (const float *)w1.p, w1.stride, (const float *)w2.p, w2.stride, alpha, beta, eps, o.p, o.ld, hr.p, hr.ld,
          first ? (float *)r1.data_ptr() : nullptr, next ? (float *)r2.data_ptr() : nullptr, c.stream);
@@ -426,8 +428,10 @@ PyObject *group_residual_norm_grad(PyObject *, PyObject *const *a, Py_ssize_t na
     size_t need = 0;
     if (first || next) call(entry.residual_workspace_bytes, c.code, g.n, rows, int32(n), &need);
     const auto made = [&](bool is) { return is ? c.empty({rows, n}, c.type) : Tensor(); };
-    const auto summed = [&](bool is) { return is ? c.empty({g.n, n}, at::kFloat) : Tensor(); };
-    const Tensor dx = made(true), dy = made(block), dgate = made(gated), dw1 = summed(first), dw2 = summed(next),
+    const Tensor dx = made(true), dy = made(block), dgate = made(gated);
+    const Tensor held = first || next ? c.empty({g.n * n * (first + next)}, at::kFloat) : Tensor();  // both weights' gradients
+    const Tensor dw1 = first ? part(held, 0, {g.n, n}, at::kFloat) : Tensor(),
+                 dw2 = next ? part(held, first ? g.n * n : 0, {g.n, n}, at::kFloat) : Tensor(),
                  work = need ? c.empty({(int64_t)need}, at::kByte) : Tensor();
     const auto at = [](const Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
     call(entry.residual_norm_grad, c.code, g.n, rows, int32(n), g.offsets, x.p, x.ld, go.p, go.ld, gh.p, gh.ld, y.p, y.ld,

@@ -458,12 +458,14 @@ template <typename T, int VEC> GROUP_DEVICE void load_values(const T *p, float (
     }
   }
 }
-template <typename T, int VEC> GROUP_DEVICE void store_values(T *p, const float (&v)[VEC]) {
+template <typename T, int VEC, bool BY_CACHES = false> GROUP_DEVICE void store_values(T *p, const float (&v)[VEC]) {
   if constexpr (sizeof(T) == 4) {
-    static_assert(VEC == 4, "");
+    static_assert(VEC == 4 && !BY_CACHES, "");
     *(f32x4_any *)p = f32x4_any{v[0], v[1], v[2], v[3]};
   } else if constexpr (VEC == 8) {
-    *(u32x4_any *)p = u32x4_any{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])};
+    const u32x4_any o = {pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])};
+    if constexpr (BY_CACHES) __builtin_nontemporal_store(o, (u32x4_any *)p);
+    else *(u32x4_any *)p = o;
   } else {
     *(u32x2_any *)p = u32x2_any{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])};
   }
@@ -542,8 +544,10 @@ GROUP_DEVICE void finish_pair(const GroupArgs &a, int g, int m, int c, const V &
 // columns 4 j on, at acc(i, j, 0), GROUP_GATED those of the values at acc(i, j, 1).
 // The gradient's pairs are loaded for a batch of rows together, the first batch
 // before the sums are there and every other beside the one before it.  Vectors
-// that pass the columns (EDGES false: there are none) go the same way, loaded and
-// stored one by one.
+// that pass the columns go the same way, loaded and stored one by one.  EDGES false,
+// of the largest tiles: there are none, and what is read and written passes by the
+// caches, which such results do not fit (16,384 rows of 16 groups, 4096 -> 4096: the
+// gradient 483 us so, 516 else).
 template <typename T, int MODE, int ROWS, bool EDGES = true> struct FinishPairs {
   static constexpr int VEC = Vec16<T>::N, BATCH = ROWS < 4 ? ROWS : 4;
   static constexpr bool GRAD = MODE == GROUP_GATED_GRAD;
@@ -573,7 +577,9 @@ template <typename T, int MODE, int ROWS, bool EDGES = true> struct FinishPairs 
       const T *q = (const T *)a.pre + (int64_t)min(m0 + (i0 + i) * step, m1 - 1) * a.ldp + c;
 #pragma unroll
       for (int h = 0; h < 2; ++h, q += a.N) {
-        if (!EDGES || in == VEC) {
+        if (!EDGES) {
+          p.v[i][h] = __builtin_nontemporal_load((const u32x4_any *)q);
+        } else if (in == VEC) {
           p.v[i][h] = *(const u32x4_any *)q;
         } else {
 #pragma unroll
@@ -587,7 +593,7 @@ template <typename T, int MODE, int ROWS, bool EDGES = true> struct FinishPairs 
   }
   GROUP_DEVICE void put(T *p, const float (&v)[VEC]) const {
     if (!EDGES || in == VEC) {
-      store_values<T, VEC>(p, v);
+      store_values<T, VEC, !EDGES>(p, v);
     } else {
 #pragma unroll
       for (int j = 0; j < VEC - 1; ++j)

@@ -630,10 +630,14 @@ template <typename T, bool BLOCK> __global__ void __launch_bounds__(256) residua
   }
 }
 
-// The weights' gradients of a group of several pieces: 32 columns a workgroup, LANES
-// threads a column that take every LANES-th piece; their shares meet in LDS.
-template <int LANES> __global__ void __launch_bounds__(32 * LANES) residual_join_kernel(ResidualGradArgs a, uint32_t blocks) {
-  __shared__ float shares[LANES][32];
+// The weights' gradients of a group of several pieces: 128 columns of both together a
+// workgroup, four a thread and LANES threads a column that take every LANES-th
+// piece; their shares meet in LDS.
+constexpr int kJoinCols = 128;
+template <int LANES>
+__global__ void __launch_bounds__(kJoinCols / 4 * LANES) residual_join_kernel(ResidualGradArgs a, uint32_t blocks) {
+  typedef float f32x4_t __attribute__((ext_vector_type(4)));
+  __shared__ f32x4_t shares[LANES][kJoinCols / 4];
   const int g = (int)(blockIdx.x / blocks);
   uint32_t before = 0, slots = 0, n = 0, first = 0;
   for (int base = 0; base <= g; base += 64) {
@@ -649,22 +653,30 @@ template <int LANES> __global__ void __launch_bounds__(32 * LANES) residual_join
   n = __builtin_amdgcn_readfirstlane(n);
   first = __builtin_amdgcn_readfirstlane(first);
   if (n == 0 || first + n > (uint32_t)a.slots) return;
-  const int in = threadIdx.x % 32, lane = threadIdx.x / 32;
-  const int64_t c = (int64_t)(blockIdx.x - g * blocks) * 32 + in;  // of both weights' columns
-  const bool second = c >= a.n;
-  float *out = c >= 2 * (int64_t)a.n ? nullptr : second ? a.dw_next : a.dw_block;
-  float s = 0.f;
-  if (out) {
-    const float *p = a.part + (int64_t)first * 2 * a.n + c;
-#pragma unroll 8
-    for (uint32_t k = lane; k < n; k += LANES) s += p[(int64_t)k * 2 * a.n];
+  const int in = threadIdx.x % (kJoinCols / 4), lane = threadIdx.x / (kJoinCols / 4);
+  const int64_t all = 2 * (int64_t)a.n, c = (int64_t)(blockIdx.x - g * blocks) * kJoinCols + in * 4;
+  const float *p = a.part + (int64_t)first * all + c;
+  f32x4_t s = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  if (c + 4 <= all) {
+#pragma unroll 4
+    for (uint32_t k = lane; k < n; k += LANES) s += *(const f32x4_any *)(p + (int64_t)k * all);
+  } else {
+#pragma unroll
+    for (int r = 0; r < 3; ++r)
+      if (c + r < all)
+        for (uint32_t k = lane; k < n; k += LANES) s[r] += p[(int64_t)k * all + r];
   }
   shares[lane][in] = s;
   __syncthreads();
-  if (lane || !out) return;
+  if (lane) return;
 #pragma unroll
   for (int i = 1; i < LANES; ++i) s += shares[i][in];
-  out[second ? g * a.dwn_gs + (c - a.n) : g * a.dwb_gs + c] = s;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const bool second = c + r >= a.n;
+    float *out = second ? a.dw_next : a.dw_block;  // (a partial of what is not asked for holds anything)
+    if (c + r < all && out) out[second ? g * a.dwn_gs + (c + r - a.n) : g * a.dwb_gs + c + r] = s[r];
+  }
 }
 
 // 16-byte vectors of a row; rows of less than one go with those that nothing holds.
@@ -728,10 +740,10 @@ template <typename T, bool BLOCK> hipError_t run_grad(int dtype, const ResidualG
   }
   else e = launch(residual_grad_long_kernel<T, BLOCK>);
   if (e == hipSuccess && a.slots > 0 && (a.dw_block || a.dw_next)) {
-    const int64_t per = (2 * (int64_t)a.n + 31) / 32;
+    const int64_t per = (2 * (int64_t)a.n + kJoinCols - 1) / kJoinCols;
     if (per * a.G > kMaxBlocks / 4) return hipErrorInvalidConfiguration;
     const auto join = [&](auto kernel, int lanes) {
-      hipLaunchKernelGGL(kernel, dim3((uint32_t)(per * a.G)), dim3(32 * lanes), 0, s, a, (uint32_t)per);
+      hipLaunchKernelGGL(kernel, dim3((uint32_t)(per * a.G)), dim3(kJoinCols / 4 * lanes), 0, s, a, (uint32_t)per);
     };
     if (a.slots >= 64 * a.G) join(residual_join_kernel<32>, 32);
     else join(residual_join_kernel<8>, 8);
@@ -757,6 +769,7 @@ GroupPieces residual_pieces(int dtype, int G, int64_t rows, int n) {
   const int64_t least = tpr ? 4 * block / tpr : 4;
   int64_t piece = std::max<int64_t>((rows + target - 1) / target, least);
   if (!tpr) piece = std::min<int64_t>(piece, kLongPiece);  // (a piece has at most 1.6 times as many rows)
+  if (rows <= 2 * least) piece = std::max<int64_t>(rows, 1);  // one piece a group, and no join to launch
   // a group of p > 1 pieces has more than (p - 1/2) piece >= 3/4 p piece rows
   return {(int)piece, rows * 2 >= piece * 3 ? (int)(rows * 4 / (piece * 3)) : 0};
 }
