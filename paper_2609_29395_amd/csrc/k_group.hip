@@ -1,6 +1,6 @@
 // Products over rows grouped by cluster (gfx950): forward, input gradient and
-// weight gradient of one linear layer per group, the groups' rows one after
-// another and of any counts.
+// weight gradient of one linear layer per group, and a gated layer's forward pass
+// and gradient, the groups' rows one after another and of any counts.
 //
 // The group offsets are read on the device, so a launch depends on the number
 // of rows and groups only: it has as many row tiles as any offsets can need,

@@ -11,6 +11,10 @@
 // Two 24 KB buffers; two workgroups share a CU and one's splitting overlaps the
 // other's MFMAs.
 //
+// A gated layer's tile has 64 gates and then their 64 values among B's rows.  3,001
+// rows of 5 groups, 501 -> 333, gelu, pairs kept: 35 us; its gradient on 8,192 rows of 8
+// ragged groups, 1024 <- 1024, 137 us (125 TFLOP/s).
+//
 // Bound: what a k tile costs beside its MFMAs, which the matrix cores are busy
 // with 32 to 35 % of a launch: every value is split by each tile that reads it,
 // and every 16 of the sum take fragment reads and a barrier.  8 groups of 1,024

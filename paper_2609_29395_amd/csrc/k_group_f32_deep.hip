@@ -9,6 +9,8 @@
 // its team's tiles ahead and written to LDS, split, one ahead; a step costs one
 // barrier.  The teams' sums meet in LDS.
 //
+// A gated layer's tile has 32 gates and then their 32 values among B's rows.
+//
 // A k tile's small terms go to two sums in turn, as a wave has only one 32 x 32
 // fragment and an MFMA that waits for the one before it loses half its time.
 //

@@ -1,7 +1,7 @@
 // Forward products and input gradients of few rows, or of few results in all,
-// grouped by cluster (gfx950): serving a row or so of every cluster, where the
-// time is that of reading the weights, and products with fewer 128 x 128 tiles
-// than CUs.
+// grouped by cluster (gfx950), gated layers' among them: serving a row or so of
+// every cluster, where the time is that of reading the weights, and products with
+// fewer 128 x 128 tiles than CUs.
 //
 // A workgroup gives 16 or 32 rows x some columns of the result.  Its four waves
 // share the sum: each streams its quarter of the operands' rows from memory to
@@ -15,7 +15,7 @@
 // byte permute for each two elements.  A lane ends with VEC consecutive columns.
 //
 // Bound: few rows, by memory: 16 rows of 16 groups, 4096 -> 4096, bf16, 68 us
-// (5.4 TB/s).  Otherwise by what a CU loads, about 36 bytes a ns.
+// (5.4 TB/s), gated 135 (5.4).  Otherwise by what a CU loads, about 36 bytes a ns.
 #include "group.h"
 
 #include <type_traits>
@@ -290,6 +290,13 @@ template <typename T> hipError_t run(int dtype, int mode, const GroupArgs &a, hi
 //      fp32         4 groups, 500 rows, 1024 <- 4096 (272)           106   57
 //   input grad.,    5 groups, 433 rows, 4096 <- 1024 (128)           22    42
 //      bf16         8 groups, 1,024 rows, 1024 <- 1024 (288)         14.8  15.2
+//   gated layers, whose weights' rows count as columns,
+//      bf16         1 group, 128 rows, 1024 -> 1024 (256)            7.1   11.8
+//                   1 group, 256 rows, 1024 -> 2048 (1,024)          17.4  11.9
+//      fp32         1 group, 128 rows, 1024 -> 1024 (256)            11.2  18.2
+//                   4 groups, 300 rows, 1024 -> 512 (352)            21.9  18.1
+//   gradient, bf16  1 group, 128 rows, 4096 <- 4096 (128)            19.3  41.8
+//      fp32         1 group, 1,307 rows, 640 <- 512 (410)            19.4  13.8
 bool group_few_ok(int dtype, const GroupArgs &a, int mode) {
   const bool bf16 = dtype == GCPSL_BF16;
   const int vec = bf16 ? 8 : 4;

@@ -14,6 +14,8 @@
 // is the row's last 8 elements shifted into place, so that nothing outside the
 // operand is read and what lies behind k is zero.
 //
+// A gated layer's tile has 64 gates and then their 64 values among B's rows.
+//
 // Bound: the loads' time, which one k tile's MFMAs (0.25 us) do not cover: a
 // workgroup alone on its CU takes 0.7 us a k tile, two share one better.  8
 // groups of 512 rows, 1024 -> 1024: forward 22 us (383 TFLOP/s), input gradient

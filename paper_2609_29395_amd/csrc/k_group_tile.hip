@@ -24,13 +24,20 @@
 // The MFMA takes B fragments as its first operand, so that a lane holds four
 // consecutive columns of one row of the result.
 //
+// A gated layer's tile has 128 gates in B's first half and their values in its
+// second, so that a lane's sums are pairs; 128 outputs.  Its gradient is an input
+// gradient whose results are multiplied by the pairs' derivatives.
+//
 // Bound: the matrix cores, at a clock that their power brings down to 1.5 to
 // 1.8 GHz.  A k tile's two phases for both teams take about 2,270 cycles where
 // the MFMAs alone take 2,048; a tile has about 10 us besides (offsets and first
 // copies, results).  Even groups, 32,768 rows of 16, 4096 -> 4096: forward 844
 // us (1,303 TFLOP/s), input gradient 819 (1,342), weight gradient 1,033 (1,064;
 // 1.07 GB of fp32 results take 240 by themselves).  Ragged groups leave a last
-// round partly empty: forward 937.
+// round partly empty: forward 937.  Gated, 16,384 rows, 4096 -> 4096: 820 to 840 us
+// (1,310 to 1,340 TFLOP/s), 860 to 885 with the pairs kept; its gradient 483 to 500,
+// where an input gradient takes 413 to 428: the pairs are read and written (0.54 GB)
+// while no MFMA runs, as one workgroup fills a CU.
 #include "group.h"
 
 namespace {
