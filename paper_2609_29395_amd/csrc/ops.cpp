@@ -335,6 +335,7 @@ extern "C" int gcpsl_group_residual_norm(int32_t dtype, int32_t G, int64_t rows,
                                          void *stream) {
   gcpsl_clear_error();
   CHECK(bad_residual(dtype, G, rows, n, offsets));
+  if (rows > kMaxGroupRows) return fail(GCPSL_EUNSUPPORTED, "more than 2^31 - 1024 grouped rows");
   const size_t e = elem_bytes(dtype);
   CHECK(bad_tensor(x, e, rows, n, ldx, false));
   if (rows > 0 && !y && (gate || w_block || out || alpha != 1.0))

@@ -87,7 +87,11 @@ def test_too_many_rows_or_workgroups_are_refused():
     assert call("gcpsl_group_gated_forward", GATED, rows=2 ** 31 - 1) == g.EUNSUPPORTED
     assert call("gcpsl_group_gated_forward", GATED, rows=2 ** 31 - 2048, n=2 ** 27, k=1, ldy=2 ** 31 - 1,
                 ldpre=2 ** 31 - 1) == g.EUNSUPPORTED
+    assert call("gcpsl_group_residual_norm", NORM, rows=2 ** 31 - 1) == g.EUNSUPPORTED
     assert call("gcpsl_group_residual_norm_grad", NORM_GRAD, rows=2 ** 31 - 1) == g.EUNSUPPORTED
+    assert call("gcpsl_group_residual_norm_grad", NORM_GRAD, rows=1, n=2 ** 28, G=1024, ldo=2 ** 28, ldgo=2 ** 28,
+                ldgh=2 ** 28, lddx=2 ** 28, lddy=2 ** 28, lddgate=2 ** 28, dw_block_gs=2 ** 28,
+                dw_next_gs=2 ** 28) == g.EUNSUPPORTED
 
 
 @built

@@ -59,12 +59,16 @@ def run_both(z, cls, val, temperature, labels, what=""):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,L,top", [(1, 1, 1), (3, 2, 2), (40, 10, 5), (17, 64, 64), (5, 65, 3), (9, 100, 100),
                                         (33, 777, 20), (6, 1024, 32), (4, 1025, 256), (7, 2049, 8), (3, 5003, 17),
-                                        (1, 50021, 20), (2, 131072, 64), (1100, 300, 4), (600, 2100, 5)])
+                                        (1, 50021, 20), (2, 131072, 64), (1100, 300, 4), (600, 2100, 5), (50, 150, 256),
+                                        (70, 30, 200)])
 def test_sizes(rows, L, top, dtype):
     for i, (temperature, labelled) in enumerate([(1.0, True), (2.0, True), (0.5, False), (1.0, False)]):
         if rows * L > 100000 and i > 1:
             continue
         z, cls, val, labels = inputs(100 + i, rows, L, top, TYPES[dtype], masked=i % 2 == 1)
+        if top > L:  # more entries than classes: some again
+            again = torch.arange(top) % L
+            cls, val = cls[:, again].contiguous(), (val[:, again] - 0.5 * (torch.arange(top) // L)).contiguous()
         run_both(z, cls, val, temperature, labels if labelled else None, (temperature, labelled))
 
 
