@@ -170,6 +170,7 @@ template <typename T, bool HELD> struct Cols {
         else v[j] = 0;
       }
   }
+  // 0 for what is not its own: an infinite one times a cleared value would be NaN.
   __device__ __forceinline__ void load_weights(const float *p, float (&w)[VEC]) const {
     if (HELD || i + VEC <= n) {
 #pragma unroll
@@ -178,6 +179,10 @@ template <typename T, bool HELD> struct Cols {
 #pragma unroll
         for (int r = 0; r < 4; ++r) w[j + r] = v[r];
       }
+      if (HELD && __builtin_expect(drop > 0, 0))  // (a branch, so that no other thread waits for the loads here)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+          if (j < drop) w[j] = 0.f;
     } else {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) w[j] = i + j < n ? p[i + j] : 0.f;
@@ -538,7 +543,8 @@ __global__ void __launch_bounds__(block_of(TPR), TPR < 64 ? 3 : 4) residual_grad
       float s[3] = {0.f, 0.f, 0.f};
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        cols(v).clear(now[v].gh);  // (then every sum's terms are 0)
+        cols(v).clear(now[v].gh);  // (then every sum's terms are 0, those of an infinite g_out too)
+        cols(v).clear(now[v].go);
         if (BLOCK) cols(v).clear(now[v].y);
         grad_sums<BLOCK, T>(a, now[v], b1[v], b2[v], r, s);
       }

@@ -131,6 +131,24 @@ def test_nans_stay_in_their_rows(act):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("counts,n,k", [([5, 0, 70], 130, 67), ([700, 0, 1, 1300], 264, 131), ([16] * 16, 72, 501),
+                                        ([3], 10, 3), ([1, 1], 300, 258)])
+def test_infinities_at_the_products_end(counts, n, k, dtype):
+    """An infinite value in the last column makes its row's sums infinite, an infinite weight its column's: none is NaN."""
+    off, o, x, w, b, dz, v, pre = inputs(550, counts, n, k, TYPES[dtype])
+    x[0, k - 1] = float("inf")
+    w[-1, 1, k - 1] = -float("inf")
+    p = gcpsl.group_gated_forward(gpu(x), o, gpu(w), keep=True).pre.cpu()
+    want = torch.zeros(p.shape, dtype=torch.bool)
+    want[0] = want[off[-2]:off[-1], 1] = True
+    assert not torch.isnan(p).any() and torch.equal(torch.isinf(p), want)
+    dz[0, k - 1] = float("inf")
+    d = gcpsl.group_gated_grad(gpu(dz), o, gpu(v), gpu(pre), act="silu").cpu()
+    assert torch.equal(torch.isinf(d).nonzero()[:, 0].unique(), torch.tensor([0])) and not torch.isnan(d).any()
+    assert torch.isinf(d[0]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_shared_weights(dtype):
     """A group stride of 0: every group the same weights; their gradient is the groups' sum."""
     T, counts, n, k = TYPES[dtype], [30, 0, 41], 24, 40

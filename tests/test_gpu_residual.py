@@ -171,6 +171,30 @@ def test_rows_of_zeros_nans_and_far_values():
     assert torch.isnan(res.dw_next[1]).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [13, 43, 1003, 4099, 9001])
+def test_infinities_near_a_rows_end(n, dtype):
+    """An infinite weight or gradient gives what the formula does, also where the row's last vector overlaps the one before."""
+    off, o, t = inputs(650, [3, 2], n, TYPES[dtype])
+    col = n - (8 if dtype == "bf16" else 4)
+    t["w_block"][1, col] = float("inf")
+    t["y"][:, col] = 1.0
+    w = {k: gpu(t[k]) for k in ("y", "gate", "w_block", "w_next")}
+    got = gcpsl.group_residual_norm(gpu(t["x"]), o, **w)
+    want, _ = blocks.residual(t["x"], off, t["y"], t["gate"], t["w_block"], t["w_next"])
+    assert (want["r_next"][0][3:] == 0).all()
+    assert torch.equal(got.h.cpu()[3:].double().nan_to_num(7.0), want["h"][0][3:].nan_to_num(7.0))
+    t["w_block"][1, col] = 1.0
+    t["g_out"][4, col] = -float("inf")
+    r1 = got.r_block
+    res = gcpsl.group_residual_norm_grad(got.out, o, g_out=gpu(t["g_out"]), y=w["y"], w_block=gpu(t["w_block"]), r_block=r1)
+    want, _ = blocks.residual_grad(got.out.cpu(), off, t["g_out"], y=t["y"], w_block=t["w_block"], r_block=r1.cpu())
+    far = want["dy"][0][4]
+    assert torch.isinf(far).sum() == n - 1 and torch.isnan(far[col])
+    assert torch.equal(res.dy.cpu()[4].double().nan_to_num(7.0), far.nan_to_num(7.0))
+    assert torch.isfinite(res.dx.cpu()[4]).sum() == n - 1 and torch.isfinite(res.dy.cpu()[:4]).all()
+
+
 def test_no_rows():
     x, o = torch.zeros(0, 40, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
     w = torch.ones(3, 40, device="cuda")
