@@ -11,9 +11,17 @@
 // Two 24 KB buffers; two workgroups share a CU and one's splitting overlaps the
 // other's MFMAs.
 //
-// A gated layer's tile has 64 gates and then their 64 values among B's rows.  3,001
-// rows of 5 groups, 501 -> 333, gelu, pairs kept: 35 us; its gradient on 8,192 rows of 8
-// ragged groups, 1024 <- 1024, 137 us (125 TFLOP/s).
+// A gated layer's tile has 64 gates and then their 64 values among B's rows.  Where
+// its tiles, or its gradient's, are at most one a CU, two teams of four waves share a
+// tile's sum, every second k tile a team's, as two workgroups of a CU would share its
+// matrix cores; with more tiles those do, and the teams' join costs (us with and
+// without teams, all groups even):
+//   2,000 rows of 4 groups, 1024 -> 512 (136 tiles), 34.0 and 48.5; 3,001 of 5, 501 ->
+//   333 (150), 29.0 and 32.9; 2,048 of 1, 4096 -> 1024 (256), 175 and 183; 6,500 of 3,
+//   1024 -> 512 (416), 90.6 and 86.0; 16,384 of 16, 512 -> 512 (1,088), 114 and 101;
+//   gradients: 3,000 rows of 16 groups, 600 <- 600 (155), 33.5 and 41.5; 667 of 6,
+//   4096 <- 4096 (256), 175 and 224; 6,000 of 4, 500 <- 700 (288), 54.8 and 47.3.
+// Gradient of 8,192 rows of 8 ragged groups, 1024 <- 1024, 137 us (125 TFLOP/s).
 //
 // Bound: what a k tile costs beside its MFMAs, which the matrix cores are busy
 // with 32 to 35 % of a launch: every value is split by each tile that reads it,
@@ -40,7 +48,7 @@ __device__ __forceinline__ int at(int r, int c) { return r * 32 + ((c ^ ((r >> 3
 // columns past the n inside are taken as the last ones inside (what they give
 // is not stored), so that loads need no test: a thread whose columns pass the
 // end takes the last two instead.
-template <bool T, int ROWS = 2> struct Stage {
+template <bool T, int ROWS = 2, int TEAMS = 1> struct Stage {
   const char *base;  // of the next tile
   int64_t step;
   int row, chunk;                // first row (T: column) in LDS, 16-byte piece
@@ -49,10 +57,11 @@ template <bool T, int ROWS = 2> struct Stage {
   float v[J][8];                 // [row or column][k]
 
   // pair: rows from the gates' to the values' of a gated layer, the second of a thread's rows (0: none)
-  __device__ __forceinline__ void init(const float *p, int64_t ld_, int n, int t, int pair = 0) {
-    base = (const char *)p;
-    ld = (uint32_t)ld_ * 4u;
+  __device__ __forceinline__ void init(const float *p, int64_t ld_, int n, int t, int team, int pair = 0) {
     step = T ? ld_ * (4 * BK) : 4 * BK;
+    base = (const char *)p + (TEAMS > 1 ? team * step : 0);
+    step *= TEAMS;
+    ld = (uint32_t)ld_ * 4u;
     if constexpr (T) {
       chunk = t >> 6;
       row = min((t & 63) * 2, n - 2);  // -1 in a tile of one column, which is not the first
@@ -104,6 +113,11 @@ template <bool T, int ROWS = 2> struct Stage {
           v[j][i] = in ? x : 0.f;
         }
       }
+    } else if (TEAMS > 1) {  // (a team's last tile is written also where all of it is past the sum's end)
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[j][i] = 0.f;
     }
   }
   // splits the values and writes them; returns the largest magnitude so far
@@ -134,11 +148,16 @@ struct Tile {
   bool sums;  // of A's columns, too (the bias gradient)
 };
 
-// The tile's sums and results; waves of 32 FJ x 64 outputs.
-template <int MODE, int FJ>
-__device__ __forceinline__ void group_f32_tile(const GroupArgs &a, const Tile &t, char *lds) {
+// The tile's sums and results; waves of 32 FJ x 64 outputs.  TEAMS of four waves share
+// the sum, every k tile a team's, with buffers of its own.
+template <int MODE, int FJ, int TEAMS>
+__device__ __forceinline__ void group_f32_tile(const GroupArgs &a, const Tile &t, char *all_lds) {
   constexpr bool AT = MODE == GROUP_DW, BT = group_across(MODE), PAIR = MODE == GROUP_GATED;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  static_assert(TEAMS == 1 || MODE != GROUP_DW, "");
+  const int tid = TEAMS > 1 ? threadIdx.x & 255 : threadIdx.x, lane = tid & 63;
+  const int team = TEAMS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
+  char *const lds = all_lds + team * (2 * BUFFER);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1, li = lane & 31, lg = lane >> 5;
   const float *const A = t.A, *const B = t.B;
   const int g = t.g, row0 = t.row0, rows = t.rows, c0 = t.c0, cols = t.cols, Q = t.Q, slot = t.slot;
@@ -156,6 +175,8 @@ __device__ __forceinline__ void group_f32_tile(const GroupArgs &a, const Tile &t
       for (int r = 0; r < 16; ++r) big[i][j][r] = small[i][j][r] = 0.f;
   float top = 0.f, colsum[2] = {0.f, 0.f};
 
+  constexpr int KT = TEAMS * BK;  // k of a tile of every team
+  const int own = team * BK;
   const auto run = [&](auto &stage, bool is_a) {
     char *const mine = lds + (is_a ? 0 : 3 * PLANE);
     const auto write = [&](int p) {  // to buffer p
@@ -183,9 +204,9 @@ __device__ __forceinline__ void group_f32_tile(const GroupArgs &a, const Tile &t
       if constexpr (decltype(all)::value) {
         write(1 - p);
         stage.load_all();
-      } else if (Q - k0 > BK) {
+      } else if (Q - k0 > KT) {
         write(1 - p);
-        stage.load(Q - k0 - 2 * BK);
+        stage.load(Q - k0 - 2 * KT - own);
       }
       // term by term, so that a sum's next product is four MFMAs away
       constexpr int kw[6] = {2, 0, 1, 1, 0, 0}, kx[6] = {0, 2, 1, 0, 1, 0};
@@ -200,26 +221,26 @@ __device__ __forceinline__ void group_f32_tile(const GroupArgs &a, const Tile &t
           }
       __syncthreads();
     };
-    stage.load(Q);
+    stage.load(Q - own);
     if (Q > 0) write(0);
-    stage.load(Q - BK);
+    stage.load(Q - KT - own);
     __syncthreads();
     int k0 = 0, p = 0;
-    for (; k0 + 3 * BK <= Q; k0 += BK, p ^= 1) tile(k0, p, std::true_type{});
-    for (; k0 < Q; k0 += BK, p ^= 1) tile(k0, p, std::false_type{});
+    for (; k0 + 3 * KT <= Q; k0 += KT, p ^= 1) tile(k0, p, std::true_type{});
+    for (; k0 < Q; k0 += KT, p ^= 1) tile(k0, p, std::false_type{});
   };
   if constexpr (AT == BT) {
-    Stage<AT> stage;
-    if (wave < 2) stage.init(A, a.lda, rows, tid);
-    else stage.init(B, a.ldb, cols, tid - 128, PAIR ? a.N : 0);
+    Stage<AT, 2, TEAMS> stage;
+    if (wave < 2) stage.init(A, a.lda, rows, tid, team);
+    else stage.init(B, a.ldb, cols, tid - 128, team, PAIR ? a.N : 0);
     run(stage, wave < 2);
   } else if (wave < 2) {
-    Stage<AT, FJ> stage;
-    stage.init(A, a.lda, rows, tid);
+    Stage<AT, FJ, TEAMS> stage;
+    stage.init(A, a.lda, rows, tid, team);
     run(stage, true);
   } else {
-    Stage<BT> stage;
-    stage.init(B, a.ldb, cols, tid - 128);
+    Stage<BT, 2, TEAMS> stage;
+    stage.init(B, a.ldb, cols, tid - 128, team);
     run(stage, false);
   }
 
@@ -231,7 +252,7 @@ __device__ __forceinline__ void group_f32_tile(const GroupArgs &a, const Tile &t
       for (int j = 0; j < FJ; ++j)
 #pragma unroll
         for (int r = 0; r < 16; ++r) big[i][j][r] = small[i][j][r] = 0.f;
-    for (int k0 = 0; k0 < Q; k0 += 2) {
+    for (int k0 = 2 * team; k0 < Q; k0 += 2 * TEAMS) {
       const int k = k0 + lg;
       float x[FJ], w[2];
 #pragma unroll
@@ -248,12 +269,14 @@ __device__ __forceinline__ void group_f32_tile(const GroupArgs &a, const Tile &t
   }
 
   // The results go through LDS, the rows of two waves (32 FJ of 512 bytes) at a
-  // time, so that whole rows of the tile are written at once.
-  const auto place = [&](int r, int c) { return lds + r * 512 + ((c >> 2) ^ ((r & 15) << 1)) * 16; };
+  // time, so that whole rows of the tile are written at once, by all teams.
+  const auto place = [&](int r, int c, int of = 0) {
+    return all_lds + of * (2 * BUFFER) + r * 512 + ((c >> 2) ^ ((r & 15) << 1)) * 16;
+  };
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    constexpr int LANES = group_outputs(MODE, BN) / 4, STEP = 256 / LANES, ROWS = 32 * FJ / STEP;
-    const int m0 = h * 32 * FJ, r0 = tid / LANES, c4 = tid % LANES * 4;
+    constexpr int LANES = group_outputs(MODE, BN) / 4, STEP = 256 * TEAMS / LANES, ROWS = 32 * FJ / STEP;
+    const int m0 = h * 32 * FJ, r0 = threadIdx.x / LANES, c4 = threadIdx.x % LANES * 4;
     if (m0 >= rows) break;
     using Finish = std::conditional_t<group_is_pair(MODE), FinishPairs<float, MODE, ROWS>,
                                       FinishRows<float, MODE == GROUP_DX ? GROUP_DX : GROUP_FWD, ROWS>>;
@@ -269,16 +292,19 @@ __device__ __forceinline__ void group_f32_tile(const GroupArgs &a, const Tile &t
             f32x4_t v;
 #pragma unroll
             for (int r = 0; r < 4; ++r) v[r] = big[i][j][4 * q + r] + small[i][j][4 * q + r];
-            *(f32x4_t *)place(j * 32 + li, wn * 64 + i * 32 + 8 * q + 4 * lg) = v;
+            *(f32x4_t *)place(j * 32 + li, wn * 64 + i * 32 + 8 * q + 4 * lg, team) = v;
           }
     __syncthreads();
-    const auto sum = [&](int i, int) { return *(const f32x4_t *)place(r0 + 8 * i, c4); };
+    const auto sum = [&](int i, int, int half = 0) {
+      const int r = r0 + STEP * i, c = half * (BN / 2) + c4;
+      f32x4_t v = *(const f32x4_t *)place(r, c);
+      if constexpr (TEAMS > 1) v += *(const f32x4_t *)place(r, c, 1);
+      return v;
+    };
     if constexpr (MODE == GROUP_DW) {
       if (c0 + c4 < a.N)
         for (int i = 0; i < 4 * FJ && m0 + r0 + 8 * i < rows; ++i)
           store_grad(a, g, slot, row0 + m0 + r0 + 8 * i, c0 + c4, sum(i, 0));
-    } else if constexpr (group_is_pair(MODE)) {
-      out.store(a, [&](int i, int, int half) { return *(const f32x4_t *)place(r0 + STEP * i, half * (BN / 2) + c4); });
     } else {
       out.store(a, sum);
     }
@@ -296,11 +322,13 @@ __device__ __forceinline__ void group_f32_tile(const GroupArgs &a, const Tile &t
   }
 }
 
-template <int MODE>
-__global__ void __launch_bounds__(256, 2) group_f32_kernel(GroupArgs a, int NT) {
+template <int MODE, int TEAMS>
+__global__ void __launch_bounds__(256 * TEAMS, 2) group_f32_kernel(GroupArgs a, int NT) {
   constexpr bool BT = group_across(MODE);
   constexpr int COLS = group_outputs(MODE, BN);
-  __shared__ __attribute__((aligned(16))) char lds[2 * BUFFER];
+  extern __shared__ __attribute__((aligned(16))) char teams_lds[];
+  __shared__ __attribute__((aligned(16))) char own_lds[TEAMS > 1 ? 16 : 2 * BUFFER];
+  char *const lds = TEAMS > 1 ? teams_lds : own_lds;
   Tile t{(const float *)a.a, (const float *)a.b, 0, 0, 0, 0, 0, a.Q, -1, false};
   int nt;
   if constexpr (MODE == GROUP_DW) {
@@ -325,8 +353,8 @@ __global__ void __launch_bounds__(256, 2) group_f32_kernel(GroupArgs a, int NT) 
   }
   t.cols = min(COLS, a.N - t.c0);
   t.sums = MODE == GROUP_DW && a.db != nullptr && nt == 0;
-  if (MODE != GROUP_DW && t.rows <= BM / 2) group_f32_tile<MODE, 1>(a, t, lds);
-  else group_f32_tile<MODE, 2>(a, t, lds);
+  if (MODE != GROUP_DW && t.rows <= BM / 2) group_f32_tile<MODE, 1, TEAMS>(a, t, lds);
+  else group_f32_tile<MODE, 2, TEAMS>(a, t, lds);
 }
 
 template <int MODE> hipError_t run_mode(const GroupArgs &a, hipStream_t s) {
@@ -334,8 +362,23 @@ template <int MODE> hipError_t run_mode(const GroupArgs &a, hipStream_t s) {
   const int64_t NT = (a.N + COLS - 1) / COLS;
   const int64_t blocks = MODE == GROUP_DW ? piece_blocks(a, (int64_t)((a.M + BM - 1) / BM) * NT)
                                           : tile_blocks(a.M, a.G, BM, NT);
+  if constexpr (group_is_pair(MODE)) {
+    constexpr int LDS_BYTES = 4 * BUFFER;
+    // a group's last tile half full on average
+    if (((int64_t)a.M + 64 * a.G) / BM * NT <= kCUs && blocks <= kMaxBlocks / 2) {
+      static PerDeviceOnce once;
+      if (once.needed()) {
+        const hipError_t e = hipFuncSetAttribute((const void *)group_f32_kernel<MODE, 2>,
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES);
+        if (e != hipSuccess) return e;
+        once.mark();
+      }
+      hipLaunchKernelGGL((group_f32_kernel<MODE, 2>), dim3((uint32_t)blocks), dim3(512), LDS_BYTES, s, a, (int)NT);
+      return hipGetLastError();
+    }
+  }
   if (blocks > kMaxBlocks) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL(group_f32_kernel<MODE>, dim3((uint32_t)blocks), dim3(256), 0, s, a, (int)NT);
+  hipLaunchKernelGGL((group_f32_kernel<MODE, 1>), dim3((uint32_t)blocks), dim3(256), 0, s, a, (int)NT);
   return hipGetLastError();
 }
 

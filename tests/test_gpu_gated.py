@@ -58,6 +58,12 @@ def test_many_tiles(counts, n, k, m, dtype):
     check_both(*inputs(350, counts, n, k, TYPES[dtype], m), "silu")
 
 
+@pytest.mark.parametrize("k", [1, 15, 16, 17, 31, 32, 33, 47, 48, 49, 64, 65, 95, 96, 97])
+def test_sums_shared_by_two_teams(k):
+    """Fewer tiles than compute units, whose k tiles two teams of waves take in turn: sums that end in either's."""
+    check_both(*inputs(370, [700, 0, 1, 1300], 600, k, torch.float32), ACTS[k % 3])
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rest", range(8))
 @pytest.mark.parametrize("counts,n,k", [([5, 0, 70], 128, 64), ([200, 131], 72, 136), ([129], 8, 200)])
@@ -132,7 +138,7 @@ def test_nans_stay_in_their_rows(act):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("counts,n,k", [([5, 0, 70], 130, 67), ([700, 0, 1, 1300], 264, 131), ([16] * 16, 72, 501),
-                                        ([3], 10, 3), ([1, 1], 300, 258)])
+                                        ([700, 0, 1, 1300], 600, 67), ([3], 10, 3), ([1, 1], 300, 258)])
 def test_infinities_at_the_products_end(counts, n, k, dtype):
     """An infinite value in the last column makes its row's sums infinite, an infinite weight its column's: none is NaN."""
     off, o, x, w, b, dz, v, pre = inputs(550, counts, n, k, TYPES[dtype])
