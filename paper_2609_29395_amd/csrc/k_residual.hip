@@ -83,7 +83,9 @@ template <int TPR, int N> __device__ __forceinline__ void row_sum(float (&v)[N],
   }
 }
 
-// Groups of rows: the first 64 groups' bounds stay in the lanes.
+// Groups of rows: the first 64 groups' bounds stay in the lanes, a group a lane.  So
+// all 64 lanes have to be active in every lookup, those too that have no row (any
+// row will do for them): a group whose lane is switched off would not be seen.
 struct Finder {
   const int32_t *off;
   int G, rows, begin, end;
@@ -252,7 +254,7 @@ __global__ void __launch_bounds__(block_of(TPR)) residual_kernel(ResidualArgs a,
 #pragma unroll
     for (int v = 0; v < NV; ++v) now[v] = next[v];
     if (first + R < r1) load(min(row + R, r1 - 1), next);
-    const int g = row < r1 ? finder.of_lane_rows<TPR>(row) : finder.of_lane_rows<TPR>(r1 - 1);
+    const int g = finder.of_lane_rows<TPR>(min(row, r1 - 1));
     const bool live = row < r1 && g >= 0;
     if (g >= 0 && g != held) {
 #pragma unroll
