@@ -393,6 +393,7 @@ extern "C" int gcpsl_group_residual_norm_grad(
   CHECK(bad_residual(dtype, G, rows, n, offsets));
   if (rows > kMaxGroupRows) return fail(GCPSL_EUNSUPPORTED, "more than 2^31 - 1024 grouped rows");
   const size_t e = elem_bytes(dtype);
+  if (g_h && !w_next) return fail(GCPSL_EINVAL, "g_h without w_next");  // (the weights' gradients without rows, too)
   if (rows > 0) {
     if (!g_out && !g_h) return fail(GCPSL_EINVAL, "no gradient given");
     if (!g_h != !w_next || (g_h && (!r_next || !out))) return fail(GCPSL_EINVAL, "g_h, w_next, r_next and out come together");
