@@ -321,9 +321,10 @@ template <typename T> __global__ void __launch_bounds__(256) residual_long_kerne
   const int t = threadIdx.x, n = a.n;
   const Finder finder(a.off, a.G, (int)a.rows);
   int parity = 0;
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, parity ^= 1) {
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const int g = finder.of((int)row);
     if (g < 0) continue;
+    parity ^= 1;  // (of the rows that are taken: two in turn must not share a buffer, as only one of the sums may be asked for)
     const T *x = (const T *)a.x + row * a.ldx, *y = (const T *)a.y + row * a.ldy, *gate = (const T *)a.gate + row * a.ldg;
     const float *w1 = a.w_block ? a.w_block + g * a.wb_gs : nullptr, *w2 = a.w_next ? a.w_next + g * a.wn_gs : nullptr;
     const auto each = [&](auto f) {
