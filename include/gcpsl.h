@@ -463,7 +463,9 @@ int gcpsl_timing_read(gcpsl_ctx *ctx, gcpsl_kernel_stat *out, int32_t cap, int32
  * arguments, so that it may be captured in a graph.  No rows is a valid
  * call.  EINVAL on a bad argument, EHIP on a failed launch, EUNSUPPORTED where
  * a grouped product's one launch would need 2^32 threads (256 or 512 for every
- * tile that any offsets can make) or rows pass 2^31 - 1024.
+ * tile that any offsets can make), where a residual norm's gradient has 2^30
+ * weights or more in its G groups (n taken up to a multiple of 64), or where
+ * grouped rows pass 2^31 - 1024.
  *
  * Grouped rows: offsets is a device array [G + 1], 1 <= G <= 1024; rows
  * [offsets[g], offsets[g + 1]) belong to group g, 0 <= offsets[0] <= ... <=

@@ -726,7 +726,7 @@ int grad_threads(int dtype, int n) {
 
 template <typename T, bool BLOCK> hipError_t run_grad(int dtype, const ResidualGradArgs &a, hipStream_t s) {
   const int64_t blocks = a.rows / a.piece + a.G, joins = (2 * (int64_t)a.n + kJoinCols - 1) / kJoinCols * a.G;
-  if (std::max(blocks, joins) > kMaxBlocks / 4) return hipErrorInvalidConfiguration;  // (of up to 1,024 threads)
+  if (blocks > kMaxBlocks / 4 || joins > kMaxBlocks) return hipErrorInvalidConfiguration;  // (of up to 1,024 threads; 256)
   const int tpr = grad_threads(dtype, a.n);
   const auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(block_of(tpr)), 0, s, a);
@@ -752,7 +752,7 @@ template <typename T, bool BLOCK> hipError_t run_grad(int dtype, const ResidualG
     const auto join = [&](auto kernel, int lanes) {
       hipLaunchKernelGGL(kernel, dim3((uint32_t)joins), dim3(kJoinCols / 4 * lanes), 0, s, a, (uint32_t)(joins / a.G));
     };
-    if (a.slots >= 64 * a.G) join(residual_join_kernel<32>, 32);
+    if (a.slots >= 64 * a.G && joins <= kMaxBlocks / 4) join(residual_join_kernel<32>, 32);
     else join(residual_join_kernel<8>, 8);
     e = hipGetLastError();
   }
