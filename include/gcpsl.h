@@ -553,7 +553,8 @@ int gcpsl_group_gated_grad(int32_t dtype, int32_t G, int64_t rows, int32_t m, in
  * the next block, r_next not written.  y NULL: the norm alone, out = x, not
  * written: gate, w_block and out NULL and alpha 1.  out may be x (ldo = ldx).
  * alpha and beta are finite, 2^-100 <= eps <= 2^100; 1 <= n <= 2^28.  Squares are
- * summed in fp32: a row with values of 2^63 or more may have r = 0.
+ * summed in fp32: a row whose squares add up to 2^128 or more (values of 2^58
+ * where n is 4,096) has r = 0.
  */
 int gcpsl_group_residual_norm(int32_t dtype, int32_t G, int64_t rows, int32_t n, const int32_t *offsets, const void *x,
                               int64_t ldx, const void *y, int64_t ldy, const void *gate, int64_t ldgate,
@@ -639,9 +640,11 @@ int gcpsl_score_grad(int32_t dtype, int64_t rows, int32_t L, const void *z, int6
  * and, as gcpsl_score has them, logp of the row's label and lse (T = 1).  Entries
  * of a class outside [0, L) are left out, as are those of value -inf; a row
  * without any left has kl 0.  A class given twice counts with both entries.  A
- * class that the row rules out (-inf) and the teacher does not makes kl +inf, a
- * NaN or +inf among a row's logits or the entries left makes it NaN.  1 <= top
- * <= 256, 2^-10 <= T <= 2^10, 1 <= L <= 2^28.  kl, lse_t, logp and lse may be NULL
+ * class that the row rules out (-inf) and the teacher gives a weight makes kl
+ * +inf; a NaN or +inf among a row's logits or the entries left makes it NaN.  An
+ * entry 88 T or more below the row's best one has no weight in fp32, here and in
+ * the gradient, and adds nothing.  1 <= top <= 256, 2^-10 <= T <= 2^10, 1 <= L <=
+ * 2^28.  kl, lse_t, logp and lse may be NULL
  * (labels too if logp is).  The summation order depends on dtype, rows, L and the
  * row's address modulo 16.  workspace: gcpsl_distill_workspace_bytes() bytes on
  * the device, 16-byte aligned (NULL if that is 0), used until the call's work on
