@@ -21,7 +21,8 @@
 //   1024 -> 512 (416), 90.6 and 86.0; 16,384 of 16, 512 -> 512 (1,088), 114 and 101;
 //   gradients: 3,000 rows of 16 groups, 600 <- 600 (155), 33.5 and 41.5; 667 of 6,
 //   4096 <- 4096 (256), 175 and 224; 6,000 of 4, 500 <- 700 (288), 54.8 and 47.3.
-// Gradient of 8,192 rows of 8 ragged groups, 1024 <- 1024, 137 us (125 TFLOP/s).
+// Gradient of 8,192 rows of 8 groups, 1024 <- 1024: even 109 us (157 TFLOP/s), ragged
+// 137 to 150 by card (125 to 114).
 //
 // Bound: what a k tile costs beside its MFMAs, which the matrix cores are busy
 // with 32 to 35 % of a launch: every value is split by each tile that reads it,

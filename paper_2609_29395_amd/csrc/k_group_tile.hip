@@ -34,10 +34,10 @@
 // copies, results).  Even groups, 32,768 rows of 16, 4096 -> 4096: forward 844
 // us (1,303 TFLOP/s), input gradient 819 (1,342), weight gradient 1,033 (1,064;
 // 1.07 GB of fp32 results take 240 by themselves).  Ragged groups leave a last
-// round partly empty: forward 937.  Gated, 16,384 rows, 4096 -> 4096: 820 to 840 us
-// (1,310 to 1,340 TFLOP/s), 860 to 885 with the pairs kept; its gradient 483 to 500,
-// where an input gradient takes 413 to 428: the pairs are read and written (0.54 GB)
-// while no MFMA runs, as one workgroup fills a CU.
+// round partly empty: forward 937.  Gated, 16,384 rows, 4096 -> 4096, by card: 820 to 890
+// us (1,340 to 1,235 TFLOP/s), 860 to 920 with the pairs kept; its gradient 483 to
+// 508, where an input gradient takes 413 to 428: the pairs are read and written (0.54
+// GB) while no MFMA runs, as one workgroup fills a CU.
 #include "group.h"
 
 namespace {

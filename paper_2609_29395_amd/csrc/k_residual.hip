@@ -17,10 +17,13 @@
 // weights' gradients are summed by the threads over the rows of a piece of a
 // group; pieces are joined in their order by a second kernel.
 //
-// Bound: memory.  bf16, n 4,096: 32,768 rows of 16 groups 268 us (5.0 TB/s), norms
-// alone 5.4 TB/s; the gradient of 16,384 rows 237 us (4.5), of the norm alone 90
-// (4.5).  A row's instructions, about 60 an element in the gradient, take nearly as
-// long: sigmoids are taken twice, once for the sums and once for the results.
+// Bound: memory.  bf16, n 4,096: 32,768 rows of 16 groups 268 to 274 us by card (5.0 to
+// 4.9 TB/s), norms alone 5.4 TB/s; the gradient of 16,384 rows 237 us (4.5), of the
+// norm alone 90 (4.5).  A row's instructions, about 60 an element in the gradient,
+// take nearly as long: sigmoids are taken twice, once for the sums and once for the
+// results.  Rows of four or two a wave, 16 groups: 2,048 of n 64 5.4 us in either type,
+// which is the launch; 1,000,000 in fp32 275 (4.7 TB/s) and in bf16 224 (2.9, as half
+// the lanes hold no vector of such rows); 262,144 of n 256, bf16, 141 (4.8).
 #include <algorithm>
 
 #include "group.h"
@@ -768,7 +771,10 @@ template <typename T, bool BLOCK> hipError_t run_grad(int dtype, const ResidualG
 // together (65,536 rows of 8 groups, n 256, bf16: 58 and 55 us).  Smaller ones
 // cost more in partials (16,384 rows of 16 groups, n 4,096, bf16: 32 rows a piece
 // 237 us, 16 rows 248).  Four rows at least for each of those that a workgroup
-// takes at a time.
+// takes at a time; us with at least 2, 4 and 8: 777 rows of 7 groups, n 1,001, fp32,
+// 13.1, 13.9 and 17.7, n 4,096, bf16, 25.7, 22.5 and 27.2; 4,096 of 16, n 1,024, bf16,
+// 23.8, 21.4 and 23.8; 2,000 of 16, n 4,096, bf16, 37.7, 37.5 and 34.9; 16,384 of 16, n
+// 64, fp32, 11.4, 12.2 and 14.8.
 GroupPieces residual_pieces(int dtype, int G, int64_t rows, int n) {
   const int tpr = grad_threads(dtype, n);
   const int64_t block = tpr ? block_of(tpr) : 256, full = kCUs * 1024 / block * 15 / 16,
